@@ -9,12 +9,12 @@ to the even code, values past 6 saturate).  It is one byte buffer,
 [n_kv_heads][ctx_cap / 32] records of 34 * head_dim bytes for 32 slots each:
 
 - keys, 16 * hd bytes, [2 s][4 g][4 i][4 j][hd/32 u][4 c]: byte c holds the
-  elements 32u + 8g + 2c (low four bits) and 32u + 8g + 2c + 1 of slot
-  8i + 4s + j;
-- values, 16 * hd bytes, [hd/64 m][4 g][16 r][2 n][8 j]: a byte holds the
-  elements 32b + r (low) and 32b + 16 + r, b = 2m + n, of slot 8g + j;
-- key scales, hd bytes, [4 i][4 j][2 s][hd/32 u] (slot 8i + 4s + j);
-- value scales, hd bytes, [32 slots][hd/32 b].
+  elements d = g hd/4 + 8u + 2c (low four bits) and d + 1 of slot 8i + 4s + j;
+- values, 16 * hd bytes, [hd/64 m][4 g][hd/32 b][w r][2 n][8 j], w = 512 / hd:
+  a byte holds the elements d = 32b + w (4m + 2n) + r (low) and d + w of slot
+  8g + j;
+- key scales, hd bytes, [hd/32 b][4 i][4 j][2 s] (slot 8i + 4s + j);
+- value scales, hd bytes, [hd/32 b][32 slots].
 
 A case is one of the calls that a decoding program makes:
 
@@ -222,19 +222,19 @@ def _parts(cache):
     hd = cache.shape[-1] // 34
     lead, u = cache.shape[:2], hd // 32
     at = [0, 16 * hd, 32 * hd, 33 * hd, 34 * hd]
-    dims = [(2, 4, 4, 4, u, 4), (u // 2, 4, 16, 2, 8), (4, 4, 2, u), (4, 8, u)]
+    dims = [(2, 4, 4, 4, u, 4), (u // 2, 4, u, 16 // u, 2, 8), (u, 4, 4, 2), (u, 32)]
     return [cache[..., at[i] : at[i + 1]].unflatten(-1, dims[i]) for i in range(4)], lead, hd
 
 
 def _codes_of(cache):
     """Key and value codes [heads][slots][hd] and scale bytes [heads][slots][hd/32]."""
     (k, v, ks, vs), (heads, _), hd = _parts(cache)
-    k = k.permute(0, 1, 4, 2, 5, 6, 3, 7).reshape(heads, -1, hd // 2)
+    k = k.permute(0, 1, 4, 2, 5, 3, 6, 7).reshape(heads, -1, hd // 2)
     k = torch.stack((k & 15, k >> 4), -1).flatten(-2)
-    v = v.permute(0, 1, 3, 6, 2, 5, 4).reshape(heads, -1, hd // 32, 16)
-    v = torch.cat((v & 15, v >> 4), -1).flatten(-2)
-    ks = ks.permute(0, 1, 2, 4, 3, 5).reshape(heads, -1, hd // 32)
-    return k, ks, v, vs.reshape(heads, -1, hd // 32)
+    v = torch.stack((v & 15, v >> 4), -1)  # heads, tile, m, g, b, r, n, j, half
+    v = v.permute(0, 1, 3, 7, 4, 2, 6, 8, 5).reshape(heads, -1, hd)
+    ks = ks.permute(0, 1, 3, 5, 4, 2).reshape(heads, -1, hd // 32)
+    return k, ks, v, vs.transpose(-1, -2).reshape(heads, -1, hd // 32)
 
 
 def _store(cache, k4, v4, slot0):
@@ -242,21 +242,21 @@ def _store(cache, k4, v4, slot0):
     n = k4[0].shape[1]
     t0, t1 = slot0 // 32, (slot0 + n + 31) // 32
     part = cache[:, t0:t1]
-    k, ks, v, vs = _codes_of(part)
     at = slice(slot0 - 32 * t0, slot0 - 32 * t0 + n)
-    k[:, at], ks[:, at], v[:, at] = k4[0], k4[1], v4[0]
-    vs = vs.clone()
-    vs[:, at] = v4[1]
+    rows = _codes_of(part)
+    for held, new in zip(rows, (*k4, *v4)):
+        held[:, at] = new
+    k, ks, v, vs = rows
     (pk, pv, pks, pvs), (heads, tiles), hd = _parts(part)
     u = hd // 32
     k = k.unflatten(-1, (-1, 2))
-    k = (k[..., 0] | (k[..., 1] << 4)).reshape(heads, tiles, 4, 2, 4, u, 4, 4)
-    pk.copy_(k.permute(0, 1, 3, 6, 2, 4, 5, 7))
-    v = v.unflatten(-1, (u, 2, 16))
-    v = (v[..., 0, :] | (v[..., 1, :] << 4)).reshape(heads, tiles, 4, 8, u // 2, 2, 16)
-    pv.copy_(v.permute(0, 1, 4, 2, 6, 5, 3))
-    pks.copy_(ks.reshape(heads, tiles, 4, 2, 4, u).permute(0, 1, 2, 4, 3, 5))
-    pvs.copy_(vs.reshape(heads, tiles, 4, 8, u))
+    k = (k[..., 0] | (k[..., 1] << 4)).reshape(heads, tiles, 4, 2, 4, 4, u, 4)
+    pk.copy_(k.permute(0, 1, 3, 5, 2, 4, 6, 7))
+    v = v.reshape(heads, tiles, 4, 8, u, u // 2, 2, 2, 16 // u)  # g, j, b, m, n, half, r
+    v = v[..., 0, :] | (v[..., 1, :] << 4)
+    pv.copy_(v.permute(0, 1, 5, 2, 4, 7, 6, 3))
+    pks.copy_(ks.reshape(heads, tiles, 4, 2, 4, u).permute(0, 1, 5, 2, 4, 3))
+    pvs.copy_(vs.reshape(heads, tiles, 32, u).transpose(-1, -2))
 
 
 def _values(code, scale):
@@ -386,10 +386,13 @@ def _exact_slots(cache, slots, hd):
     s, d = slots[:, None], torch.arange(hd, device=slots.device)[None, :]
     rec, w, u = (s // 32) * (34 * hd), s % 32, hd // 32
     i, h, j = w // 8, w // 4 % 2, w % 4
-    kb = rec + ((((h * 4 + d // 8 % 4) * 4 + i) * 4 + j) * u + d // 32) * 4 + d % 8 // 2
-    ke = rec + 32 * hd + ((i * 4 + j) * 2 + h) * u + d // 32
-    vb = rec + 16 * hd + (((d // 64 * 4 + w // 8) * 16 + d % 16) * 2 + d // 32 % 2) * 8 + w % 8
-    ve = rec + 33 * hd + w * u + d // 32
+    g, rest = d // (hd // 4), d % (hd // 4)
+    kb = rec + ((((h * 4 + g) * 4 + i) * 4 + j) * u + rest // 8) * 4 + rest % 8 // 2
+    ke = rec + 32 * hd + ((d // 32 * 4 + i) * 4 + j) * 2 + h
+    wide = 16 // u
+    x, r = d % 32 // wide, d % wide  # x = 4m + 2n + half
+    vb = rec + 16 * hd + ((((x // 4 * 4 + w // 8) * u + d // 32) * wide + r) * 2 + x // 2 % 2) * 8 + w % 8
+    ve = rec + 33 * hd + d // 32 * 32 + w
     flat = cache.reshape(cache.shape[0], -1)
 
     def value(at, high, scale_at):
@@ -399,7 +402,7 @@ def _exact_slots(cache, slots, hd):
         x = torch.where(m < 2, m * 0.5, (1 + (m % 2) * 0.5) * torch.exp2((m // 2 - 1).double()))
         return torch.where(n < 8, x, -x) * torch.exp2(flat[:, scale_at].double() - 127)
 
-    return value(kb, (d % 2 == 1).expand_as(kb), ke), value(vb, (d // 16 % 2 == 1).expand_as(vb), ve)
+    return value(kb, (d % 2 == 1).expand_as(kb), ke), value(vb, (x % 2 == 1).expand_as(vb), ve)
 
 
 def exact(case, seed):
