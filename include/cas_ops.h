@@ -191,6 +191,85 @@ cas_status cas_op_gemm_qx(int32_t wtype, const int8_t* W, const float* ws, const
                           int32_t T, int32_t qmax, float* parts, void* work, size_t work_bytes, void* stream);
 
 /*
+ * The 4-bit KV cache (App. C: activation quantisation of the "(partial) KV
+ * cache"): rows appended to it, attended and read back by the three calls
+ * below.  Keys and values are microscaled floats (OCP MX, E2M1 elements): 32
+ * consecutive elements x of a token's head row share the scale 2^e, e =
+ * max(floor(log2 max|x|) - 2, -125), held as the byte e + 127, and an element
+ * is the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} to x / 2^e (codes 0-7, sign
+ * in bit 3; ties to the even code; saturating at 6).  A block that holds a NaN
+ * or an infinity has the scale byte 255 and reads as NaN.  Every value held is
+ * exact in bf16.
+ *   kv4: cas_op_kv4_bytes(...) bytes, 16-byte aligned: [n_kv_heads][ctx_cap /
+ *        32] records of 34 * head_dim bytes for 32 slots, in this order (hd =
+ *        head_dim, w = 512 / hd, the last index fastest):
+ *          16 hd  key codes [2 s][4 g][4 i][4 j][hd/32 u][4 c]: elements d =
+ *                 g hd/4 + 8u + 2c (low four bits) and d + 1 of slot 8i + 4s + j
+ *          16 hd  value codes [hd/64 m][4 g][hd/32 b][w r][2 n][8 j]: elements
+ *                 d = 32b + w (4m + 2n) + r (low four bits) and d + w of slot 8g + j
+ *             hd  key scales [hd/32 b][4 i][4 j][2 s] (slot 8i + 4s + j)
+ *             hd  value scales [hd/32 b][32 slots]
+ *        Nothing outside the records matters to a later call, so a cache may be
+ *        copied, saved and cut at record boundaries; slots never appended may
+ *        hold anything.
+ * Limits: head_dim 64 or 128; ctx_cap a multiple of 32, at most 1048576;
+ * n_kv_heads at most 65535.
+ */
+size_t cas_op_kv4_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t ctx_cap);
+
+/*
+ * Append T tokens' keys and values: quantise them into slots slot0 ..
+ * slot0 + T - 1 (of every kv head).  Other slots' bytes are not touched.
+ *   k, v:  bf16 rows of n_kv_heads * head_dim elements, ldk and ldv elements
+ *          apart (at least that many: rows of a wider product can be passed in
+ *          place).  Rows that start at multiples of 16 bytes load fastest
+ *   rope_cos, rope_sin: NULL (the keys are stored as they are), or [n_pos]
+ *          [head_dim/2] fp32: the keys are rotated first, pairs (i, i +
+ *          head_dim/2) as in cas.h, the exact rotated value rounded once to
+ *          fp32 and quantised from there
+ *   pos:   [T] positions (device), or NULL: row t's position is slot0 + t.  A
+ *          position outside [0, n_pos) stores that row's keys as NaN.  Not
+ *          read without a rotation
+ * 1 <= T, 0 <= slot0, slot0 + T <= ctx_cap.
+ */
+cas_status cas_op_kv4_append(const void* k, const void* v, int64_t ldk, int64_t ldv, int32_t T, int32_t slot0,
+                             const int32_t* pos, const float* rope_cos, const float* rope_sin, int32_t n_pos,
+                             int32_t n_kv_heads, int32_t head_dim, void* kv4, int32_t ctx_cap, void* stream);
+
+/* The values that slots slot0 .. slot0 + n - 1 hold, as bf16: k, v
+ * [n_kv_heads][n][head_dim], 16-byte aligned. */
+cas_status cas_op_kv4_read(const void* kv4, int32_t ctx_cap, int32_t slot0, int32_t n, int32_t n_kv_heads,
+                           int32_t head_dim, void* k, void* v, void* stream);
+
+/*
+ * Tree-masked attention over a cache whose first n4 slots are held in 4 bits:
+ * the rule, q, anc and out of cas_op_attention, with fp32 softmax.
+ *   n4:    slots [0, n4) are read from kv4, the others from k, v.  A multiple
+ *          of 32, or Lc + n_tree (every slot in 4 bits, the round's too)
+ *   k, v:  bf16 [n_kv_heads][kv_cap][head_dim], row j holding slot n4 + j,
+ *          kv_cap >= Lc + n_tree - n4 (NULL where no slot needs them)
+ *   attn_sink, attn_window: as in cas_draft_opts (0: every committed slot)
+ *   q, k, v and out are 16-byte aligned
+ * Slots and rows that a row does not see never reach it, whatever they hold.
+ * A row that sees no slot gives zeros; one that sees a key that is not finite
+ * gives NaN, and one that sees such a value NaN at its element.
+ * Probabilities are rounded to bf16 for the product with the values (each by
+ * at most 2^-8 of itself).  The result does not depend on earlier calls or on
+ * timing; it may depend in the last bits on T.
+ * 1 <= T <= 128, 1 <= n_tree <= 128, 0 <= Lc, Lc + n_tree <= ctx_cap, where
+ * ctx_cap is that of the records (n4 <= ctx_cap; the bf16 rows need no record).
+ * work: device scratch of cas_op_attention_kv4_work_bytes(...) bytes, 16-byte
+ * aligned, used by one call at a time.
+ */
+size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t n_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t attn_sink, int32_t attn_window);
+cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap, int32_t n4, const void* k,
+                                const void* v, int32_t kv_cap, int32_t Lc, int32_t n_tree, int32_t T,
+                                int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t attn_sink,
+                                int32_t attn_window, const uint64_t* anc, void* out, void* work, size_t work_bytes,
+                                void* stream);
+
+/*
  * How a prefill block of T rows (129 to 2048) runs a linear layer; host only.
  *   wtype:  CAS_W_F32 or CAS_W_BF16; W [N][K]
  *   resid:  1 for the O and down projections (added to the residual stream)

@@ -49,7 +49,8 @@ EXPORTS = ("cas_create", "cas_destroy", "cas_last_error", "cas_create_error", "c
            "cas_op_attn_merge", "cas_op_attn_merge_work_bytes", "cas_op_gemm_qx", "cas_op_gemm_qx_splits",
            "cas_op_gemm_qx_work_bytes", "cas_op_attention_noalloc", "cas_op_attention_noalloc_max_bytes",
            "cas_debug_build", "cas_debug_check", "cas_debug_limit_slots",
-           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block")
+           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_op_kv4_bytes",
+           "cas_op_kv4_append", "cas_op_kv4_read", "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes")
 # device check codes (cas_debug_check)
 DEVICE_CHECKS = ["none", "tree size", "token id", "parent order", "slot capacity", "RoPE position",
                  "KV write slot", "attention slots", "compaction path", "acceptance parent"]
@@ -133,6 +134,11 @@ def lib(debug: bool = False):
             "cas_debug_limit_slots": ([P, I], I),
             "cas_debug_limit_prefill": ([P, I], I),
             "cas_op_prefill_block": ([I, I, I, I, I, P], I),
+            "cas_op_kv4_bytes": ([I, I, I], Z),
+            "cas_op_kv4_append": ([P, P, ctypes.c_int64, ctypes.c_int64, I, I, P, P, P, I, I, I, P, I, P], I),
+            "cas_op_kv4_read": ([P, I, I, I, I, I, P, P, P], I),
+            "cas_op_attention_kv4": ([P, P, I, I, P, P, I, I, I, I, I, I, I, I, I, P, P, P, Z, P], I),
+            "cas_op_attention_kv4_work_bytes": ([I] * 8, Z),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -464,3 +470,44 @@ def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, s
     work = _work(lib().cas_op_gemm_qx_work_bytes(wtype, N, K, T))
     _ochk(lib().cas_op_gemm_qx(wtype, _dp(W), _dp(ws), _dp(x), N, K, T, int(qmax), _dp(parts), _dp(work),
                                int(work.numel()), _stream(stream)), "cas_op_gemm_qx")
+
+
+# the 4-bit KV cache (device byte tensors of kv4_bytes(...) bytes)
+
+def kv4_bytes(Hkv: int, hd: int, ctx_cap: int) -> int:
+    """Bytes of a 4-bit KV cache of ctx_cap slots (0: the shape has none)."""
+    return int(lib().cas_op_kv4_bytes(Hkv, hd, ctx_cap))
+
+
+def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int, pos=None, cos=None, sin=None,
+                  ldk: Optional[int] = None, ldv: Optional[int] = None, stream=None) -> None:
+    """Quantise T rows of keys and values (bf16, Hkv * hd elements, ldk and
+    ldv elements apart) into slots slot0 .. slot0 + T - 1.  With cos and sin
+    ([positions][hd/2] fp32) the keys are rotated by pos ([T] int32; None:
+    their slots) first."""
+    ld = Hkv * hd
+    _ochk(lib().cas_op_kv4_append(_dp(k), _dp(v), ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0,
+                                  _dp(pos), _dp(cos), _dp(sin), 0 if cos is None else int(cos.shape[0]), Hkv, hd,
+                                  _dp(kv4), ctx_cap, _stream(stream)), "cas_op_kv4_append")
+
+
+def op_kv4_read(kv4, ctx_cap: int, slot0: int, n: int, Hkv: int, hd: int, k, v, stream=None) -> None:
+    """The values of slots slot0 .. slot0 + n - 1 into k, v [Hkv][n][hd] bf16."""
+    _ochk(lib().cas_op_kv4_read(_dp(kv4), ctx_cap, slot0, n, Hkv, hd, _dp(k), _dp(v), _stream(stream)),
+          "cas_op_kv4_read")
+
+
+def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int, H: int, Hkv: int, hd: int, anc, out,
+                     k=None, v=None, kv_cap: Optional[int] = None, sink: int = 0, window: int = 0, stream=None,
+                     work=None) -> None:
+    """Tree attention with slots [0, n4) from the 4-bit cache and the others
+    from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap: k's second
+    dimension by default)."""
+    L = lib()
+    if work is None:
+        work = _work(L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window))
+    if kv_cap is None:
+        kv_cap = 0 if k is None else int(k.shape[1])
+    _ochk(L.cas_op_attention_kv4(_dp(q), _dp(kv4), ctx_cap, n4, _dp(k), _dp(v), kv_cap, Lc, n_tree, T, H, Hkv, hd,
+                                 sink, window, _dp(anc), _dp(out), _dp(work),
+                                 int(work.numel() * work.element_size()), _stream(stream)), "cas_op_attention_kv4")

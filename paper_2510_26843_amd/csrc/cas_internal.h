@@ -270,6 +270,41 @@ hipError_t launch_attn_merge(const AttnArgs& a, int S, hipStream_t s);
 hipError_t launch_kv_convert(int atype, void* kc, void* vt, const void* k_rows, const void* v_rows, int Hkv,
                              int n, int hd, int ctx_cap, int to_cache, hipStream_t s);
 
+// ---- the 4-bit KV cache (kv4.hip): [Hkv][ctx_cap / 32] records of 34 * hd bytes
+struct Kv4AppendArgs {
+    const uint16_t *k, *v;  // rows of Hkv * hd bf16, ldk / ldv elements apart
+    size_t ldk, ldv;
+    int vec;                // the rows allow 16-byte loads
+    int T, slot0;
+    const int* pos;         // positions of the rows (nullptr: their slots)
+    const float *cos, *sin; // [n_pos][hd / 2] (nullptr: no rotation)
+    int n_pos;
+    int Hkv, hd, ctx_cap;
+    uint8_t* kv4;
+};
+hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s);
+struct Kv4ReadArgs {
+    const uint8_t* kv4;
+    int ctx_cap, slot0, n, Hkv, hd;
+    uint16_t *k, *v;        // [Hkv][n][hd]
+};
+hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s);
+// Tree attention over slots [0, n4) of the 4-bit cache and the rest in bf16.
+// With a.sp (the decoder) n4 is the committed length rounded down to whole
+// records, the rest comes from the decoder's cache (a.kc, a.vt), and Lc_host
+// and n_tree_host are those of sp; without, the three come from here and the
+// rest from rows kr, vr.
+struct Kv4AttnArgs {
+    AttnArgs a;
+    const uint8_t* kv4;
+    int n4;
+    const uint16_t *kr, *vr;  // [Hkv][kv_cap][hd], slot n4 first
+    int kv_cap;
+    int direct;  // set by the launch: one split, the kernel writes the output itself
+};
+int kv4_attention_splits(int Lc, int n_tree, int T, int H, int Hkv, int win_sink, int win_len);
+hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s);
+
 // RMSNorm of rows of the fp32 residual stream h [T][d] with gains g:
 // writes the normalised rows as tiled activations of act type (out) or, with
 // q != NULL, their int8 quantisation (tiled int8 q, scales qs [T]) instead.

@@ -1691,6 +1691,119 @@ cas_status cas_op_gemm_qx(int32_t wtype, const int8_t* W, const float* ws, const
     return e == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
 }
 
+// ---- the 4-bit KV cache
+
+static constexpr int KV4_MAX_CAP = 1 << 20;
+static bool kv4_shape(int32_t Hkv, int32_t hd, int32_t ctx_cap, cas_status* st) {
+    *st = CAS_ERR_ARG;
+    if (Hkv < 1 || ctx_cap < 32 || ctx_cap % 32) return false;
+    *st = CAS_ERR_UNSUPPORTED;
+    if ((hd != 64 && hd != 128) || ctx_cap > KV4_MAX_CAP || Hkv > 65535) return false;
+    *st = CAS_OK;
+    return true;
+}
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+size_t cas_op_kv4_bytes(int32_t Hkv, int32_t hd, int32_t ctx_cap) {
+    cas_status st;
+    return kv4_shape(Hkv, hd, ctx_cap, &st) ? (size_t)Hkv * (ctx_cap / 32) * 34 * hd : 0;
+}
+
+cas_status cas_op_kv4_append(const void* k, const void* v, int64_t ldk, int64_t ldv, int32_t T, int32_t slot0,
+                             const int32_t* pos, const float* cos, const float* sin, int32_t n_pos, int32_t Hkv,
+                             int32_t hd, void* kv4, int32_t ctx_cap, void* stream) {
+    cas_status st;
+    if (!k || !v || !kv4 || !cos != !sin) return CAS_ERR_ARG;
+    if (!kv4_shape(Hkv, hd, ctx_cap, &st)) return st;
+    const int64_t w = (int64_t)Hkv * hd;
+    if (T < 1 || slot0 < 0 || T > ctx_cap || slot0 > ctx_cap - T || ldk < w || ldv < w) return CAS_ERR_ARG;
+    if (cos && n_pos < 1) return CAS_ERR_ARG;
+    if (!aligned16(kv4) || (((uintptr_t)k | (uintptr_t)v) & 1)) return CAS_ERR_ARG;
+    Kv4AppendArgs a{};
+    a.k = (const uint16_t*)k;
+    a.v = (const uint16_t*)v;
+    a.ldk = (size_t)ldk;
+    a.ldv = (size_t)ldv;
+    a.vec = aligned16(k) && aligned16(v) && ldk % 8 == 0 && ldv % 8 == 0;
+    a.T = T;
+    a.slot0 = slot0;
+    a.pos = pos;
+    a.cos = cos;
+    a.sin = sin;
+    a.n_pos = n_pos;
+    a.Hkv = Hkv;
+    a.hd = hd;
+    a.ctx_cap = ctx_cap;
+    a.kv4 = (uint8_t*)kv4;
+    return launch_kv4_append(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
+cas_status cas_op_kv4_read(const void* kv4, int32_t ctx_cap, int32_t slot0, int32_t n, int32_t Hkv, int32_t hd, void* k,
+                           void* v, void* stream) {
+    cas_status st;
+    if (!k || !v || !kv4) return CAS_ERR_ARG;
+    if (!kv4_shape(Hkv, hd, ctx_cap, &st)) return st;
+    if (n < 1 || slot0 < 0 || n > ctx_cap || slot0 > ctx_cap - n) return CAS_ERR_ARG;
+    if (!aligned16(kv4) || !aligned16(k) || !aligned16(v)) return CAS_ERR_ARG;
+    const Kv4ReadArgs a{(const uint8_t*)kv4, ctx_cap, slot0, n, Hkv, hd, (uint16_t*)k, (uint16_t*)v};
+    return launch_kv4_read(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
+static bool attention_kv4_shape(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
+                                int32_t sink, int32_t window) {
+    return T >= 1 && T <= 128 && n_tree >= 1 && n_tree <= 128 && Lc >= 0 && Lc <= KV4_MAX_CAP - n_tree && Hkv >= 1 &&
+           H >= 1 && H % Hkv == 0 && H <= 65535 && sink >= 0 && window >= 0 && (hd == 64 || hd == 128);
+}
+
+size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
+                                       int32_t sink, int32_t window) {
+    if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return 0;
+    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, window ? sink : 0, window);
+    return 256 + S * H * T * ((size_t)hd + 2) * 4;
+}
+
+cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap, int32_t n4, const void* k,
+                                const void* v, int32_t kv_cap, int32_t Lc, int32_t n_tree, int32_t T, int32_t H,
+                                int32_t Hkv, int32_t hd, int32_t sink, int32_t window, const uint64_t* anc, void* out,
+                                void* work, size_t work_bytes, void* stream) {
+    cas_status st;
+    if (!q || !anc || !out || !work) return CAS_ERR_ARG;
+    if (hd != 64 && hd != 128) return CAS_ERR_UNSUPPORTED;
+    if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return CAS_ERR_ARG;
+    const int n_slots = Lc + n_tree;
+    if (n4 < 0 || n4 > n_slots || (n4 % 32 && n4 != n_slots)) return CAS_ERR_ARG;
+    if (n4 > 0) {
+        if (!kv4 || !aligned16(kv4)) return CAS_ERR_ARG;
+        if (!kv4_shape(Hkv, hd, ctx_cap, &st)) return st;
+        if (n4 > ctx_cap) return CAS_ERR_ARG;
+    }
+    if (n4 < n_slots && (!k || !v || kv_cap < n_slots - n4 || !aligned16(k) || !aligned16(v))) return CAS_ERR_ARG;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(work) || ((uintptr_t)anc & 7)) return CAS_ERR_ARG;
+    if (work_bytes < cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)) return CAS_ERR_ARG;
+    Kv4AttnArgs a{};
+    a.a.q = q;
+    a.a.anc = anc;
+    a.a.Lc_host = Lc;
+    a.a.n_tree_host = n_tree;
+    a.a.out = out;
+    a.a.T = T;
+    a.a.H = H;
+    a.a.Hkv = Hkv;
+    a.a.hd = hd;
+    a.a.ctx_cap = n4 > 0 ? ctx_cap : 32;
+    a.a.win_sink = window ? sink : 0;
+    a.a.win_len = window;
+    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, a.a.win_sink, a.a.win_len);
+    a.a.part_o = (float*)work;
+    a.a.part_ml = a.a.part_o + S * H * T * hd;
+    a.kv4 = (const uint8_t*)kv4;
+    a.n4 = n4;
+    a.kr = (const uint16_t*)k;
+    a.vr = (const uint16_t*)v;
+    a.kv_cap = kv_cap;
+    return launch_attention_kv4(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
 cas_status cas_op_copy(void* dst, const void* src, size_t bytes, void* stream) {
     if (!dst || !src || bytes % 16) return CAS_ERR_ARG;
     hipError_t e = launch_copy(dst, src, bytes, (hipStream_t)stream);
