@@ -224,9 +224,9 @@ size_t cas_op_kv4_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t ctx_cap);
  *          apart (at least that many: rows of a wider product can be passed in
  *          place).  Rows that start at multiples of 16 bytes load fastest
  *   rope_cos, rope_sin: NULL (the keys are stored as they are), or [n_pos]
- *          [head_dim/2] fp32: the keys are rotated first, pairs (i, i +
- *          head_dim/2) as in cas.h, the exact rotated value rounded once to
- *          fp32 and quantised from there
+ *          [head_dim/2] fp32, 16-byte aligned: the keys are rotated first,
+ *          pairs (i, i + head_dim/2) as in cas.h, the exact rotated value
+ *          rounded once to fp32 and quantised from there
  *   pos:   [T] positions (device), or NULL: row t's position is slot0 + t.  A
  *          position outside [0, n_pos) stores that row's keys as NaN.  Not
  *          read without a rotation
@@ -258,8 +258,8 @@ cas_status cas_op_kv4_read(const void* kv4, int32_t ctx_cap, int32_t slot0, int3
  * timing; it may depend in the last bits on T.
  * 1 <= T <= 128, 1 <= n_tree <= 128, 0 <= Lc, Lc + n_tree <= ctx_cap, where
  * ctx_cap is that of the records (n4 <= ctx_cap; the bf16 rows need no record).
- * work: device scratch of cas_op_attention_kv4_work_bytes(...) bytes, 16-byte
- * aligned, used by one call at a time.
+ * work: device scratch of cas_op_attention_kv4_work_bytes(...) bytes (0: none
+ * is needed, work may be NULL), 16-byte aligned, used by one call at a time.
  */
 size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t n_heads, int32_t n_kv_heads,
                                        int32_t head_dim, int32_t attn_sink, int32_t attn_window);

@@ -374,7 +374,8 @@ def _dp(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        # (torch.cuda.current_stream() takes 2.8 us of every call to make an object of it)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return int(stream)
 
 
@@ -474,6 +475,12 @@ def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, s
 
 # the 4-bit KV cache (device byte tensors of kv4_bytes(...) bytes)
 
+def _on_current_device(t, what: str) -> None:
+    import torch
+    if t.get_device() != torch.cuda.current_device():
+        raise CasError(ERR_ARG, what + ": the cache is not on the current device")
+
+
 def kv4_bytes(Hkv: int, hd: int, ctx_cap: int) -> int:
     """Bytes of a 4-bit KV cache of ctx_cap slots (0: the shape has none)."""
     return int(lib().cas_op_kv4_bytes(Hkv, hd, ctx_cap))
@@ -485,6 +492,7 @@ def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int
     ldv elements apart) into slots slot0 .. slot0 + T - 1.  With cos and sin
     ([positions][hd/2] fp32) the keys are rotated by pos ([T] int32; None:
     their slots) first."""
+    _on_current_device(kv4, "cas_op_kv4_append")
     ld = Hkv * hd
     _ochk(lib().cas_op_kv4_append(_dp(k), _dp(v), ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0,
                                   _dp(pos), _dp(cos), _dp(sin), 0 if cos is None else int(cos.shape[0]), Hkv, hd,
@@ -493,6 +501,7 @@ def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int
 
 def op_kv4_read(kv4, ctx_cap: int, slot0: int, n: int, Hkv: int, hd: int, k, v, stream=None) -> None:
     """The values of slots slot0 .. slot0 + n - 1 into k, v [Hkv][n][hd] bf16."""
+    _on_current_device(kv4, "cas_op_kv4_read")
     _ochk(lib().cas_op_kv4_read(_dp(kv4), ctx_cap, slot0, n, Hkv, hd, _dp(k), _dp(v), _stream(stream)),
           "cas_op_kv4_read")
 
@@ -503,11 +512,13 @@ def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int
     """Tree attention with slots [0, n4) from the 4-bit cache and the others
     from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap: k's second
     dimension by default)."""
+    _on_current_device(q, "cas_op_attention_kv4")
     L = lib()
     if work is None:
-        work = _work(L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window))
+        need = L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)
+        work = _work(need) if need else None
     if kv_cap is None:
         kv_cap = 0 if k is None else int(k.shape[1])
     _ochk(L.cas_op_attention_kv4(_dp(q), _dp(kv4), ctx_cap, n4, _dp(k), _dp(v), kv_cap, Lc, n_tree, T, H, Hkv, hd,
-                                 sink, window, _dp(anc), _dp(out), _dp(work),
-                                 int(work.numel() * work.element_size()), _stream(stream)), "cas_op_attention_kv4")
+                                 sink, window, _dp(anc), _dp(out), _dp(work), 0 if work is None else work.nbytes,
+                                 _stream(stream)), "cas_op_attention_kv4")

@@ -302,7 +302,7 @@ struct Kv4AttnArgs {
     int kv_cap;
     int direct;  // set by the launch: one split, the kernel writes the output itself
 };
-int kv4_attention_splits(int Lc, int n_tree, int T, int H, int Hkv, int win_sink, int win_len);
+int kv4_attention_splits(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len);
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s);
 
 // RMSNorm of rows of the fp32 residual stream h [T][d] with gains g:

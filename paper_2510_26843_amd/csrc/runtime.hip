@@ -1718,7 +1718,7 @@ cas_status cas_op_kv4_append(const void* k, const void* v, int64_t ldk, int64_t 
     const int64_t w = (int64_t)Hkv * hd;
     if (T < 1 || slot0 < 0 || T > ctx_cap || slot0 > ctx_cap - T || ldk < w || ldv < w) return CAS_ERR_ARG;
     if (cos && n_pos < 1) return CAS_ERR_ARG;
-    if (!aligned16(kv4) || (((uintptr_t)k | (uintptr_t)v) & 1)) return CAS_ERR_ARG;
+    if (!aligned16(kv4) || !aligned16(cos) || !aligned16(sin) || (((uintptr_t)k | (uintptr_t)v) & 1)) return CAS_ERR_ARG;
     Kv4AppendArgs a{};
     a.k = (const uint16_t*)k;
     a.v = (const uint16_t*)v;
@@ -1758,8 +1758,8 @@ static bool attention_kv4_shape(int32_t Lc, int32_t n_tree, int32_t T, int32_t H
 size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
                                        int32_t sink, int32_t window) {
     if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return 0;
-    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, window ? sink : 0, window);
-    return 256 + S * H * T * ((size_t)hd + 2) * 4;
+    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window);
+    return S > 1 ? S * H * T * ((size_t)hd + 2) * 4 : 0;
 }
 
 cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap, int32_t n4, const void* k,
@@ -1767,7 +1767,7 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
                                 int32_t Hkv, int32_t hd, int32_t sink, int32_t window, const uint64_t* anc, void* out,
                                 void* work, size_t work_bytes, void* stream) {
     cas_status st;
-    if (!q || !anc || !out || !work) return CAS_ERR_ARG;
+    if (!q || !anc || !out) return CAS_ERR_ARG;
     if (hd != 64 && hd != 128) return CAS_ERR_UNSUPPORTED;
     if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return CAS_ERR_ARG;
     const int n_slots = Lc + n_tree;
@@ -1779,7 +1779,8 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     }
     if (n4 < n_slots && (!k || !v || kv_cap < n_slots - n4 || !aligned16(k) || !aligned16(v))) return CAS_ERR_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(work) || ((uintptr_t)anc & 7)) return CAS_ERR_ARG;
-    if (work_bytes < cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)) return CAS_ERR_ARG;
+    const size_t need = cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window);
+    if (need && (!work || work_bytes < need)) return CAS_ERR_ARG;
     Kv4AttnArgs a{};
     a.a.q = q;
     a.a.anc = anc;
@@ -1793,7 +1794,7 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     a.a.ctx_cap = n4 > 0 ? ctx_cap : 32;
     a.a.win_sink = window ? sink : 0;
     a.a.win_len = window;
-    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, a.a.win_sink, a.a.win_len);
+    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, hd, a.a.win_sink, a.a.win_len);
     a.a.part_o = (float*)work;
     a.a.part_ml = a.a.part_o + S * H * T * hd;
     a.kv4 = (const uint8_t*)kv4;

@@ -62,8 +62,8 @@ def test_read_refuses(change, status):
                                      None) == status
 
 
-ATTEND = dict(q=P, kv4=P, cap=64, n4=32, k=P, v=P, kv_cap=20, Lc=40, n_tree=3, T=3, H=8, Hkv=2, hd=64, sink=0,
-              window=0, anc=P, out=P, work=P, nbytes=1 << 30)
+ATTEND = dict(q=P, kv4=P, cap=65536, n4=32000, k=P, v=P, kv_cap=20, Lc=32008, n_tree=3, T=3, H=8, Hkv=2, hd=64,
+              sink=0, window=0, anc=P, out=P, work=P, nbytes=1 << 30)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -72,8 +72,8 @@ ATTEND = dict(q=P, kv4=P, cap=64, n4=32, k=P, v=P, kv_cap=20, Lc=40, n_tree=3, T
     (dict(work=None), cas.ERR_ARG), (dict(nbytes=16), cas.ERR_ARG), (dict(q=P + 8), cas.ERR_ARG),
     (dict(out=P + 2), cas.ERR_ARG), (dict(k=P + 2), cas.ERR_ARG), (dict(anc=P + 4), cas.ERR_ARG),
     (dict(kv4=P + 4), cas.ERR_ARG), (dict(work=P + 4), cas.ERR_ARG), (dict(n4=31), cas.ERR_ARG),
-    (dict(n4=-32), cas.ERR_ARG), (dict(n4=64), cas.ERR_ARG), (dict(kv_cap=10), cas.ERR_ARG),
-    (dict(n4=43, cap=32), cas.ERR_ARG), (dict(T=0), cas.ERR_ARG), (dict(T=129), cas.ERR_ARG),
+    (dict(n4=-32), cas.ERR_ARG), (dict(n4=32032), cas.ERR_ARG), (dict(kv_cap=10), cas.ERR_ARG),
+    (dict(n4=32011, cap=32000), cas.ERR_ARG), (dict(T=0), cas.ERR_ARG), (dict(T=129), cas.ERR_ARG),
     (dict(n_tree=0), cas.ERR_ARG), (dict(n_tree=129), cas.ERR_ARG), (dict(Lc=-1), cas.ERR_ARG),
     (dict(Lc=2**31 - 1), cas.ERR_ARG), (dict(H=7), cas.ERR_ARG), (dict(Hkv=0), cas.ERR_ARG),
     (dict(sink=-1), cas.ERR_ARG), (dict(window=-1), cas.ERR_ARG), (dict(hd=80), cas.ERR_UNSUPPORTED),
@@ -87,4 +87,6 @@ def test_attention_refuses(change, status):
 
 def test_work_bytes():
     assert cas.lib().cas_op_attention_kv4_work_bytes(40, 3, 0, 8, 2, 64, 0, 0) == 0
-    assert cas.lib().cas_op_attention_kv4_work_bytes(40, 3, 3, 8, 2, 64, 0, 0) >= 3 * 8 * 66 * 4
+    assert cas.lib().cas_op_attention_kv4_work_bytes(40, 3, 3, 8, 2, 64, 0, 0) == 0  # one run of tiles: none
+    need = cas.lib().cas_op_attention_kv4_work_bytes(100000, 3, 3, 8, 2, 64, 0, 0)
+    assert need >= 2 * 3 * 8 * 66 * 4 and need % (3 * 8 * 66 * 4) == 0
