@@ -198,6 +198,26 @@ typedef struct {
 cas_status cas_forward_draft(cas_ctx* ctx, const int32_t* tokens, const int32_t* tree_parent, int32_t n,
                              int32_t node_offset, const cas_draft_opts* opts, float* logits_host);
 
+/* The 4-bit copy of the KV cache behind cas_forward_draft_kv4 (App. C,
+ * activation quantisation: the "(partial) KV cache"; the form is that of
+ * cas_op_kv4_append in cas_ops.h): allocates it (17/64 of the cache; freed with
+ * the context).  bf16 models only (CAS_ERR_UNSUPPORTED); a second call does
+ * nothing. */
+cas_status cas_build_kv4(cas_ctx* ctx);
+
+/*
+ * cas_forward_draft whose attention reads the committed slots, but for the
+ * last Lc % 32, from the 4-bit copy: a draft of a long context moves 17/64 of
+ * those slots' KV bytes.  The other slots and the round's nodes are read from
+ * the cache, and the nodes' KV is written there, as by every draft.  Before the
+ * forward the call packs the committed slots that the copy does not hold yet
+ * (those committed, or restored with cas_kv_load, since the last such call).
+ * Needs cas_build_kv4.  Same arguments, limits, errors and synchronisation as
+ * cas_forward_draft; never a verify call.
+ */
+cas_status cas_forward_draft_kv4(cas_ctx* ctx, const int32_t* tokens, const int32_t* tree_parent, int32_t n,
+                                 int32_t node_offset, const cas_draft_opts* opts, float* logits_host);
+
 /*
  * Greedy verification of the tree of the last verify call: g[i] is the
  * argmax of node i's logits (lowest index on ties).  From the root, move to
@@ -237,8 +257,8 @@ cas_status cas_kv_compact(cas_ctx* ctx, const int32_t* accepted, int32_t n_accep
  * output may be NULL. */
 cas_status cas_tree_info(const int32_t* tree_parent, int32_t n, int32_t* depth, uint64_t* anc);
 
-/* Capture the forward's launches in HIP graphs keyed on (n, node_offset,
- * skip mask, act_quant, attention split count) and replay them (1, default),
+/* Capture the forward's launches in HIP graphs keyed on (n, skip mask,
+ * act_quant, attention window and splits, 4-bit KV) and replay them (1, default),
  * or launch kernel by kernel (0). */
 cas_status cas_set_graphs(cas_ctx* ctx, int32_t enable);
 

@@ -49,7 +49,7 @@ EXPORTS = ("cas_create", "cas_destroy", "cas_last_error", "cas_create_error", "c
            "cas_op_attn_merge", "cas_op_attn_merge_work_bytes", "cas_op_gemm_qx", "cas_op_gemm_qx_splits",
            "cas_op_gemm_qx_work_bytes", "cas_op_attention_noalloc", "cas_op_attention_noalloc_max_bytes",
            "cas_debug_build", "cas_debug_check", "cas_debug_limit_slots",
-           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_op_kv4_bytes",
+           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_build_kv4", "cas_forward_draft_kv4", "cas_op_kv4_bytes",
            "cas_op_kv4_append", "cas_op_kv4_read", "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes")
 # device check codes (cas_debug_check)
 DEVICE_CHECKS = ["none", "tree size", "token id", "parent order", "slot capacity", "RoPE position",
@@ -134,6 +134,8 @@ def lib(debug: bool = False):
             "cas_debug_limit_slots": ([P, I], I),
             "cas_debug_limit_prefill": ([P, I], I),
             "cas_op_prefill_block": ([I, I, I, I, I, P], I),
+            "cas_build_kv4": ([P], I),
+            "cas_forward_draft_kv4": ([P, P, P, I, I, P, P], I),
             "cas_op_kv4_bytes": ([I, I, I], Z),
             "cas_op_kv4_append": ([P, P, ctypes.c_int64, ctypes.c_int64, I, I, P, P, P, I, I, I, P, I, P], I),
             "cas_op_kv4_read": ([P, I, I, I, I, I, P, P, P], I),
@@ -236,6 +238,10 @@ class Model:
         """The int4 weight copy behind act_quant = 2 (W4A4 drafts)."""
         self._chk(self._L.cas_build_int4(self.h))
 
+    def build_kv4(self) -> None:
+        """The 4-bit copy of the KV cache behind forward(..., kv4=True)."""
+        self._chk(self._L.cas_build_kv4(self.h))
+
     # state ----------------------------------------------------------------------
     @property
     def committed(self) -> int:
@@ -267,9 +273,11 @@ class Model:
     # the step -------------------------------------------------------------------
     def forward(self, tokens: Sequence[int], parents: Sequence[int], node_offset: int = 0,
                 skip: Optional[Sequence[int]] = None, act_quant: int = 0,
-                logits: bool = True, attn_window: Optional[Tuple[int, int]] = None) -> Optional[np.ndarray]:
+                logits: bool = True, attn_window: Optional[Tuple[int, int]] = None,
+                kv4: bool = False) -> Optional[np.ndarray]:
         """act_quant: 0, 1 (or True) = W8A8, 2 = W4A4.  attn_window = (sink,
-        window): efficient-attention draft."""
+        window): efficient-attention draft.  kv4: a draft that reads the
+        committed KV from its 4-bit copy."""
         t = np.ascontiguousarray(tokens, dtype=np.int32)
         p = np.ascontiguousarray(parents, dtype=np.int32)
         n = t.shape[0]
@@ -281,11 +289,11 @@ class Model:
             if sk.shape[0] != self.shape.n_layers:
                 raise ValueError("skip mask length")
         out = np.empty((n, self.shape.vocab), dtype=np.float32) if logits else None
-        if attn_window:
-            o = DraftOpts(None if sk is None else _p(sk), int(act_quant), int(attn_window[0]),
-                          int(attn_window[1]))
-            self._chk(self._L.cas_forward_draft(self.h, _p(t), _p(p), n, int(node_offset), ctypes.byref(o),
-                                              None if out is None else _p(out)))
+        if attn_window or kv4:
+            sink, window = attn_window or (0, 0)
+            o = DraftOpts(None if sk is None else _p(sk), int(act_quant), int(sink), int(window))
+            fn = self._L.cas_forward_draft_kv4 if kv4 else self._L.cas_forward_draft
+            self._chk(fn(self.h, _p(t), _p(p), n, int(node_offset), ctypes.byref(o), None if out is None else _p(out)))
         else:
             self._chk(self._L.cas_forward(self.h, _p(t), _p(p), n, int(node_offset), None if sk is None else _p(sk),
                                         int(act_quant), None if out is None else _p(out)))

@@ -289,6 +289,16 @@ struct Kv4ReadArgs {
     uint16_t *k, *v;        // [Hkv][n][hd]
 };
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s);
+// Records tile0 .. tile0 + tiles - 1 of `heads` (layer, kv head) pairs from the
+// decoder's bf16 cache [heads][ctx_cap][hd].
+hipError_t launch_kv4_pack(const void* kc, const void* vt, int heads, int hd, int ctx_cap, int tile0, int tiles,
+                           uint8_t* kv4, hipStream_t s);
+// How a call's attention runs: query tiles per workgroup and splits (at most
+// max_S, whose partial states are [S][H][T][hd] and [S][H][T][2] fp32).
+struct Kv4Plan {
+    int jt, S;
+};
+Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len, int max_S = 64);
 // Tree attention over slots [0, n4) of the 4-bit cache and the rest in bf16.
 // With a.sp (the decoder) n4 is the committed length rounded down to whole
 // records, the rest comes from the decoder's cache (a.kc, a.vt), and Lc_host
@@ -300,9 +310,9 @@ struct Kv4AttnArgs {
     int n4;
     const uint16_t *kr, *vr;  // [Hkv][kv_cap][hd], slot n4 first
     int kv_cap;
+    Kv4Plan plan;
     int direct;  // set by the launch: one split, the kernel writes the output itself
 };
-int kv4_attention_splits(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len);
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s);
 
 // RMSNorm of rows of the fp32 residual stream h [T][d] with gains g:

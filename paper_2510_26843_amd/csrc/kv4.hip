@@ -153,34 +153,32 @@ __device__ __forceinline__ void kv4_rotate(const float* cos, const float* sin, s
     }
 }
 
-template <int HD> __device__ __forceinline__ void kv4_record(const Kv4AppendArgs& a, int tile, int h, uint8_t* img) {
+// A record of a tile's rows in LDS.  SRC: rows k(sl, d0) of 8 key elements, v4(s4,
+// d0, x) of four slots' 8 value elements, and rot(sl, d0, x, y), which turns the
+// keys' pieces at d0 and d0 + hd/2.
+template <int HD, typename K, typename V, typename R>
+__device__ __forceinline__ void kv4_record(uint8_t* img, K k, V v4, R rot) {
     constexpr int CH = HD / 8;
-    const int t0 = tile * 32 - a.slot0, tid = threadIdx.x;
-    auto row = [&](int sl) { return (size_t)min(max(t0 + sl, 0), a.T - 1); };
+    const int tid = threadIdx.x;
     if (tid < 128) {
         constexpr int PR = CH / 2, NK = 32 * PR / 128;  // pairs of pieces per row, and per thread
         i32x4 lo[NK], hi[NK];
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            const int item = k * 128 + tid;
-            const uint16_t* p = a.k + row(item / PR) * a.ldk + h * HD + item % PR * 8;
-            lo[k] = ld8_bf(p, a.vec);
-            hi[k] = ld8_bf(p + HD / 2, a.vec);
+        for (int i = 0; i < NK; ++i) {
+            const int item = i * 128 + tid;
+            lo[i] = k(item / PR, item % PR * 8);
+            hi[i] = k(item / PR, item % PR * 8 + HD / 2);
         }
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            const int item = k * 128 + tid, sl = item / PR, d0 = item % PR * 8;
+        for (int i = 0; i < NK; ++i) {
+            const int item = i * 128 + tid, sl = item / PR, d0 = item % PR * 8;
             float x[8], y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = piece_val<uint16_t>(lo[k], i);
-                y[i] = piece_val<uint16_t>(hi[k], i);
+            for (int e = 0; e < 8; ++e) {
+                x[e] = piece_val<uint16_t>(lo[i], e);
+                y[e] = piece_val<uint16_t>(hi[i], e);
             }
-            if (a.cos) {
-                const int pos = a.pos ? a.pos[row(sl)] : tile * 32 + sl;
-                const bool ok = pos >= 0 && pos < a.n_pos;
-                kv4_rotate<HD>(a.cos, a.sin, (size_t)(ok ? pos : 0) * (HD / 2) + d0, ok, x, y);
-            }
+            rot(sl, d0, x, y);
             uint32_t byte;
             uint32_t w = kv4_quantise(x, &byte);
             kv4_put_key<HD>(img, sl, d0, w, byte);
@@ -189,18 +187,14 @@ template <int HD> __device__ __forceinline__ void kv4_record(const Kv4AppendArgs
         }
     } else if (tid < 128 + 8 * CH) {
         const int item = tid - 128, d0 = item % CH * 8, s4 = item / CH * 4;  // slots s4 .. s4 + 3
-        i32x4 v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = ld8_bf(a.v + row(s4 + j) * a.ldv + h * HD + d0, a.vec);
+        float x[4][8];
+        v4(s4, d0, x);
         const int b = d0 >> 5, q = (d0 >> 3) & 3;
         uint32_t e[4], o[4], scales = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = piece_val<uint16_t>(v[j], i);
             uint32_t byte;
-            uint32_t w = kv4_quantise(x, &byte);
+            uint32_t w = kv4_quantise(x[j], &byte);
             scales |= byte << (8 * j);
             if (HD == 64) {  // a d tile's 8 rows pair with the neighbour's: rows 0-3 to the even lane
                 const uint32_t n = quad_xor1(w);
@@ -280,7 +274,24 @@ template <int HD> __global__ void __launch_bounds__(KV4_THREADS) k_kv4_append(co
         kv4_pieces<HD>(a, tile, h, first, last, rec);
         return;
     }
-    kv4_record<HD>(a, tile, h, img);
+    auto row = [&](int sl) { return (size_t)min(max(tile * 32 + sl - a.slot0, 0), a.T - 1); };
+    kv4_record<HD>(
+        img, [&](int sl, int d0) { return ld8_bf(a.k + row(sl) * a.ldk + h * HD + d0, a.vec); },
+        [&](int s4, int d0, float (&x)[4][8]) {
+            i32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = ld8_bf(a.v + row(s4 + j) * a.ldv + h * HD + d0, a.vec);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = piece_val<uint16_t>(v[j], e);
+        },
+        [&](int sl, int d0, float (&x)[8], float (&y)[8]) {
+            if (!a.cos) return;
+            const int pos = a.pos ? a.pos[row(sl)] : tile * 32 + sl;
+            const bool ok = pos >= 0 && pos < a.n_pos;
+            kv4_rotate<HD>(a.cos, a.sin, (size_t)(ok ? pos : 0) * (HD / 2) + d0, ok, x, y);
+        });
     __syncthreads();
     if (first == 0 && last == 32) {
         for (int i = threadIdx.x; i < 34 * HD / 16; i += KV4_THREADS) ((i32x4*)rec)[i] = ((const i32x4*)img)[i];
@@ -308,6 +319,45 @@ hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s) {
     const dim3 grid(((a.slot0 + a.T - 1) >> 5) - (a.slot0 >> 5) + 1, a.Hkv);
     if (a.hd == 128) hipLaunchKernelGGL(k_kv4_append<128>, grid, dim3(KV4_THREADS), 0, s, a);
     else if (a.hd == 64) hipLaunchKernelGGL(k_kv4_append<64>, grid, dim3(KV4_THREADS), 0, s, a);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+// Records tile0 .. tile0 + gridDim.x - 1 of every (layer, kv head) from the
+// decoder's bf16 cache (whole 32-slot tiles; its keys are rotated).
+template <int HD>
+__global__ void __launch_bounds__(KV4_THREADS) k_kv4_pack(const uint16_t* kc, const uint16_t* vt, int ctx_cap, int tile0,
+                                                          uint8_t* kv4) {
+    __shared__ __attribute__((aligned(16))) uint8_t img[34 * HD];
+    const int tile = tile0 + blockIdx.x;
+    const size_t src = ((size_t)blockIdx.y * ctx_cap + (size_t)tile * 32) * HD;
+    kv4_record<HD>(
+        img, [&](int sl, int d0) { return *(const i32x4*)(kc + src + kv_k_tiled(sl, d0, HD)); },
+        [&](int s4, int d0, float (&x)[4][8]) {
+            i32x2 v[8];  // four slots at a d are 8 bytes
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = *(const i32x2*)(vt + src + kv_v_tiled(s4, d0 + e, HD));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = (uint32_t)v[e][j >> 1];
+                    x[j][e] = __uint_as_float((j & 1) ? (w & 0xffff0000u) : (w << 16));
+                }
+        },
+        [](int, int, float (&)[8], float (&)[8]) {});
+    __syncthreads();
+    i32x4* rec = (i32x4*)(kv4 + ((size_t)blockIdx.y * (ctx_cap >> 5) + tile) * (34 * HD));
+    for (int i = threadIdx.x; i < 34 * HD / 16; i += KV4_THREADS) rec[i] = ((const i32x4*)img)[i];
+}
+
+hipError_t launch_kv4_pack(const void* kc, const void* vt, int heads, int hd, int ctx_cap, int tile0, int tiles,
+                           uint8_t* kv4, hipStream_t s) {
+    if (tiles < 1 || tile0 < 0 || tile0 + tiles > ctx_cap >> 5 || heads < 1 || heads > 65535) return hipErrorInvalidValue;
+    const dim3 grid(tiles, heads);
+    const uint16_t *k = (const uint16_t*)kc, *v = (const uint16_t*)vt;
+    if (hd == 128) hipLaunchKernelGGL(k_kv4_pack<128>, grid, dim3(KV4_THREADS), 0, s, k, v, ctx_cap, tile0, kv4);
+    else if (hd == 64) hipLaunchKernelGGL(k_kv4_pack<64>, grid, dim3(KV4_THREADS), 0, s, k, v, ctx_cap, tile0, kv4);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }
@@ -902,17 +952,14 @@ template <int HD> static hipError_t kv4_merge_go(const AttnArgs& a, int S, hipSt
 // 43 us with 2 tiles and 2 splits, 54 with 1 and 1; 64 rows of 13B heads over
 // 2048 slots 12.5 with 1 and 1, 16.9 with 2 and 2.  One split needs no merge:
 // one row of 13B heads over 500 slots takes 6.5 us with it, 7.9 with two.
-struct Kv4Plan {
-    int jt, S;
-};
-static Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len) {
+Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len, int max_S) {
     const int n_log = AttnWindow(Lc, n_tree, win_sink, win_len).n_log;
     const int nct = attn_query_tiles(T, H / Hkv);
     Kv4Plan best{1, 1};
     float least = INFINITY;
     for (int jt = 1; jt <= (nct > 1 ? 2 : 1); ++jt) {
         const int z = (nct + jt - 1) / jt;
-        for (int S = 1; S <= ATT_MAX_SPLITS && (S == 1 || S <= n_log); ++S) {
+        for (int S = 1; S == 1 || (S <= ATT_MAX_SPLITS && S <= max_S && S <= n_log); ++S) {
             const float wgs = (float)Hkv * z * S;
             const int rounds = (int)((wgs + 255) / 256);
             const int steps = ((n_log + S - 1) / S + KV4_WAVES - 1) / KV4_WAVES;
@@ -928,10 +975,6 @@ static Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int w
     return best;
 }
 
-int kv4_attention_splits(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len) {
-    return kv4_plan(Lc, n_tree, T, H, Hkv, hd, win_sink, win_len).S;
-}
-
 template <int HD, int JT> static hipError_t attn_kv4_go(const Kv4AttnArgs& k, dim3 grid, int tail, float c, hipStream_t s) {
     if (tail == 0) hipLaunchKernelGGL((k_attn_kv4<HD, JT, 0>), grid, dim3(64 * KV4_WAVES), 0, s, k, c);
     else if (tail == 1) hipLaunchKernelGGL((k_attn_kv4<HD, JT, 1>), grid, dim3(64 * KV4_WAVES), 0, s, k, c);
@@ -942,8 +985,8 @@ template <int HD, int JT> static hipError_t attn_kv4_go(const Kv4AttnArgs& k, di
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s) {
     const AttnArgs& a = k.a;
     if (a.T < 1 || a.T > 128 || a.Hkv < 1 || a.H % a.Hkv || a.ctx_cap % 32) return hipErrorInvalidValue;
-    const Kv4Plan plan = kv4_plan(a.Lc_host, a.n_tree_host, a.T, a.H, a.Hkv, a.hd, a.win_sink, a.win_len);
-    const int S = plan.S, jt = plan.jt, nct = attn_query_tiles(a.T, a.H / a.Hkv);
+    if (k.plan.S < 1 || k.plan.S > ATT_MAX_SPLITS || (k.plan.jt != 1 && k.plan.jt != 2)) return hipErrorInvalidValue;
+    const int S = k.plan.S, jt = k.plan.jt, nct = attn_query_tiles(a.T, a.H / a.Hkv);
     const dim3 grid(S, a.Hkv, (nct + jt - 1) / jt);
     // (the decoder's whole-tile copy always leaves slots to its bf16 cache)
     const int tail = a.sp ? 2 : k.n4 < a.Lc_host + a.n_tree_host ? 1 : 0;

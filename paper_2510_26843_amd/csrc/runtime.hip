@@ -148,6 +148,11 @@ struct cas_ctx {
     std::map<std::string, hipGraphExec_t> gcache;
     int win_sink = 0, win_len = 0;  // attention window of the forward being enqueued (0: none)
 
+    uint8_t* kv4 = nullptr;  // 4-bit copy of the KV cache, [L][Hkv] records (cas_build_kv4)
+    int kv4_len = 0;         // slots of it that hold the cache's (whole records)
+    bool kv4_call = false;   // the forward being enqueued reads it
+    Kv4Plan kv4_run{1, 1};
+
     bool prof = false;
     std::vector<ProfRec> prec;
     std::vector<hipEvent_t> ev_pool;
@@ -340,7 +345,8 @@ hipError_t enqueue_forward(cas_ctx* c, int T, const uint8_t* skip, int aq) {
     at.n_tree_host = c->n_nodes;  // already the post-call node count
     at.win_sink = c->win_sink;
     at.win_len = c->win_len;
-    const int S = attention_splits_win(at.Lc_host, at.n_tree_host, at.win_sink, at.win_len);
+    const int S = c->kv4_call ? c->kv4_run.S
+                              : attention_splits_win(at.Lc_host, at.n_tree_host, at.win_sink, at.win_len);
     at.part_o = c->d_part;
     at.part_ml = c->d_part + (size_t)S * H * T * hd;
     // act_quant 1: int8 codes against the int8 copy; 2: int4 codes (one per
@@ -429,7 +435,15 @@ hipError_t enqueue_forward(cas_ctx* c, int T, const uint8_t* skip, int aq) {
         at.qscale = fused_q ? c->d_xs : nullptr;
         at.qmax = qmax;
         at.no_merge = mx_o ? 1 : 0;
-        RUN(CAS_K_ATTN, launch_attention(et, at, s));
+        if (c->kv4_call) {
+            Kv4AttnArgs a4{};
+            a4.a = at;
+            a4.kv4 = c->kv4 + (size_t)l * Hkv * (c->ctx_cap / 32) * 34 * hd;
+            a4.plan = c->kv4_run;
+            RUN(CAS_K_ATTN, launch_attention_kv4(a4, s));
+        } else {
+            RUN(CAS_K_ATTN, launch_attention(et, at, s));
+        }
         if (aq && !fused_q && !qx_o)
             RUN(CAS_K_QUANT, launch_quant_rows(et, c->d_ao, T, H * hd, c->d_xq, c->d_xs, 1, qmax, s));
         GemmArgs go{};
@@ -603,7 +617,7 @@ hipError_t enqueue_prefill(cas_ctx* c, int T, int logit_rows) {
 
 std::string graph_key(const cas_ctx* c, int T, const uint8_t* skip, int aq, int S) {
     std::string k = std::to_string(T) + ":" + std::to_string(aq) + ":" + std::to_string(S) + ":" +
-                    (c->gemv ? "g:" : "m:") +
+                    (c->gemv ? "g:" : "m:") + (c->kv4_call ? std::to_string(c->kv4_run.jt) + "k:" : "") +
                     std::to_string(c->win_sink) + ":" + std::to_string(c->win_len) + ":";
     for (int l = 0; l < c->cfg.n_layers; ++l) k.push_back(skip && skip[l] ? '1' : '0');
     return k;
@@ -620,9 +634,22 @@ cas_status check_ready(cas_ctx* c, const uint8_t* skip) {
     return CAS_OK;
 }
 
+// Brings the 4-bit copy up to the committed slots' whole records.
+hipError_t kv4_pack(cas_ctx* c) {
+    const int t0 = c->kv4_len / 32, t1 = c->Lc / 32;
+    if (t1 <= t0) return hipSuccess;
+    const cas_config& f = c->cfg;
+    const hipError_t e = timed(c, CAS_K_QUANT, [&]() -> hipError_t {
+        return launch_kv4_pack(c->kc, c->vt, f.n_layers * f.n_kv_heads, f.head_dim, c->ctx_cap, t0, t1 - t0, c->kv4,
+                               c->stream);
+    });
+    if (e == hipSuccess) c->kv4_len = 32 * t1;
+    return e;
+}
+
 cas_status do_forward(cas_ctx* c, const int32_t* tokens, const int32_t* parent, int n, int node_offset,
                       const uint8_t* skip, int aq, float* logits_host, bool allow_graph = true, int win_sink = 0,
-                      int win_len = 0) {
+                      int win_len = 0, bool kv4 = false) {
     const cas_config& f = c->cfg;
     if (!tokens || !parent) return fail(c, CAS_ERR_ARG, "tokens and tree_parent must not be NULL");
     if (win_sink < 0 || win_len < 0) return fail(c, CAS_ERR_ARG, "attn_sink and attn_window must be >= 0");
@@ -649,11 +676,16 @@ cas_status do_forward(cas_ctx* c, const int32_t* tokens, const int32_t* parent, 
     }
     if (aq == 1 && !c->int8_ready) return fail(c, CAS_ERR_STATE, "act_quant 1 needs cas_build_int8 first");
     if (aq == 2 && !c->int4_ready) return fail(c, CAS_ERR_STATE, "act_quant 2 needs cas_build_int4 first");
+    if (kv4 && !c->kv4) return fail(c, CAS_ERR_STATE, "the 4-bit KV copy needs cas_build_kv4 first");
     std::vector<int> depth;
     std::string why;
     if (!tree_depths(parent, node_offset, n, c->parent, &depth, &why)) return fail(c, CAS_ERR_TREE, why);
     cas_status st = check_ready(c, skip);
     if (st != CAS_OK) return st;
+    if (kv4) {
+        const hipError_t e4 = kv4_pack(c);
+        if (e4 != hipSuccess) return hip_fail(c, e4, "4-bit KV copy");
+    }
 
     // upload tokens, parents and the step parameters through a pinned buffer
     hipEvent_t ev = nullptr;
@@ -680,7 +712,15 @@ cas_status do_forward(cas_ctx* c, const int32_t* tokens, const int32_t* parent, 
     c->n_nodes = node_offset + n;
     c->win_sink = win_sink;
     c->win_len = win_len;
-    const int S = attention_splits_win(c->Lc, c->n_nodes, win_sink, win_len);
+    c->kv4_call = kv4;
+    int S = attention_splits_win(c->Lc, c->n_nodes, win_sink, win_len);
+    if (kv4) {
+        // (as many splits as the partials' buffer takes for the call's rows)
+        const size_t row = (size_t)f.n_heads * n * (f.head_dim + 2) * 4;
+        c->kv4_run = kv4_plan(c->Lc, c->n_nodes, n, f.n_heads, f.n_kv_heads, f.head_dim, win_sink, win_len,
+                              (int)std::min<size_t>(c->part_bytes / row, 64));
+        S = c->kv4_run.S;
+    }
     hipError_t e;
     if (c->graphs && !c->prof && allow_graph) {
         const std::string key = graph_key(c, n, skip, aq, S);
@@ -719,7 +759,7 @@ cas_status do_forward(cas_ctx* c, const int32_t* tokens, const int32_t* parent, 
         c->parent[node_offset + i] = parent[i];
         c->token[node_offset + i] = tokens[i];
     }
-    c->verified_n = (node_offset == 0 && !any_skip && !aq && win_len == 0) ? n : 0;
+    c->verified_n = (node_offset == 0 && !any_skip && !aq && win_len == 0 && !kv4) ? n : 0;
     c->logits_rows = n;
     if (logits_host) {
         HIPCHK(c, hipMemcpyAsync(logits_host, c->d_logits, sizeof(float) * (size_t)n * f.vocab, hipMemcpyDeviceToHost,
@@ -1136,6 +1176,31 @@ cas_status cas_forward_draft(cas_ctx* c, const int32_t* tokens, const int32_t* p
                       o->attn_window);
 }
 
+cas_status cas_build_kv4(cas_ctx* c) {
+    if (!c) return CAS_ERR_ARG;
+    const cas_config& f = c->cfg;
+    if (c->et != ET_BF16) return fail(c, CAS_ERR_UNSUPPORTED, "the 4-bit KV copy needs a bf16 model");
+    if ((long)f.n_layers * f.n_kv_heads > 65535) return fail(c, CAS_ERR_UNSUPPORTED, "too many layers and kv heads");
+    if (c->kv4) return CAS_OK;
+    int cur = -1;
+    HIPCHK(c, hipGetDevice(&cur));
+    if (cur != c->dev) HIPCHK(c, hipSetDevice(c->dev));
+    const size_t bytes = (size_t)f.n_layers * f.n_kv_heads * (c->ctx_cap / 32) * 34 * f.head_dim;
+    const hipError_t e = dalloc(c, &c->kv4, bytes);
+    if (e != hipSuccess) (void)hipGetLastError();  // (the launches after it report the last error)
+    if (cur != c->dev) (void)hipSetDevice(cur);
+    if (e != hipSuccess) return fail(c, CAS_ERR_OOM, "hipMalloc of the 4-bit KV copy");
+    c->kv4_len = 0;
+    return CAS_OK;
+}
+
+cas_status cas_forward_draft_kv4(cas_ctx* c, const int32_t* tokens, const int32_t* parent, int32_t n,
+                                 int32_t node_offset, const cas_draft_opts* o, float* logits_host) {
+    if (!c) return CAS_ERR_ARG;
+    return do_forward(c, tokens, parent, n, node_offset, o ? o->skip_mask : nullptr, o ? o->act_quant : 0, logits_host,
+                      true, o ? o->attn_sink : 0, o ? o->attn_window : 0, true);
+}
+
 cas_status cas_prefill(cas_ctx* c, const int32_t* tokens, int32_t n) {
     if (!c) return CAS_ERR_ARG;
     if (!tokens || n < 1) return fail(c, CAS_ERR_ARG, "prefill needs tokens and n >= 1");
@@ -1199,6 +1264,7 @@ static cas_status kv_transfer(cas_ctx* c, int32_t layer, void* k, void* v, int32
 
 cas_status cas_kv_load(cas_ctx* c, int32_t layer, const void* k, const void* v, int32_t n) {
     if (!c) return CAS_ERR_ARG;
+    c->kv4_len = 0;  // (its slots are packed again by the next forward that reads them)
     return kv_transfer(c, layer, (void*)k, (void*)v, n, true);
 }
 
@@ -1211,6 +1277,7 @@ cas_status cas_set_committed(cas_ctx* c, int32_t n) {
     if (!c) return CAS_ERR_ARG;
     if (n < 0 || n > c->cfg.max_ctx) return fail(c, CAS_ERR_CAPACITY, "committed length out of range");
     c->Lc = n;
+    c->kv4_len = std::min(c->kv4_len, n / 32 * 32);
     c->n_nodes = 0;
     c->verified_n = 0;
     return CAS_OK;
@@ -1758,7 +1825,7 @@ static bool attention_kv4_shape(int32_t Lc, int32_t n_tree, int32_t T, int32_t H
 size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
                                        int32_t sink, int32_t window) {
     if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return 0;
-    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window);
+    const size_t S = (size_t)kv4_plan(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window).S;
     return S > 1 ? S * H * T * ((size_t)hd + 2) * 4 : 0;
 }
 
@@ -1794,9 +1861,9 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     a.a.ctx_cap = n4 > 0 ? ctx_cap : 32;
     a.a.win_sink = window ? sink : 0;
     a.a.win_len = window;
-    const size_t S = (size_t)kv4_attention_splits(Lc, n_tree, T, H, Hkv, hd, a.a.win_sink, a.a.win_len);
+    a.plan = kv4_plan(Lc, n_tree, T, H, Hkv, hd, a.a.win_sink, a.a.win_len);
     a.a.part_o = (float*)work;
-    a.a.part_ml = a.a.part_o + S * H * T * hd;
+    a.a.part_ml = a.a.part_o + (size_t)a.plan.S * H * T * hd;
     a.kv4 = (const uint8_t*)kv4;
     a.n4 = n4;
     a.kr = (const uint16_t*)k;

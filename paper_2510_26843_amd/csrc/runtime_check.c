@@ -12,7 +12,7 @@
  * Part 2 (skipped when no device can be opened, or with --host-only) runs
  * small fp32 and bf16 grouped-query decoders with random weights through
  * loads, int8 and int4 copies, prefill, many rounds of drafts (skip masks,
- * int8 and int4 activations, windows, appended levels), verify, top-K,
+ * int8 and int4 activations, windows, 4-bit KV, appended levels), verify, top-K,
  * acceptance and compaction with varying tree sizes (more shapes than the
  * graph cache holds), profiling, direct launches, KV load and read, and the
  * error paths that must leave the context unchanged.  It checks statuses and
@@ -142,6 +142,27 @@ static void host_checks(void) {
     CHECK(cas_op_attn_merge_work_bytes(4, 32, 128, 9) == 0);
     CHECK(cas_op_gemm_qx(2, NULL, NULL, NULL, 4096, 4096, 1, 127, NULL, NULL, 0, NULL) != CAS_OK);
     CHECK(cas_op_copy(NULL, NULL, 16, NULL) != CAS_OK);
+
+    /* the 4-bit KV cache: sizes and refusals (no pointer is followed) */
+    void* p = (void*)(uintptr_t)4096;
+    CHECK(cas_build_kv4(NULL) == CAS_ERR_ARG);
+    CHECK(cas_forward_draft_kv4(NULL, par, par, 1, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_bytes(8, 128, 4096) == (size_t)8 * 128 * 34 * 128);
+    CHECK(cas_op_kv4_bytes(8, 96, 4096) == 0 && cas_op_kv4_bytes(8, 128, 33) == 0);
+    CHECK(cas_op_kv4_append(NULL, p, 64, 64, 1, 0, NULL, NULL, NULL, 0, 1, 64, p, 32, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_append(p, p, 64, 64, INT32_MAX, INT32_MAX, NULL, NULL, NULL, 0, 1, 64, p, 32, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_append(p, p, 64, 64, 1, 0, NULL, (float*)p, NULL, 4, 1, 64, p, 32, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_append(p, p, INT64_MIN, 64, 1, 0, NULL, NULL, NULL, 0, 1, 64, p, 32, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_append(p, p, 64, 64, 1, 0, NULL, NULL, NULL, 0, INT32_MAX, 64, p, 32, NULL) == CAS_ERR_UNSUPPORTED);
+    CHECK(cas_op_kv4_read(p, 32, INT32_MAX, INT32_MAX, 1, 64, p, p, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_kv4_read(p, INT32_MIN, 0, 1, 1, 64, p, p, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_attention_kv4_work_bytes(100, 1, 129, 8, 2, 64, 0, 0) == 0);
+    CHECK(cas_op_attention_kv4_work_bytes(INT32_MAX, INT32_MAX, 1, 8, 2, 64, 0, 0) == 0);
+    CHECK(cas_op_attention_kv4_work_bytes(1 << 19, 128, 128, 32, 8, 128, 4, 100000) > 0);
+    CHECK(cas_op_attention_kv4(p, p, 64, 0, NULL, p, 64, 10, 1, 1, 8, 2, 64, 0, 0, (uint64_t*)p, p, p, 1 << 20, NULL) ==
+          CAS_ERR_ARG);
+    CHECK(cas_op_attention_kv4(p, p, 64, INT32_MIN, p, p, INT32_MAX, 10, 1, 1, 8, 2, 64, 0, 0, (uint64_t*)p, p, p,
+                               1 << 20, NULL) == CAS_ERR_ARG);
 }
 
 /* ------------------------------------------------------------ part 2: on a device */
@@ -290,6 +311,9 @@ static void run_model(const shape_t* s) {
     CHECK(cas_forward(c, tok, par, 1, 0, NULL, 1, NULL) == CAS_ERR_STATE);  /* no int8 copy yet */
     OK(c, cas_build_int8(c));
     OK(c, cas_build_int4(c));
+    CHECK(cas_forward_draft_kv4(c, tok, par, 1, 0, NULL, NULL) == CAS_ERR_STATE);  /* no 4-bit KV copy yet */
+    CHECK(cas_build_kv4(c) == (s->bf16 ? CAS_OK : CAS_ERR_UNSUPPORTED));
+    CHECK(cas_build_kv4(c) == (s->bf16 ? CAS_OK : CAS_ERR_UNSUPPORTED));
 
     /* prefill, then KV read back and reload */
     int32_t* prompt = (int32_t*)malloc(sizeof(int32_t) * 300);
@@ -322,6 +346,13 @@ static void run_model(const shape_t* s) {
         cas_draft_opts o = {skip, r % 3, r % 5 == 0 ? 2 : 0, r % 5 == 0 ? 32 : 0};
         OK(c, cas_forward_draft(c, tok, par, 1, 0, &o, NULL));
         OK(c, cas_topk(c, 1, 4, ids, probs));
+        if (s->bf16 && r % 2) {
+            /* over the 4-bit copy: the root again, and on some rounds the whole tree */
+            OK(c, cas_forward_draft_kv4(c, tok, par, r % 8 == 1 ? n : 1, 0, r % 6 == 1 ? NULL : &o, NULL));
+            CHECK(cas_accept_tree(c, 1, acc, &na, &bonus) == CAS_ERR_STATE);
+            CHECK(cas_forward_draft_kv4(c, tok, par, 0, 0, &o, NULL) == CAS_ERR_ARG);
+            OK(c, cas_forward_draft(c, tok, par, 1, 0, &o, NULL));
+        }
         if (n > 1) {
             /* the rest of the tree appended in two draft calls */
             const int m = 1 + (n - 1) / 2;

@@ -240,12 +240,13 @@ class LatencyModel:
 class DraftConfig:
     """A draft model: a DSIA variant of the target (skip mask over the
     layers, optional quantised activations: 1 = W8A8, 2 = W4A4, optional sink
-    + window attention) or prompt lookup (skip is None and pld is True)."""
+    + window attention, optional 4-bit KV) or prompt lookup (skip is None and pld is True)."""
     name: str
     skip: Optional[Tuple[int, ...]] = None
     act_quant: int = 0
     pld: bool = False
     window: Optional[Tuple[int, int]] = None  # efficient attention: (sink, window) committed slots
+    kv4: bool = False               # committed KV from its 4-bit copy (Model.build_kv4)
 
     def run_layers(self, n_layers: int) -> frozenset:
         if self.pld:
@@ -345,7 +346,7 @@ class LibraryBackend:
 
     def draft(self, tokens, parents, node_offset: int, cfg: DraftConfig, K: int):
         self.m.forward(tokens, parents, node_offset, skip=list(cfg.skip) if cfg.skip else None,
-                       act_quant=cfg.act_quant, logits=False, attn_window=cfg.window)
+                       act_quant=cfg.act_quant, logits=False, attn_window=cfg.window, kv4=cfg.kv4)
         return self.m.topk(K, len(tokens))
 
     def verify(self, tokens, parents) -> Tuple[List[int], int]:

@@ -45,24 +45,31 @@ def skip_mask(n_layers: int, rule: str) -> Optional[List[int]]:
 
 
 def parse_draft(spec: str, n_layers: int):
-    """A draft configuration from '<skip rule>[+int8|+int4][@sink:window]'
-    -> (skip mask, act_quant 0/1/2, window)."""
+    """A draft configuration from '<skip rule>[+int8|+int4][+kv4][@sink:window]'
+    -> (skip mask, act_quant 0/1/2, window); draft_kv4 tells of the +kv4."""
     window = None
     if "@" in spec:
         spec, w = spec.split("@")
         sink, win = w.split(":")
         window = (int(sink), int(win))
+    spec = spec[:-4] if spec.endswith("+kv4") else spec
     aq = 1 if spec.endswith("+int8") else 2 if spec.endswith("+int4") else 0
     return skip_mask(n_layers, spec.split("+")[0]), aq, window
 
 
+def draft_kv4(spec: str) -> bool:
+    """Whether a draft configuration reads the committed KV from its 4-bit copy."""
+    return spec.split("@")[0].endswith("+kv4")
+
+
 def algorithmic_bytes(shape, T: int, Lc: int, run_layers: int, int8: int = 0,
-                      window: Optional[Tuple[int, int]] = None) -> int:
+                      window: Optional[Tuple[int, int]] = None, kv4: bool = False) -> int:
     """Bytes one forward must move: the weights of the layers that run (bf16
     or fp32; int8 = 1: int8 codes, 2: 4-bit codes, plus fp32 per-channel
     scales) and the LM head once, the KV reads of all visible slots (only
-    the sink and the window of the committed ones under a window) and the
-    writes of the new ones, the embedding rows and the fp32 logits."""
+    the sink and the window of the committed ones under a window; 17/64 of the
+    committed whole records' bytes with kv4) and the writes of the new ones,
+    the embedding rows and the fp32 logits."""
     if window and window[1] > 0:
         Lc = min(Lc, window[0] + window[1])
     es = 2 if shape.dtype == "bf16" else 4
@@ -75,6 +82,8 @@ def algorithmic_bytes(shape, T: int, Lc: int, run_layers: int, int8: int = 0,
         b = run_layers * shape.layer_params() * es
     b += shape.vocab * shape.d_model * es
     b += run_layers * 2 * kv_row * (Lc + T)
+    if kv4:
+        b -= run_layers * 2 * kv_row * (Lc // 32 * 32) * 47 // 64
     b += run_layers * 2 * kv_row * T
     b += T * shape.d_model * es + T * shape.vocab * 4
     return b
@@ -95,17 +104,17 @@ def tree_for(T: int) -> List[int]:
 
 
 def time_forward(model, toks, parents, skip, aq: bool, reps: int, warmup: int = 3,
-                 window: Optional[Tuple[int, int]] = None) -> Dict[str, float]:
+                 window: Optional[Tuple[int, int]] = None, kv4: bool = False) -> Dict[str, float]:
     """Wall time per forward over `reps` back-to-back calls (logits stay on
     the device), median of three such batches."""
     for _ in range(warmup):
-        model.forward(toks, parents, 0, skip=skip, act_quant=aq, logits=False, attn_window=window)
+        model.forward(toks, parents, 0, skip=skip, act_quant=aq, logits=False, attn_window=window, kv4=kv4)
     model.sync()
     runs = []
     for _ in range(3):
         t0 = time.perf_counter()
         for _ in range(reps):
-            model.forward(toks, parents, 0, skip=skip, act_quant=aq, logits=False, attn_window=window)
+            model.forward(toks, parents, 0, skip=skip, act_quant=aq, logits=False, attn_window=window, kv4=kv4)
         model.sync()
         runs.append((time.perf_counter() - t0) / reps * 1e3)
     return {"ms": statistics.median(runs), "ms_min": min(runs), "ms_max": max(runs)}
@@ -129,8 +138,9 @@ def sweep(model, shape, Ts: Sequence[int], ctxs: Sequence[int], drafts: Sequence
             for name, skip, aq, window in configs:
                 model.set_committed(ctx)
                 run = shape.n_layers - (sum(skip) if skip else 0)
-                r = time_forward(model, toks, parents, skip, aq, reps, window=window)
-                b = algorithmic_bytes(shape, T, ctx, run, int8=aq, window=window)
+                kv4 = draft_kv4(name)
+                r = time_forward(model, toks, parents, skip, aq, reps, window=window, kv4=kv4)
+                b = algorithmic_bytes(shape, T, ctx, run, int8=aq, window=window, kv4=kv4)
                 ctx_vis = min(ctx, window[0] + window[1]) if window and window[1] > 0 else ctx
                 fl = algorithmic_flops(shape, T, ctx_vis, run, float(np.mean(depth)))
                 rec = {"config": name, "T": T, "ctx": ctx, "run_layers": run, "act_quant": aq,
@@ -163,8 +173,8 @@ def main(argv=None) -> None:
     ap.add_argument("--T", default="1,8,16,32,64,128")
     ap.add_argument("--ctx", default="512,2048,8192")
     ap.add_argument("--drafts", default="",
-                    help="draft configurations separated by ';', e.g. 'odd;q3;odd+int8;odd+int4;odd@4:1024' "
-                         "(skip rule, +int8 or +int4 activations, @sink:window attention)")
+                    help="draft configurations separated by ';', e.g. 'odd;q3;odd+int8;odd+int4+kv4;odd@4:1024' "
+                         "(skip rule, +int8 or +int4 activations, +kv4: 4-bit KV, @sink:window attention)")
     ap.add_argument("--reps", type=int, default=20)
     ap.add_argument("--out", default="")
     ap.add_argument("--md", default="")
@@ -179,10 +189,12 @@ def main(argv=None) -> None:
     w = synth.gen_weights(shape, seed=0)
     m = cas.Model(shape, max_ctx=max(ctxs) + max(Ts), max_tree=max(128, max(Ts)), device=0)
     m.load_weights(w)
-    if any(d.split("@")[0].endswith("+int8") for d in drafts):
+    if any("+int8" in d for d in drafts):
         m.build_int8()
-    if any(d.split("@")[0].endswith("+int4") for d in drafts):
+    if any("+int4" in d for d in drafts):
         m.build_int4()
+    if any(draft_kv4(d) for d in drafts):
+        m.build_kv4()
     del w
     log(f"[latency] {args.shape} ready in {time.perf_counter() - t0:.1f} s")
     recs = sweep(m, shape, Ts, ctxs, drafts, args.reps, log)
