@@ -502,10 +502,11 @@ __device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
 template <int HD> struct Kv4Query {
     i32x8 hi, lo;
     int sh, sl;
-    // scores of half HALF of a record's slots: codes k, scale byte HALF of ks
-    template <int HALF> __device__ __forceinline__ f32x4 scores(const i32x8 k, int ks) const {
-        f32x4 c = {0.f, 0.f, 0.f, 0.f};
-        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, hi, c, 4, 0, HALF, ks, 0, sh);
+    // scores of half HALF of a record's slots (codes k, scale byte HALF of ks), in two parts
+    template <int HALF> __device__ __forceinline__ f32x4 hi_scores(const i32x8 k, int ks) const {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, hi, f32x4{0.f, 0.f, 0.f, 0.f}, 4, 0, HALF, ks, 0, sh);
+    }
+    template <int HALF> __device__ __forceinline__ f32x4 lo_scores(const i32x8 k, int ks, f32x4 c) const {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, lo, c, 4, 0, HALF, ks, 0, sl);
     }
 };
@@ -559,19 +560,19 @@ template <int HD> __device__ __forceinline__ Kv4Query<HD> kv4_query_get(const Kv
     return x;
 }
 
-// One key tile: QK(S) gives the scores of its 32 slots, V(m, f) the value
-// fragments of d tiles 2m and 2m + 1.  MASKED: vm has the visibility of the
+// One key tile: S are the scores of its 32 slots, V(m, f) gives the value
+// fragments of d tiles 2m and 2m + 1.  next() computes the next tile's scores:
+// its MFMA run while this one's probabilities and values are converted.  MASKED: vm has the visibility of the
 // lane's 8 slots to its row of each query tile.
 // The maximum follows the scores only where one passes it by KV4_SLACK (in
 // log2 units): probabilities are then at most 2^KV4_SLACK, which neither bf16
 // nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
 // sum of the (rounded) probabilities is one more row of the PV product.
 static constexpr float KV4_SLACK = 8.f;
-template <int HD, int JT, bool MASKED, typename SF, typename VF>
-__device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], float c, SF QK, VF V, const uint32_t (&vm)[JT]) {
+template <int HD, int JT, bool MASKED, typename VF, typename NF>
+__device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
+                                         const uint32_t (&vm)[JT], NF next) {
     constexpr int NDT = HD / 16;
-    f32x4 S[JT][2];
-    QK(S);
     if constexpr (MASKED) {
 #pragma unroll
         for (int j = 0; j < JT; ++j)
@@ -600,6 +601,7 @@ __device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], float c, SF QK,
             st[j].top = mn + KV4_SLACK / c;
         }
     }
+    next();
     i32x4 P[JT];
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
@@ -648,23 +650,29 @@ __device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], float c, SF QK,
     }
 }
 
-// The same for a tile of the 4-bit cache.
-template <int HD, int JT, bool MASKED>
-__device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], const Kv4Tile<HD>& t, const Kv4Query<HD> (&Q)[JT],
-                                          float c, const uint32_t (&vm)[JT]) {
-    auto QK = [&](f32x4 (&Sc)[JT][2]) {
-        i32x8 k0 = {}, k1 = {};
+// The scores of a tile of the 4-bit cache, and its step.
+template <int HD, int JT>
+__device__ __forceinline__ void kv4_scores(f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, const Kv4Query<HD> (&Q)[JT]) {
+    i32x8 k0 = {}, k1 = {};
 #pragma unroll
-        for (int u = 0; u < HD / 32; ++u) {
-            k0[u] = (int)t.k[0][u];
-            k1[u] = (int)t.k[1][u];
-        }
+    for (int u = 0; u < HD / 32; ++u) {
+        k0[u] = (int)t.k[0][u];
+        k1[u] = (int)t.k[1][u];
+    }
 #pragma unroll
-        for (int j = 0; j < JT; ++j) {
-            Sc[j][0] = Q[j].template scores<0>(k0, (int)t.ks);
-            Sc[j][1] = Q[j].template scores<1>(k1, (int)t.ks);
-        }
-    };
+    for (int j = 0; j < JT; ++j) {
+        S[j][0] = Q[j].template hi_scores<0>(k0, (int)t.ks);
+        S[j][1] = Q[j].template hi_scores<1>(k1, (int)t.ks);
+    }
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        S[j][0] = Q[j].template lo_scores<0>(k0, (int)t.ks, S[j][0]);
+        S[j][1] = Q[j].template lo_scores<1>(k1, (int)t.ks, S[j][1]);
+    }
+}
+template <int HD, int JT, bool MASKED, typename NF>
+__device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, float c,
+                                          const uint32_t (&vm)[JT], NF next) {
     float vs[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) vs[e] = kv4_scale(((uint32_t)t.vs[e >> 2] >> (8 * (e & 3))) & 0xffu);
@@ -679,7 +687,7 @@ __device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], const Kv4Tile<
             f[1][i] = (int)halves_hi(p[2 * i], p[2 * i + 1]);
         }
     };
-    kv4_step<HD, JT, MASKED>(st, c, QK, V, vm);
+    kv4_step<HD, JT, MASKED>(st, S, c, V, vm, next);
 }
 
 static constexpr int KV4_WAVES = 8;
@@ -717,7 +725,7 @@ struct Kv4Tiles {
 // the decoder's bf16 cache (tiled).
 template <int HD, int JT, int TAIL>
 __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArgs k4, float c) {
-    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, RS = HD + 4, W = KV4_WAVES, D = JT == 1 ? 3 : 2;
+    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, RS = HD + 4, W = KV4_WAVES, D = 3;
     const AttnArgs& a = k4.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
@@ -770,7 +778,10 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
         const uint32_t vm[1] = {attn_vis8(pt * 32 + 8 * g, Lc, n_slots, win, an0, an1)};
         if (TAIL == 0 || pt * 32 < n4) {
             const Kv4Query<HD> Q[1] = {kv4_query_get<HD>(sm_q[ej], g, r)};
-            kv4_step4<HD, 1, true>(es, load(pt), Q, c, vm);
+            const Kv4Tile<HD> t = load(pt);
+            f32x4 Sc[1][2];
+            kv4_scores<HD, 1>(Sc, t, Q);
+            kv4_step4<HD, 1, true>(es, Sc, t, c, vm, [] {});
         } else if constexpr (TAIL != 0) {
             const uint16_t *kt, *vt;
             if constexpr (TAIL == 1) {
@@ -781,21 +792,19 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
                 vt = (const uint16_t*)a.vt + ((size_t)kvh * a.ctx_cap + pt * 32) * HD;
             }
             auto row = [&](int sl) { return (size_t)(min(pt * 32 + sl, n_slots - 1) - n4) * HD; };
-            auto QK = [&](f32x4 (&Sc)[1][2]) {
-                Sc[0][0] = Sc[0][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            f32x4 Sc[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
-                for (int u = 0; u < UD; ++u) {
-                    const i32x4 Qf = *(const i32x4*)(qrow + g * DG + u * 8);
+            for (int u = 0; u < UD; ++u) {
+                const i32x4 Qf = *(const i32x4*)(qrow + g * DG + u * 8);
 #pragma unroll
-                    for (int h2 = 0; h2 < 2; ++h2) {
-                        i32x4 Kf;
-                        if constexpr (TAIL == 1)
-                            Kf = *(const i32x4*)(kt + row(8 * (r >> 2) + 4 * h2 + (r & 3)) + g * DG + u * 8);
-                        else Kf = *(const i32x4*)(kt + (h2 * UD + u) * 512 + lane * 8);
-                        Sc[0][h2] = mfma_step<ET_BF16>(Kf, Qf, Sc[0][h2]);
-                    }
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    i32x4 Kf;
+                    if constexpr (TAIL == 1)
+                        Kf = *(const i32x4*)(kt + row(8 * (r >> 2) + 4 * h2 + (r & 3)) + g * DG + u * 8);
+                    else Kf = *(const i32x4*)(kt + (h2 * UD + u) * 512 + lane * 8);
+                    Sc[0][h2] = mfma_step<ET_BF16>(Kf, Qf, Sc[0][h2]);
                 }
-            };
+            }
             auto V = [&](int m, i32x4 (&f)[2]) {
                 constexpr int WR = 512 / HD;
 #pragma unroll
@@ -811,7 +820,7 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
                     }
                 }
             };
-            kv4_step<HD, 1, true>(es, c, QK, V, vm);
+            kv4_step<HD, 1, true>(es, Sc, c, V, vm, [] {});
         }
     }
     mfma_result_pad();
@@ -825,13 +834,22 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
     }
 
     // the whole tiles
-    const uint32_t all[JT] = {};
-    for (int i = 0; i < n;) {
+    if (n > 0) {
+        const uint32_t all[JT] = {};
+        f32x4 Sc[D][JT][2];
+        kv4_scores<HD, JT>(Sc[0], ring[0], Q);
+        mfma_result_pad();  // (the loop's branch follows)
+        for (int i = 0; i < n;) {
 #pragma unroll
-        for (int k = 0; k < D; ++k) {
-            kv4_step4<HD, JT, false>(st, ring[k], Q, c, all);
-            ring[k] = load(tl.whole(w0 + min(i + D, n - 1) * W));
-            if (++i >= n) break;
+            for (int k = 0; k < D; ++k) {
+                kv4_step4<HD, JT, false>(st, Sc[k], ring[k], c, all,
+                                         [&] { kv4_scores<HD, JT>(Sc[(k + 1) % D], ring[(k + 1) % D], Q); });
+                // (pins them to this step: the compiler would move them to their use)
+#pragma unroll
+                for (int j = 0; j < JT; ++j) asm volatile("" : "+v"(Sc[(k + 1) % D][j][0]), "+v"(Sc[(k + 1) % D][j][1]));
+                ring[k] = load(tl.whole(w0 + min(i + D, n - 1) * W));
+                if (++i >= n) break;
+            }
         }
     }
     mfma_result_pad();
@@ -959,13 +977,14 @@ Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink
     float least = INFINITY;
     for (int jt = 1; jt <= (nct > 1 ? 2 : 1); ++jt) {
         const int z = (nct + jt - 1) / jt;
-        for (int S = 1; S == 1 || (S <= ATT_MAX_SPLITS && S <= max_S && S <= n_log); ++S) {
+        for (const int S : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 20, 24, 28, 32, 40, 48, 56, ATT_MAX_SPLITS}) {
+            if (S > 1 && (S > max_S || S > n_log)) break;
             const float wgs = (float)Hkv * z * S;
             const int rounds = (int)((wgs + 255) / 256);
             const int steps = ((n_log + S - 1) / S + KV4_WAVES - 1) / KV4_WAVES;
-            const float step = (jt == 1 ? 0.73f : 1.07f) * (hd == 128 ? 1.f : 0.6f);
-            float us = rounds * ((jt == 1 ? 3.0f : 3.9f) + steps * step);
-            if (S > 1) us += 2.8f + 0.35e-6f * S * H * T * hd * 8;
+            const float step = (jt == 1 ? 0.71f : 1.05f) * (hd == 128 ? 1.f : 0.57f);
+            float us = rounds * ((jt == 1 ? 3.f : 4.f) + steps * step);
+            if (S > 1) us += 2.8f + 0.36e-6f * S * H * T * hd * 8;
             if (us < least) {
                 least = us;
                 best = Kv4Plan{jt, S};

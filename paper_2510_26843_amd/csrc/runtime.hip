@@ -1761,6 +1761,7 @@ cas_status cas_op_gemm_qx(int32_t wtype, const int8_t* W, const float* ws, const
 // ---- the 4-bit KV cache
 
 static constexpr int KV4_MAX_CAP = 1 << 20;
+static constexpr int KV4_MAX_HEADS = 4096;  // query heads: 16-row tiles of one kv head stay a grid dimension
 static bool kv4_shape(int32_t Hkv, int32_t hd, int32_t ctx_cap, cas_status* st) {
     *st = CAS_ERR_ARG;
     if (Hkv < 1 || ctx_cap < 32 || ctx_cap % 32) return false;
@@ -1819,14 +1820,17 @@ cas_status cas_op_kv4_read(const void* kv4, int32_t ctx_cap, int32_t slot0, int3
 static bool attention_kv4_shape(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
                                 int32_t sink, int32_t window) {
     return T >= 1 && T <= 128 && n_tree >= 1 && n_tree <= 128 && Lc >= 0 && Lc <= KV4_MAX_CAP - n_tree && Hkv >= 1 &&
-           H >= 1 && H % Hkv == 0 && H <= 65535 && sink >= 0 && window >= 0 && (hd == 64 || hd == 128);
+           H >= 1 && H % Hkv == 0 && H <= KV4_MAX_HEADS && sink >= 0 && window >= 0 && (hd == 64 || hd == 128);
+}
+
+static size_t attention_kv4_work(const Kv4Plan& p, int32_t T, int32_t H, int32_t hd) {
+    return p.S > 1 ? (size_t)p.S * H * T * ((size_t)hd + 2) * 4 : 0;
 }
 
 size_t cas_op_attention_kv4_work_bytes(int32_t Lc, int32_t n_tree, int32_t T, int32_t H, int32_t Hkv, int32_t hd,
                                        int32_t sink, int32_t window) {
     if (!attention_kv4_shape(Lc, n_tree, T, H, Hkv, hd, sink, window)) return 0;
-    const size_t S = (size_t)kv4_plan(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window).S;
-    return S > 1 ? S * H * T * ((size_t)hd + 2) * 4 : 0;
+    return attention_kv4_work(kv4_plan(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window), T, H, hd);
 }
 
 cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap, int32_t n4, const void* k,
@@ -1846,9 +1850,10 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     }
     if (n4 < n_slots && (!k || !v || kv_cap < n_slots - n4 || !aligned16(k) || !aligned16(v))) return CAS_ERR_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(work) || ((uintptr_t)anc & 7)) return CAS_ERR_ARG;
-    const size_t need = cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window);
-    if (need && (!work || work_bytes < need)) return CAS_ERR_ARG;
     Kv4AttnArgs a{};
+    a.plan = kv4_plan(Lc, n_tree, T, H, Hkv, hd, window ? sink : 0, window);
+    const size_t need = attention_kv4_work(a.plan, T, H, hd);
+    if (need && (!work || work_bytes < need)) return CAS_ERR_ARG;
     a.a.q = q;
     a.a.anc = anc;
     a.a.Lc_host = Lc;
@@ -1861,7 +1866,6 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     a.a.ctx_cap = n4 > 0 ? ctx_cap : 32;
     a.a.win_sink = window ? sink : 0;
     a.a.win_len = window;
-    a.plan = kv4_plan(Lc, n_tree, T, H, Hkv, hd, a.a.win_sink, a.a.win_len);
     a.a.part_o = (float*)work;
     a.a.part_ml = a.a.part_o + (size_t)a.plan.S * H * T * hd;
     a.kv4 = (const uint8_t*)kv4;

@@ -239,6 +239,33 @@ def test_values_that_are_not_finite_reach_their_rows_only(n4):
         assert np.array_equal(got[~bad], want[~bad])
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_query_that_is_not_finite_spoils_its_row_only(value):
+    c = _Case(4, 2, 64, 3, 3, 200, 192, junk=False)
+    want = c.run().double().cpu().numpy().reshape(3, 4, 64)
+    c.qd[1, 2, 17] = value
+    got = c.run().double().cpu().numpy().reshape(3, 4, 64)
+    assert np.isnan(got[1, 2]).all()
+    got[1, 2] = want[1, 2]
+    assert np.array_equal(got, want)
+
+
+def test_query_ranges():
+    """Queries whose elements differ by many binades, tiny and large ones: the
+    scores stay those of bf16 queries."""
+    r = _rng(3)
+    for scale in (2.0**-60, 2.0**-8, 1.0):
+        c = _Case(4, 2, 128, 5, 5, 300, 288)
+        c.q = R.bf16(r.normal(0, 1, c.q.shape) * np.exp2(r.integers(-12, 3, c.q.shape)) * scale)
+        c.qd = _dev_bf16(c.q)
+        c.check(c.run())
+
+
+def test_many_query_heads_of_one_kv_head():
+    c = _Case(96, 1, 64, 2, 2, 77, None)
+    c.check(c.run())
+
+
 def test_same_bits_again_and_on_another_stream():
     c = _Case(8, 2, 128, 5, 20, 3000, 2976)
     a = c.run()

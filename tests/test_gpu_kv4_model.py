@@ -231,6 +231,25 @@ def test_refusals(weights):
     f.close()
 
 
+def test_device_checks(weights):
+    """The build with device checks: none fails in a round over the copy, and
+    one that does (slots past a limit set for the test) is reported."""
+    shape = GQA
+    m = cas.Model(shape, max_ctx=512, max_tree=64, debug=True)
+    m.load_weights(weights["gqa_small"])
+    m.build_kv4()
+    m.prefill(_prompt(shape, 150))
+    toks, parents = _tree(shape, 20)
+    a = m.forward(toks, parents, kv4=True)
+    assert np.isfinite(a).all() and m.debug_check() == 0
+    m.debug_limit_slots(160)
+    m.forward(toks, parents, kv4=True, logits=False)
+    assert m.debug_check() != 0
+    m.debug_limit_slots(0)
+    assert np.array_equal(_bits(m.forward(toks, parents, kv4=True)), _bits(a)) and m.debug_check() == 0
+    m.close()
+
+
 def test_small_cache_and_many_splits(weights):
     """A model whose partial-state buffer is small (a short cache, a small
     tree): a call takes no more splits than it holds."""

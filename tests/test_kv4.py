@@ -75,7 +75,8 @@ ATTEND = dict(q=P, kv4=P, cap=65536, n4=32000, k=P, v=P, kv_cap=20, Lc=32008, n_
     (dict(n4=-32), cas.ERR_ARG), (dict(n4=32032), cas.ERR_ARG), (dict(kv_cap=10), cas.ERR_ARG),
     (dict(n4=32011, cap=32000), cas.ERR_ARG), (dict(T=0), cas.ERR_ARG), (dict(T=129), cas.ERR_ARG),
     (dict(n_tree=0), cas.ERR_ARG), (dict(n_tree=129), cas.ERR_ARG), (dict(Lc=-1), cas.ERR_ARG),
-    (dict(Lc=2**31 - 1), cas.ERR_ARG), (dict(H=7), cas.ERR_ARG), (dict(Hkv=0), cas.ERR_ARG),
+    (dict(Lc=2**31 - 1), cas.ERR_ARG), (dict(H=7), cas.ERR_ARG), (dict(H=4098), cas.ERR_ARG), (dict(Lc=1 << 20), cas.ERR_ARG),
+    (dict(Hkv=0), cas.ERR_ARG),
     (dict(sink=-1), cas.ERR_ARG), (dict(window=-1), cas.ERR_ARG), (dict(hd=80), cas.ERR_UNSUPPORTED),
     (dict(cap=40), cas.ERR_ARG)])
 def test_attention_refuses(change, status):
