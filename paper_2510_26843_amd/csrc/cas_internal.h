@@ -311,7 +311,11 @@ struct Kv4AttnArgs {
     const uint16_t *kr, *vr;  // [Hkv][kv_cap][hd], slot n4 first
     int kv_cap;
     Kv4Plan plan;
-    int direct;  // set by the launch: one split, the kernel writes the output itself
+    // set by the launch: one split, the kernel writes the output itself; the
+    // query heads of a kv head, attn_head_rows, and ceil(2^32 / x) (0 for 1) of
+    // it and of the splits
+    int direct, G, Rp;
+    uint32_t inv_Rp, inv_S;
 };
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s);
 

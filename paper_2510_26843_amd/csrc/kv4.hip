@@ -14,17 +14,18 @@
 // codes, key scales, value scales), each part in the order in which the
 // attention's lanes read it (kv4_* below; MFMA operands as in kernels.hip):
 //   lane (g, r) of a wave reads, in one 16-byte (hd 128; 8 at hd 64) load per
-//   half s, the key codes of slot 8 (r/4) + 4 s + r%4, d = g hd/4 + [0, hd/4),
-//   which lie in one block: one key scale per lane and half;
+//   half s, the key codes of slot 8 (r/4) + 4 s + r%4, d = g hd/4 + [0, hd/4):
+//   with the block's scale (one per lane and half) an operand of the scaled
+//   MFMA as it stands, the keys are never converted;
 //   and in 16-byte loads the value codes of slots 8g + [0, 8) at the d of
 //   block r/w (w = 512 / hd) with d % w = r % w: one scale per slot and lane,
-//   and the two d of a byte are w apart, so one conversion serves two of the
-//   PV product's d tiles.
-// The conversion (two codes and a scale to two bf16) is one instruction.
+//   and the two d of a byte are w apart, so one conversion (two codes and a
+//   scale to two bf16, one instruction) serves two of the PV product's d tiles.
 #include "kernel_common.h"
 
 namespace cas {
 
+typedef unsigned short uint16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -409,21 +410,31 @@ hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
 
 // ---------------------------------------------------------------- attention
 
-// Workgroup = (run of key tiles, kv head, JT query tiles of 16 rows); its four
-// waves take the run's tiles (32 slots) in turn, each with the running maximum
-// and sum of a softmax of its own, and join them through LDS at the end.
-// MFMA operands as in k_attn_bf16: scores come out with slots along the row
-// index, which is the k-order of P in the PV product, so probabilities stay in
-// registers.  Tiles of the 4-bit cache are converted to bf16 in registers;
-// the next tile's codes are loaded before the current one is used.  The
-// probabilities enter the PV product as bf16, each off by at most 2^-8 of
-// itself; their sum and the output stay in fp32.
+// Workgroup = (run of key tiles, kv head, JT query tiles of 16 rows); its eight
+// waves share the run's tiles (32 slots), each with the running maximum and sum
+// of a softmax of its own, and join them through LDS at the end.  The scores
+// come out of the scaled MFMA with slots along the row index, which is the
+// k-order of P in the PV product (on bf16 MFMA, its values converted in
+// registers), so probabilities stay in registers.  They enter that product as
+// bf16, each off by at most 2^-8 of itself; their sum, which is of the rounded
+// ones, and the output stay in fp32.
 //
-// A tile whose slots some row does not see whole takes the masked form: the
-// scores of unseen slots are replaced before use, and values that are not
+// Whole tiles, which every row sees, are a wave's main loop: a ring of three
+// tiles' codes in registers, loaded two steps ahead, the next tile's scores
+// issued under this one's exponentials and conversions.  The others, the edge
+// tiles (Kv4Tiles), take the masked form and are spread over the waves first:
+// the scores of unseen slots are replaced before use, and values that are not
 // finite (an unused slot may hold anything) are taken out of the product, in
-// which a probability of 0 does not hide them, and given back to the rows
-// that see their slot.
+// which a probability of 0 does not hide them, and given back to the rows that
+// see their slot.
+//
+// What bounds it: for few rows the bytes (one row of 8B heads over 131072
+// slots: 142.6 MB in 26 us, and 4 to join); for many the vector unit, which a step keeps busy
+// for all but a tenth of its time: per tile and query tile 8 exponentials a
+// lane at twice an instruction's cost, 4 conversions of P, and at hd 128 32 of
+// the values' codes and 32 to bring the two d tiles apart, shared by JT (128
+// rows of 8B heads over 16001 slots: 33.7 GFLOP in 40.3 us, 840 TFLOP/s); for short calls the
+// launch, the query's conversion and the two joins.
 
 template <int HD> struct Kv4Tile {  // a lane's share of a record
     uint32_t k[2][HD / 32];
@@ -431,11 +442,11 @@ template <int HD> struct Kv4Tile {  // a lane's share of a record
     i32x4 v[HD / 64];
     i32x2 vs;
 };
-template <int HD> __device__ __forceinline__ Kv4Tile<HD> kv4_load(const uint8_t* rec, int lane) {
-    const int r = lane & 15, g = lane >> 4;
+template <int HD> __device__ __forceinline__ Kv4Tile<HD> kv4_load(const uint8_t* rec, uint32_t lane) {
+    const uint32_t r = lane & 15, g = lane >> 4;
     Kv4Tile<HD> t;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (uint32_t s = 0; s < 2; ++s) {
         if constexpr (HD == 128) {
             const i32x4 w = *(const i32x4*)(rec + (s * 64 + lane) * 16);
 #pragma unroll
@@ -448,7 +459,7 @@ template <int HD> __device__ __forceinline__ Kv4Tile<HD> kv4_load(const uint8_t*
     }
     t.ks = *(const uint16_t*)(rec + 32 * HD + ((HD == 128 ? g : g >> 1) * 16 + r) * 2);
 #pragma unroll
-    for (int m = 0; m < HD / 64; ++m) t.v[m] = *(const i32x4*)(rec + 16 * HD + (m * 64 + lane) * 16);
+    for (uint32_t m = 0; m < HD / 64; ++m) t.v[m] = *(const i32x4*)(rec + 16 * HD + (m * 64 + lane) * 16);
     t.vs = *(const i32x2*)(rec + 33 * HD + (r / (512 / HD)) * 32 + 8 * g);
     return t;
 }
@@ -562,14 +573,15 @@ template <int HD> __device__ __forceinline__ Kv4Query<HD> kv4_query_get(const Kv
 
 // One key tile: S are the scores of its 32 slots, V(m, f) gives the value
 // fragments of d tiles 2m and 2m + 1.  next() computes the next tile's scores:
-// its MFMA run while this one's probabilities and values are converted.  MASKED: vm has the visibility of the
-// lane's 8 slots to its row of each query tile.
+// its MFMA run while this one's probabilities and values are converted.
+// MASKED: vm has the visibility of the lane's 8 slots to its row of each query
+// tile; CARE: values of unseen slots may not be finite.
 // The maximum follows the scores only where one passes it by KV4_SLACK (in
 // log2 units): probabilities are then at most 2^KV4_SLACK, which neither bf16
 // nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
 // sum of the (rounded) probabilities is one more row of the PV product.
 static constexpr float KV4_SLACK = 8.f;
-template <int HD, int JT, bool MASKED, typename VF, typename NF>
+template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
 __device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
                                          const uint32_t (&vm)[JT], NF next) {
     constexpr int NDT = HD / 16;
@@ -619,7 +631,7 @@ __device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][
     for (int m = 0; m < NDT / 2; ++m) {
         i32x4 Vf[2];
         V(m, Vf);
-        if constexpr (MASKED) {
+        if constexpr (CARE) {
             i32x4 bad[2] = {take_nonfinite(Vf[0]), take_nonfinite(Vf[1])};
             int any = 0;
 #pragma unroll
@@ -670,7 +682,7 @@ __device__ __forceinline__ void kv4_scores(f32x4 (&S)[JT][2], const Kv4Tile<HD>&
         S[j][1] = Q[j].template lo_scores<1>(k1, (int)t.ks, S[j][1]);
     }
 }
-template <int HD, int JT, bool MASKED, typename NF>
+template <int HD, int JT, bool MASKED, bool CARE, typename NF>
 __device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, float c,
                                           const uint32_t (&vm)[JT], NF next) {
     float vs[8];
@@ -687,7 +699,7 @@ __device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT]
             f[1][i] = (int)halves_hi(p[2 * i], p[2 * i + 1]);
         }
     };
-    kv4_step<HD, JT, MASKED>(st, S, c, V, vm, next);
+    kv4_step<HD, JT, MASKED, CARE>(st, S, c, V, vm, next);
 }
 
 static constexpr int KV4_WAVES = 8;
@@ -734,38 +746,51 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
     if (a.sp && !dcheck(a.chk, Lc >= 0 && n_slots <= a.sp->cap && a.sp->cap <= a.ctx_cap, CHK_ATTN_SLOTS)) return;
     const int n4 = a.sp ? Lc & ~31 : k4.n4;
     const AttnWindow win(Lc, n_tree, a.win_sink, a.win_len);
-    const int T = a.T, G = a.H / a.Hkv, Rp = attn_head_rows(T);
-    const int nct = attn_query_tiles(T, G);
+    const int T = a.T, G = k4.G, Rp = k4.Rp;
     const uint16_t* q = (const uint16_t*)a.q;
+    // packed row p's token and head of the group (rows past the group's: a valid row, not stored)
+    auto head_of = [&](int p) { return k4.inv_Rp ? (int)__umulhi((uint32_t)p, k4.inv_Rp) : p; };
+    auto row_of = [&](int p, int* t) {
+        const int hg = head_of(p);
+        *t = min(p - hg * Rp, T - 1);
+        return q + ((size_t)*t * a.H + kvh * G + min(hg, G - 1)) * HD;
+    };
 
-    // this thread's piece of the query rows (rows past the group's read a valid
-    // row; what comes of them is not stored)
+    // this thread's piece of the query rows
     __shared__ Kv4QueryLds sm_q[JT];
+    __shared__ float sm_m[W][16], sm_l[W][16];
+    __shared__ __attribute__((aligned(16))) float sm_o[W][16][RS];  // a wave's part: 32 x (hd + 4) bf16 or its state
     constexpr int PP = HD / 32;
     const int qj = threadIdx.x / (64 * PP), qr = threadIdx.x / (4 * PP) % 16, qk = threadIdx.x / PP % 4,
               qp = threadIdx.x % PP;
     i32x4 qv = {0, 0, 0, 0};
-    if (qj < JT) {
-        const int p = (JT * rc + qj) * 16 + qr;
-        const int t = min(p % Rp, T - 1), head = kvh * G + min(p / Rp, G - 1);
-        qv = *(const i32x4*)(q + ((size_t)t * a.H + head) * HD + qk * DG + qp * 8);
-    }
+    int tok;
+    if (qj < JT) qv = *(const i32x4*)(row_of((JT * rc + qj) * 16 + qr, &tok) + qk * DG + qp * 8);
     // (each wave takes edge tiles for one of the query tiles, ej; this lane's row of it)
-    const int ej = JT == 1 ? 0 : wave % JT, ep = (JT * rc + ej) * 16 + r;
-    const int et = min(ep % Rp, T - 1);
-    const uint16_t* qrow = q + ((size_t)et * a.H + kvh * G + min(ep / Rp, G - 1)) * HD;
-    const uint64_t an0 = a.anc[2 * et], an1 = a.anc[2 * et + 1];
+    const int ej = JT == 1 ? 0 : wave % JT;
+    const uint16_t* qrow = row_of((JT * rc + ej) * 16 + r, &tok);
+    const uint64_t an0 = a.anc[2 * tok], an1 = a.anc[2 * tok + 1];
 
-    // the split's share of the whole tiles, of which the wave takes every W-th
+    // The split's share of the whole tiles, and the wave's run [w0, w0 + n) of
+    // it.  Edge tiles are dealt to the splits, then to the waves from the last
+    // on; a wave with one takes EC whole tiles less, the time that it takes:
+    // at(w) tiles lie before wave w's (a sum that rises by cost / W per wave,
+    // less EC per edge tile; it ends at ns, so cut to [0, ns] it never falls).
+    constexpr int EC = (TAIL ? 4 : 2) / JT, WJ = W / JT;
     const Kv4Tiles tl(win, Lc, n_slots, n4);
-    const int w0 = tl.n_whole * split / S + wave, w1 = tl.n_whole * (split + 1) / S;
-    const int n = (w1 - w0 + W - 1) / W;
+    auto by_S = [&](int x) { return k4.inv_S ? (int)__umulhi((uint32_t)x, k4.inv_S) : x; };
+    const int s0 = by_S(tl.n_whole * split), ns = by_S(tl.n_whole * (split + 1)) - s0;
+    const int workers = S * WJ, e_all = by_S(tl.n_edge) / WJ, e_more = tl.n_edge - e_all * workers;
+    const int more = by_S(max(e_more - split + S - 1, 0)) * JT;  // the last waves that take one more
+    const int cost = ns + EC * (W * e_all + more);
+    auto at = [&](int w) { return min(max(cost * w / W - EC * (e_all * w + max(0, w - (W - more))), 0), ns); };
+    const int w0 = s0 + at(wave), n = at(wave + 1) - at(wave);
     const uint8_t* rec0 = k4.kv4 + (size_t)kvh * (a.ctx_cap >> 5) * (34 * HD);
     auto load = [&](int pt) { return kv4_load<HD>(rec0 + (size_t)pt * (34 * HD), lane); };
     Kv4Tile<HD> ring[D];
     if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < D; ++k) ring[k] = load(tl.whole(w0 + min(k, n - 1) * W));
+        for (int k = 0; k < D; ++k) ring[k] = load(tl.whole(w0 + min(k, n - 1)));
     }
     if (qj < JT) kv4_query_put<HD>(sm_q[qj], qr, qk, qp, qv);
     __syncthreads();
@@ -773,54 +798,83 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
     // the edge tiles, over the splits and the waves of each query tile
     Kv4State<HD> es[1];
     es[0].clear();
-    for (int e = split + S * (W / JT - 1 - wave / JT); e < tl.n_edge; e += S * (W / JT)) {
+    for (int e = split + S * (WJ - 1 - wave / JT); e < tl.n_edge; e += workers) {
         const int pt = tl.edge(e);
         const uint32_t vm[1] = {attn_vis8(pt * 32 + 8 * g, Lc, n_slots, win, an0, an1)};
+        f32x4 Sc[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
         if (TAIL == 0 || pt * 32 < n4) {
-            const Kv4Query<HD> Q[1] = {kv4_query_get<HD>(sm_q[ej], g, r)};
             const Kv4Tile<HD> t = load(pt);
-            f32x4 Sc[1][2];
+            const Kv4Query<HD> Q[1] = {kv4_query_get<HD>(sm_q[ej], g, r)};
             kv4_scores<HD, 1>(Sc, t, Q);
-            kv4_step4<HD, 1, true>(es, Sc, t, c, vm, [] {});
-        } else if constexpr (TAIL != 0) {
-            const uint16_t *kt, *vt;
-            if constexpr (TAIL == 1) {
-                kt = k4.kr + (size_t)kvh * k4.kv_cap * HD;
-                vt = k4.vr + (size_t)kvh * k4.kv_cap * HD;
-            } else {
-                kt = (const uint16_t*)a.kc + ((size_t)kvh * a.ctx_cap + pt * 32) * HD;
-                vt = (const uint16_t*)a.vt + ((size_t)kvh * a.ctx_cap + pt * 32) * HD;
+            // (scales of 252 and more, whose values bf16 may not hold)
+            uint32_t big = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t x = (uint32_t)t.vs[i], y = x & (x << 1);
+                big |= y & (y << 2) & (y << 4) & 0x80808080u;
             }
+            if (__any(big)) kv4_step4<HD, 1, true, true>(es, Sc, t, c, vm, [] {});
+            else kv4_step4<HD, 1, true, false>(es, Sc, t, c, vm, [] {});
+        } else if constexpr (TAIL != 0) {
+            // keys and values of bf16 as MFMA fragments; rows' values come as 16-byte
+            // pieces along the rows and are turned in the wave's part of sm_o
+            // (gathered by 2 bytes from memory they took 5 us)
+            constexpr int NV = HD / 16, VS = HD + 4, WR = 512 / HD;  // pieces per lane or d tiles; row stride in LDS
+            const uint16_t* kt = TAIL == 1 ? k4.kr + (size_t)kvh * k4.kv_cap * HD
+                                           : (const uint16_t*)a.kc + ((size_t)kvh * a.ctx_cap + pt * 32) * HD;
+            const uint16_t* vt = TAIL == 1 ? k4.vr + (size_t)kvh * k4.kv_cap * HD
+                                           : (const uint16_t*)a.vt + ((size_t)kvh * a.ctx_cap + pt * 32) * HD;
             auto row = [&](int sl) { return (size_t)(min(pt * 32 + sl, n_slots - 1) - n4) * HD; };
-            f32x4 Sc[1][2] = {{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}};
+            i32x4 ek[UD][2], ev[NV];
+#pragma unroll
+            for (int u = 0; u < UD; ++u)
+#pragma unroll
+                for (int h2 = 0; h2 < 2; ++h2)
+                    ek[u][h2] = *(const i32x4*)(TAIL == 1 ? kt + row(8 * (r >> 2) + 4 * h2 + (r & 3)) + g * DG + u * 8
+                                                         : kt + (h2 * UD + u) * 512 + lane * 8);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int p = i * 64 + lane, d = 32 * (r / WR) + WR * i + r % WR;
+                ev[i] = *(const i32x4*)(TAIL == 1 ? vt + row(p / (HD / 8)) + p % (HD / 8) * 8
+                                                  : vt + ((d >> 4) * 64 + g * 16 + (d & 15)) * 8);
+            }
+            uint16_t* stage = (uint16_t*)&sm_o[wave][0][0];
+            uint16x2 most = {0, 0};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(uint16x2, (uint32_t)ev[i][w] & 0x7fff7fffu));
+                if constexpr (TAIL == 1) {
+                    const int p = i * 64 + lane;
+                    i32x2* to = (i32x2*)(stage + p / (HD / 8) * VS + p % (HD / 8) * 8);
+                    to[0] = i32x2{ev[i][0], ev[i][1]};
+                    to[1] = i32x2{ev[i][2], ev[i][3]};
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int u = 0; u < UD; ++u) {
                 const i32x4 Qf = *(const i32x4*)(qrow + g * DG + u * 8);
 #pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
-                    i32x4 Kf;
-                    if constexpr (TAIL == 1)
-                        Kf = *(const i32x4*)(kt + row(8 * (r >> 2) + 4 * h2 + (r & 3)) + g * DG + u * 8);
-                    else Kf = *(const i32x4*)(kt + (h2 * UD + u) * 512 + lane * 8);
-                    Sc[0][h2] = mfma_step<ET_BF16>(Kf, Qf, Sc[0][h2]);
-                }
+                for (int h2 = 0; h2 < 2; ++h2) Sc[0][h2] = mfma_step<ET_BF16>(ek[u][h2], Qf, Sc[0][h2]);
             }
             auto V = [&](int m, i32x4 (&f)[2]) {
-                constexpr int WR = 512 / HD;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int d = 32 * (r / WR) + WR * (2 * m + h) + r % WR;
                     if constexpr (TAIL == 1) {
+                        const uint16_t* at = stage + 8 * g * VS + 32 * (r / WR) + WR * (2 * m + h) + r % WR;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            f[h][i] = (int)((uint32_t)vt[row(8 * g + 2 * i) + d] |
-                                            ((uint32_t)vt[row(8 * g + 2 * i + 1) + d] << 16));
+                            f[h][i] = (int)((uint32_t)at[2 * i * VS] | ((uint32_t)at[(2 * i + 1) * VS] << 16));
                     } else {
-                        f[h] = *(const i32x4*)(vt + ((d >> 4) * 64 + g * 16 + (d & 15)) * 8);
+                        f[h] = ev[2 * m + h];
                     }
                 }
             };
-            kv4_step<HD, 1, true>(es, Sc, c, V, vm, [] {});
+            if (__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) kv4_step<HD, 1, true, true>(es, Sc, c, V, vm, [] {});
+            else kv4_step<HD, 1, true, false>(es, Sc, c, V, vm, [] {});
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
     mfma_result_pad();
@@ -839,24 +893,29 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
         f32x4 Sc[D][JT][2];
         kv4_scores<HD, JT>(Sc[0], ring[0], Q);
         mfma_result_pad();  // (the loop's branch follows)
+        // Of the two waves of a SIMD the elder goes first wherever both can, and
+        // ends at two thirds of the other's time, which is then alone: it
+        // yields in every third step (128 rows of 8B heads over 16001 slots
+        // 41.5 -> 40.1 us).
+        if (wave >= W / 2) __builtin_amdgcn_s_setprio(1);
         for (int i = 0; i < n;) {
 #pragma unroll
             for (int k = 0; k < D; ++k) {
-                kv4_step4<HD, JT, false>(st, Sc[k], ring[k], c, all,
+                if (wave < W / 2) k == 1 ? __builtin_amdgcn_s_setprio(0) : __builtin_amdgcn_s_setprio(2);
+                kv4_step4<HD, JT, false, false>(st, Sc[k], ring[k], c, all,
                                          [&] { kv4_scores<HD, JT>(Sc[(k + 1) % D], ring[(k + 1) % D], Q); });
                 // (pins them to this step: the compiler would move them to their use)
 #pragma unroll
                 for (int j = 0; j < JT; ++j) asm volatile("" : "+v"(Sc[(k + 1) % D][j][0]), "+v"(Sc[(k + 1) % D][j][1]));
-                ring[k] = load(tl.whole(w0 + min(i + D, n - 1) * W));
+                ring[k] = load(tl.whole(w0 + min(i + D, n - 1)));
                 if (++i >= n) break;
             }
         }
+        __builtin_amdgcn_s_setprio(0);
     }
     mfma_result_pad();
 
     // ---- join the waves, one query tile after another
-    __shared__ float sm_m[W][16], sm_l[W][16];
-    __shared__ __attribute__((aligned(16))) float sm_o[W][16][RS];
     constexpr int D4 = HD / 4;
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
@@ -870,8 +929,8 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
         __syncthreads();
         for (int idx = threadIdx.x; idx < 16 * D4; idx += 64 * W) {
             const int rr = idx / D4, d4 = (idx % D4) * 4;
-            const int ct = JT * rc + j, p = ct * 16 + rr, hg = p / Rp, t = p % Rp;
-            if (ct >= nct || hg >= G || t >= T) continue;
+            const int p = (JT * rc + j) * 16 + rr, hg = head_of(p), t = p - hg * Rp;
+            if (hg >= G || t >= T) continue;
             float mw[W], M = -INFINITY;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -882,7 +941,7 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
             float L = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const float f = attn_merge_weight(mw[w], M);
+                const float f = __builtin_amdgcn_exp2f(mw[w] - M);
                 attn_merge_o(acc, *(const f32x4*)(&sm_o[w][rr][d4]), f);
                 attn_merge_l(L, sm_l[w][rr], f);
             }
@@ -902,7 +961,7 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
 // The join of S splits' partial states: SG (at most 256 / (hd / 4)) groups of
 // hd/4 threads per row take every SG-th split, four at a time, and join through
 // LDS: with 32 splits of one row one round of loads where a thread that takes
-// all splits waits for four (4.6 us, KV4_T2).
+// all splits waits for four (32 heads' row: 4.0 us for 4.6).
 static constexpr int KV4_MERGE_THREADS = 256;
 template <int HD> __global__ void __launch_bounds__(KV4_MERGE_THREADS) k_kv4_merge(const AttnArgs a, int S, int SG) {
     constexpr int D4 = HD / 4, NG = KV4_MERGE_THREADS / D4;
@@ -962,14 +1021,14 @@ template <int HD> static hipError_t kv4_merge_go(const AttnArgs& a, int S, hipSt
 
 // Query tiles per workgroup (jt) and splits of the key tiles (S), by the time
 // that a call takes as the sum of its parts in microseconds, fitted to calls of
-// 1 to 128 rows over 33 to 131071 slots with every jt and S up to 32 (10% off
+// 1 to 128 rows over 33 to 131071 slots with every jt and S up to 32 (13% off
 // in the mean): the rounds in which 256 CUs take the workgroups one at a time
 // (two waves per SIMD), each its start and end and its waves' steps, and the
 // merge of the partials.  Two query tiles share a step's conversions but leave
 // fewer workgroups, which end later: 128 rows of 8B heads over 16001 slots take
-// 43 us with 2 tiles and 2 splits, 54 with 1 and 1; 64 rows of 13B heads over
-// 2048 slots 12.5 with 1 and 1, 16.9 with 2 and 2.  One split needs no merge:
-// one row of 13B heads over 500 slots takes 6.5 us with it, 7.9 with two.
+// 40.6 us with 2 tiles and 2 splits, 49.3 with 1 and 1; 64 rows of 13B heads
+// over 2048 slots 10.7 with 1 and 1, 14.8 with 2 and 1.  One split needs no
+// merge: one row of 13B heads over 500 slots takes 5.7 us with it, 7.1 with two.
 Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len, int max_S) {
     const int n_log = AttnWindow(Lc, n_tree, win_sink, win_len).n_log;
     const int nct = attn_query_tiles(T, H / Hkv);
@@ -982,9 +1041,9 @@ Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink
             const float wgs = (float)Hkv * z * S;
             const int rounds = (int)((wgs + 255) / 256);
             const int steps = ((n_log + S - 1) / S + KV4_WAVES - 1) / KV4_WAVES;
-            const float step = (jt == 1 ? 0.71f : 1.05f) * (hd == 128 ? 1.f : 0.57f);
-            float us = rounds * ((jt == 1 ? 3.f : 4.f) + steps * step);
-            if (S > 1) us += 2.8f + 0.36e-6f * S * H * T * hd * 8;
+            const float step = (jt == 1 ? 0.68f : 0.95f) * (hd == 128 ? 1.f : 0.59f);
+            float us = rounds * ((jt == 1 ? 2.3f : 3.5f) + steps * step);
+            if (S > 1) us += 2.9f + 0.33e-6f * S * H * T * hd * 8;
             if (us < least) {
                 least = us;
                 best = Kv4Plan{jt, S};
@@ -1011,6 +1070,12 @@ hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s) {
     const int tail = a.sp ? 2 : k.n4 < a.Lc_host + a.n_tree_host ? 1 : 0;
     const float c = (1.0f / sqrtf((float)a.hd)) * 1.4426950408889634f;
     Kv4AttnArgs k2 = k;
+    k2.G = a.H / a.Hkv;
+    k2.Rp = attn_head_rows(a.T);
+    // (multiplying by these and taking the high word divides exactly below 2^25)
+    auto inverse = [](int d) { return d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u; };
+    k2.inv_Rp = inverse(k2.Rp);
+    k2.inv_S = inverse(S);
     k2.direct = S == 1 && !a.out_tiled && !a.qout && !a.no_merge;
     hipError_t e = hipErrorInvalidValue;
     if (a.hd == 128)
