@@ -49,8 +49,9 @@ EXPORTS = ("cas_create", "cas_destroy", "cas_last_error", "cas_create_error", "c
            "cas_op_attn_merge", "cas_op_attn_merge_work_bytes", "cas_op_gemm_qx", "cas_op_gemm_qx_splits",
            "cas_op_gemm_qx_work_bytes", "cas_op_attention_noalloc", "cas_op_attention_noalloc_max_bytes",
            "cas_debug_build", "cas_debug_check", "cas_debug_limit_slots",
-           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_build_kv4", "cas_forward_draft_kv4", "cas_op_kv4_bytes",
-           "cas_op_kv4_append", "cas_op_kv4_read", "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes")
+           "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_build_kv4",
+           "cas_forward_draft_kv4", "cas_op_kv4_bytes", "cas_op_kv4_append", "cas_op_kv4_read",
+           "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes")
 # device check codes (cas_debug_check)
 DEVICE_CHECKS = ["none", "tree size", "token id", "parent order", "slot capacity", "RoPE position",
                  "KV write slot", "attention slots", "compaction path", "acceptance parent"]
@@ -483,12 +484,13 @@ def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, s
 
 # the 4-bit KV cache (device byte tensors of kv4_bytes(...) bytes)
 
-def _stream_at(t, stream, what: str) -> int:
-    """The stream of a call on tensor t, which has to be on the current device."""
+def _stream_at(stream, what: str, *tensors) -> int:
+    """The stream of a call on tensors (or None), which have to be on the current device."""
     import torch
     dev = torch.cuda.current_device()
-    if t.get_device() != dev:
-        raise CasError(ERR_ARG, what + ": the tensors are not on the current device")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise CasError(ERR_ARG, what + ": the tensors are not on the current device")
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream)
 
 
@@ -503,7 +505,7 @@ def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int
     ldv elements apart) into slots slot0 .. slot0 + T - 1.  With cos and sin
     ([positions][hd/2] fp32) the keys are rotated by pos ([T] int32; None:
     their slots) first."""
-    s = _stream_at(kv4, stream, "cas_op_kv4_append")
+    s = _stream_at(stream, "cas_op_kv4_append", k, v, kv4, pos, cos, sin)
     ld = Hkv * hd
     _ochk(lib().cas_op_kv4_append(_dp(k), _dp(v), ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0,
                                   _dp(pos), _dp(cos), _dp(sin), 0 if cos is None else int(cos.shape[0]), Hkv, hd,
@@ -512,7 +514,7 @@ def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int
 
 def op_kv4_read(kv4, ctx_cap: int, slot0: int, n: int, Hkv: int, hd: int, k, v, stream=None) -> None:
     """The values of slots slot0 .. slot0 + n - 1 into k, v [Hkv][n][hd] bf16."""
-    s = _stream_at(kv4, stream, "cas_op_kv4_read")
+    s = _stream_at(stream, "cas_op_kv4_read", kv4, k, v)
     _ochk(lib().cas_op_kv4_read(_dp(kv4), ctx_cap, slot0, n, Hkv, hd, _dp(k), _dp(v), s), "cas_op_kv4_read")
 
 
@@ -522,7 +524,7 @@ def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int
     """Tree attention with slots [0, n4) from the 4-bit cache and the others
     from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap: k's second
     dimension by default)."""
-    s = _stream_at(q, stream, "cas_op_attention_kv4")
+    s = _stream_at(stream, "cas_op_attention_kv4", q, kv4, anc, out, k, v, work)
     L = lib()
     if work is None:
         need = L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)

@@ -52,14 +52,14 @@ def parse_draft(spec: str, n_layers: int):
         spec, w = spec.split("@")
         sink, win = w.split(":")
         window = (int(sink), int(win))
-    spec = spec[:-4] if spec.endswith("+kv4") else spec
+    spec = spec.replace("+kv4", "")
     aq = 1 if spec.endswith("+int8") else 2 if spec.endswith("+int4") else 0
     return skip_mask(n_layers, spec.split("+")[0]), aq, window
 
 
 def draft_kv4(spec: str) -> bool:
     """Whether a draft configuration reads the committed KV from its 4-bit copy."""
-    return spec.split("@")[0].endswith("+kv4")
+    return "kv4" in spec.split("@")[0].split("+")[1:]
 
 
 def algorithmic_bytes(shape, T: int, Lc: int, run_layers: int, int8: int = 0,

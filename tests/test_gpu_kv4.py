@@ -266,6 +266,56 @@ def test_many_query_heads_of_one_kv_head():
     c.check(c.run())
 
 
+@pytest.mark.parametrize("H,Hkv,hd", HEADS[:3])
+@pytest.mark.parametrize("T,n_tree,Lc,n4", [(128, 128, 33, 96), (40, 100, 20, 64), (3, 40, 0, 32), (9, 70, 60, 128)])
+def test_some_of_the_rounds_nodes_in_4_bits(H, Hkv, hd, T, n_tree, Lc, n4):
+    c = _Case(H, Hkv, hd, T, n_tree, Lc, n4)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("H,Hkv,hd,T", [(33, 1, 128, 128), (64, 1, 64, 128), (41, 1, 64, 100), (80, 2, 128, 61)])
+@pytest.mark.parametrize("Lc,n4,sink,window", [(700, None, 0, 0), (700, 672, 0, 0), (333, 0, 0, 0), (30, None, 0, 0),
+                                               (900, 896, 40, 300)])
+def test_more_query_tiles_than_the_card_has_places(H, Hkv, hd, T, Lc, n4, sink, window):
+    """Over 256 tiles of 16 query rows: workgroups of two (in the third shape
+    an odd number of them)."""
+    c = _Case(H, Hkv, hd, T, T, Lc, n4, sink, window)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("H,Hkv,hd,T", [(8, 1, 128, 1), (4, 2, 64, 3)])
+def test_many_splits(H, Hkv, hd, T):
+    c = _Case(H, Hkv, hd, T, T, 40001, None)
+    assert cas.lib().cas_op_attention_kv4_work_bytes(40001, T, T, H, Hkv, hd, 0, 0) > 32 * H * T * (hd + 2) * 4
+    c.check(c.run())
+
+
+def test_calls_with_a_tensor_of_the_host_are_refused():
+    c = _Case(4, 2, 64, 3, 3, 100, 96)
+    for name in ("qd", "rec", "kr", "vr", "anc"):
+        x = getattr(c, name)
+        setattr(c, name, x.cpu())
+        with pytest.raises(cas.CasError, match="not on the current device"):
+            c.run()
+        setattr(c, name, x)
+    with pytest.raises(cas.CasError, match="not on the current device"):
+        c.run(work=torch.empty(64, dtype=torch.uint8))
+    rows = torch.zeros((2, 128), dtype=torch.bfloat16, device=DEV)
+    cos, sin = (torch.from_numpy(x).to(DEV) for x in _rope(64, 40))
+    pos = torch.zeros(2, dtype=torch.int32, device=DEV)
+    good = [rows, rows, c.rec, pos, cos, sin]
+    for i in range(6):
+        a = list(good)
+        a[i] = a[i].cpu()
+        with pytest.raises(cas.CasError, match="not on the current device"):
+            cas.op_kv4_append(a[0], a[1], 2, 2, 64, a[2], c.cap, 0, pos=a[3], cos=a[4], sin=a[5])
+    out = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device=DEV)
+    for a in ([c.rec.cpu(), out, out], [c.rec, out.cpu(), out], [c.rec, out, out.cpu()]):
+        with pytest.raises(cas.CasError, match="not on the current device"):
+            cas.op_kv4_read(a[0], c.cap, 0, 2, 2, 64, a[1], a[2])
+    c.check(c.run())
+
+
 def test_same_bits_again_and_on_another_stream():
     c = _Case(8, 2, 128, 5, 20, 3000, 2976)
     a = c.run()

@@ -169,6 +169,25 @@ def test_the_copy_follows_the_cache(weights):
     m.close()
 
 
+@pytest.mark.parametrize("heads,kv_heads,hd", [(40, 8, 128), (64, 8, 64)])
+@pytest.mark.parametrize("opts", [{}, {"attn_window": (40, 100)}], ids=["full", "window"])
+def test_many_heads_and_a_wide_tree(heads, kv_heads, hd, opts):
+    """More tiles of query rows than the card has places: workgroups of two."""
+    shape = synth.ModelShape("many_heads", 1, 512, heads, kv_heads, hd, 1376, 1024, 1e4, 1e-6, "bf16")
+    w = synth.gen_weights(shape, seed=9)
+    m = _model(shape, w, _prompt(shape, 330), quant=False)
+    ref = _model(shape, w, [], kv4=False, quant=False)
+    k, v = m.kv_read(0, 330)
+    k[:, :320], v[:, :320] = _held(k[:, :320]), _held(v[:, :320])
+    ref.kv_load(0, k, v)
+    ref.set_committed(330)
+    toks, parents = _tree(shape, 128)
+    err = _row_err(m.forward(toks, parents, kv4=True, **opts), ref.forward(toks, parents, **opts))
+    assert err < TOL, err
+    m.close()
+    ref.close()
+
+
 def test_graphs_and_direct_launches_give_the_same_bits(weights):
     shape = GQA
     m = _model(shape, weights["gqa_small"], _prompt(shape, 333))
@@ -286,6 +305,8 @@ def test_dytc_and_the_latency_table_take_4_bit_drafts(weights):
     plain, _ = backend.draft([prompt[-1]], [-1], 0, dytc.DraftConfig("odd", odd), 4)
     assert len(set(ids[0]) & set(plain[0])) >= 1
     assert latency.parse_draft("odd+int4+kv4@4:64", 2) == ([0, 1], 2, (4, 64)) and latency.draft_kv4("odd+kv4@4:64")
+    assert latency.parse_draft("odd+kv4+int4", 2) == ([0, 1], 2, None) and latency.draft_kv4("odd+kv4+int4")
+    assert latency.parse_draft("odd", 2) == ([0, 1], 0, None) and not latency.draft_kv4("odd+int8@4:64")
     recs = latency.sweep(m, shape, [1, 4], [100, 640], ["odd", "odd+kv4", "none+int8+kv4@4:64"], reps=2)
     assert len(recs) == 2 * 2 * 4
     by = {(r["config"], r["T"], r["ctx"]): r["bytes"] for r in recs}
