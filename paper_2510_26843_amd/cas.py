@@ -484,14 +484,20 @@ def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, s
 
 # the 4-bit KV cache (device byte tensors of kv4_bytes(...) bytes)
 
-def _stream_at(stream, what: str, *tensors) -> int:
-    """The stream of a call on tensors (or None), which have to be on the current device."""
+def _call_at(stream, what: str, *tensors):
+    """The stream of a call and the addresses of its tensors (None: none),
+    which have to be on the current device."""
     import torch
     dev = torch.cuda.current_device()
+    at = []
     for t in tensors:
-        if t is not None and t.get_device() != dev:
+        if t is None:
+            at.append(None)
+        elif t.get_device() == dev:
+            at.append(t.data_ptr())
+        else:
             raise CasError(ERR_ARG, what + ": the tensors are not on the current device")
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream), at
 
 
 def kv4_bytes(Hkv: int, hd: int, ctx_cap: int) -> int:
@@ -505,17 +511,17 @@ def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int
     ldv elements apart) into slots slot0 .. slot0 + T - 1.  With cos and sin
     ([positions][hd/2] fp32) the keys are rotated by pos ([T] int32; None:
     their slots) first."""
-    s = _stream_at(stream, "cas_op_kv4_append", k, v, kv4, pos, cos, sin)
+    s, (ka, va, at, pa, ca, sa) = _call_at(stream, "cas_op_kv4_append", k, v, kv4, pos, cos, sin)
     ld = Hkv * hd
-    _ochk(lib().cas_op_kv4_append(_dp(k), _dp(v), ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0,
-                                  _dp(pos), _dp(cos), _dp(sin), 0 if cos is None else int(cos.shape[0]), Hkv, hd,
-                                  _dp(kv4), ctx_cap, s), "cas_op_kv4_append")
+    _ochk(lib().cas_op_kv4_append(ka, va, ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0, pa, ca, sa,
+                                  0 if cos is None else int(cos.shape[0]), Hkv, hd, at, ctx_cap, s),
+          "cas_op_kv4_append")
 
 
 def op_kv4_read(kv4, ctx_cap: int, slot0: int, n: int, Hkv: int, hd: int, k, v, stream=None) -> None:
     """The values of slots slot0 .. slot0 + n - 1 into k, v [Hkv][n][hd] bf16."""
-    s = _stream_at(stream, "cas_op_kv4_read", kv4, k, v)
-    _ochk(lib().cas_op_kv4_read(_dp(kv4), ctx_cap, slot0, n, Hkv, hd, _dp(k), _dp(v), s), "cas_op_kv4_read")
+    s, (at, ka, va) = _call_at(stream, "cas_op_kv4_read", kv4, k, v)
+    _ochk(lib().cas_op_kv4_read(at, ctx_cap, slot0, n, Hkv, hd, ka, va, s), "cas_op_kv4_read")
 
 
 def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int, H: int, Hkv: int, hd: int, anc, out,
@@ -524,13 +530,12 @@ def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int
     """Tree attention with slots [0, n4) from the 4-bit cache and the others
     from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap: k's second
     dimension by default)."""
-    s = _stream_at(stream, "cas_op_attention_kv4", q, kv4, anc, out, k, v, work)
     L = lib()
     if work is None:
         need = L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)
         work = _work(need) if need else None
+    s, (qa, at, aa, oa, ka, va, wa) = _call_at(stream, "cas_op_attention_kv4", q, kv4, anc, out, k, v, work)
     if kv_cap is None:
         kv_cap = 0 if k is None else int(k.shape[1])
-    _ochk(L.cas_op_attention_kv4(_dp(q), _dp(kv4), ctx_cap, n4, _dp(k), _dp(v), kv_cap, Lc, n_tree, T, H, Hkv, hd,
-                                 sink, window, _dp(anc), _dp(out), _dp(work), 0 if work is None else work.nbytes, s),
-          "cas_op_attention_kv4")
+    _ochk(L.cas_op_attention_kv4(qa, at, ctx_cap, n4, ka, va, kv_cap, Lc, n_tree, T, H, Hkv, hd, sink, window, aa, oa,
+                                 wa, 0 if work is None else work.nbytes, s), "cas_op_attention_kv4")
