@@ -36,6 +36,11 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // The scale 2^(b - 127) of a scale byte; 255 gives an infinity, with which the
 // conversions return NaN.
 __device__ __forceinline__ float kv4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+// The scale of byte e of a dword for a conversion, which takes the exponent
+// field alone: sign and mantissa are the neighbours' bits.
+__device__ __forceinline__ float kv4_scale_of(uint32_t w, int e) {
+    return __uint_as_float(e < 3 ? w << (23 - 8 * e) : w >> 1);
+}
 // Two codes (byte B of w) as a pair of bf16 values.
 template <int B> __device__ __forceinline__ uint32_t kv4_pair(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
@@ -687,7 +692,7 @@ __device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT]
                                           const uint32_t (&vm)[JT], NF next) {
     float vs[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vs[e] = kv4_scale(((uint32_t)t.vs[e >> 2] >> (8 * (e & 3))) & 0xffu);
+    for (int e = 0; e < 8; ++e) vs[e] = kv4_scale_of((uint32_t)t.vs[e >> 2], e & 3);
     auto V = [&](int m, i32x4 (&f)[2]) {
         const uint32_t w0 = (uint32_t)t.v[m >> 1][2 * (m & 1)], w1 = (uint32_t)t.v[m >> 1][2 * (m & 1) + 1];
         const uint32_t p[8] = {kv4_pair<0>(w0, vs[0]), kv4_pair<1>(w0, vs[1]), kv4_pair<2>(w0, vs[2]),
