@@ -128,6 +128,14 @@ __device__ __forceinline__ i32x4 ld8_bf(const uint16_t* p, bool vec) {
     return v;
 }
 
+// A launch that reports its own error, not an earlier call's (and without the
+// call-configuration calls of the <<<>>> form: 2.35 us of the host for 2.55).
+template <typename... P>
+static hipError_t kv4_launch(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, P... args) {
+    void* at[] = {(void*)&args...};
+    return hipLaunchKernel((const void*)kernel, grid, dim3(threads), at, 0, s);
+}
+
 // ---------------------------------------------------------------- append
 
 // One workgroup = one record (32 slots of a kv head).  Keys are rotated in 64
@@ -323,10 +331,9 @@ template <int HD> __global__ void __launch_bounds__(KV4_THREADS) k_kv4_append(co
 hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s) {
     if (a.T < 1 || a.slot0 < 0 || a.slot0 > a.ctx_cap - a.T || a.Hkv < 1) return hipErrorInvalidValue;
     const dim3 grid(((a.slot0 + a.T - 1) >> 5) - (a.slot0 >> 5) + 1, a.Hkv);
-    if (a.hd == 128) hipLaunchKernelGGL(k_kv4_append<128>, grid, dim3(KV4_THREADS), 0, s, a);
-    else if (a.hd == 64) hipLaunchKernelGGL(k_kv4_append<64>, grid, dim3(KV4_THREADS), 0, s, a);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (a.hd == 128) return kv4_launch(k_kv4_append<128>, grid, KV4_THREADS, s, a);
+    if (a.hd == 64) return kv4_launch(k_kv4_append<64>, grid, KV4_THREADS, s, a);
+    return hipErrorInvalidValue;
 }
 
 // Records tile0 .. tile0 + gridDim.x - 1 of every (layer, kv head) from the
@@ -362,10 +369,9 @@ hipError_t launch_kv4_pack(const void* kc, const void* vt, int heads, int hd, in
     if (tiles < 1 || tile0 < 0 || tile0 + tiles > ctx_cap >> 5 || heads < 1 || heads > 65535) return hipErrorInvalidValue;
     const dim3 grid(tiles, heads);
     const uint16_t *k = (const uint16_t*)kc, *v = (const uint16_t*)vt;
-    if (hd == 128) hipLaunchKernelGGL(k_kv4_pack<128>, grid, dim3(KV4_THREADS), 0, s, k, v, ctx_cap, tile0, kv4);
-    else if (hd == 64) hipLaunchKernelGGL(k_kv4_pack<64>, grid, dim3(KV4_THREADS), 0, s, k, v, ctx_cap, tile0, kv4);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (hd == 128) return kv4_launch(k_kv4_pack<128>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
+    if (hd == 64) return kv4_launch(k_kv4_pack<64>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
+    return hipErrorInvalidValue;
 }
 
 // ---------------------------------------------------------------- read back
@@ -407,10 +413,9 @@ template <int HD> __global__ void __launch_bounds__(KV4_THREADS) k_kv4_read(cons
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
     if (a.n < 1 || a.slot0 < 0 || a.slot0 > a.ctx_cap - a.n || a.Hkv < 1) return hipErrorInvalidValue;
     const dim3 grid(((a.slot0 + a.n - 1) >> 5) - (a.slot0 >> 5) + 1, a.Hkv);
-    if (a.hd == 128) hipLaunchKernelGGL(k_kv4_read<128>, grid, dim3(KV4_THREADS), 0, s, a);
-    else if (a.hd == 64) hipLaunchKernelGGL(k_kv4_read<64>, grid, dim3(KV4_THREADS), 0, s, a);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (a.hd == 128) return kv4_launch(k_kv4_read<128>, grid, KV4_THREADS, s, a);
+    if (a.hd == 64) return kv4_launch(k_kv4_read<64>, grid, KV4_THREADS, s, a);
+    return hipErrorInvalidValue;
 }
 
 // ---------------------------------------------------------------- attention
@@ -1036,8 +1041,7 @@ template <int HD> static hipError_t kv4_merge_go(const AttnArgs& a, int S, hipSt
     int SG = 1;
     while (SG < NG && SG * 2 <= S) SG *= 2;
     const unsigned wgs = ((unsigned)(a.H * a.T) + NG / SG - 1) / (NG / SG);
-    hipLaunchKernelGGL(k_kv4_merge<HD>, dim3(wgs), dim3(KV4_MERGE_THREADS), 0, s, a, S, SG);
-    return hipGetLastError();
+    return kv4_launch(k_kv4_merge<HD>, dim3(wgs), KV4_MERGE_THREADS, s, a, S, SG);
 }
 
 // Query tiles per workgroup (jt) and splits of the key tiles (S), by the time
@@ -1047,9 +1051,9 @@ template <int HD> static hipError_t kv4_merge_go(const AttnArgs& a, int S, hipSt
 // (two waves per SIMD), each its start and end and its waves' steps, and the
 // merge of the partials.  Two query tiles share a step's conversions but leave
 // fewer workgroups, which end later: 128 rows of 8B heads over 16001 slots take
-// 40.6 us with 2 tiles and 2 splits, 49.3 with 1 and 1; 64 rows of 13B heads
-// over 2048 slots 10.7 with 1 and 1, 14.8 with 2 and 1.  One split needs no
-// merge: one row of 13B heads over 500 slots takes 5.7 us with it, 7.1 with two.
+// 38.3 us with 2 tiles and 2 splits, 40.2 with 1 and 1; 64 rows of 13B heads
+// over 2048 slots 9.6 with 1 and 1, 14.2 with 2 and 1.  One split needs no
+// merge: one row of 13B heads over 500 slots takes 5.5 us with it, 7.1 with two.
 Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink, int win_len, int max_S) {
     const int n_log = AttnWindow(Lc, n_tree, win_sink, win_len).n_log;
     const int nct = attn_query_tiles(T, H / Hkv);
@@ -1075,10 +1079,10 @@ Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink
 }
 
 template <int HD, int JT> static hipError_t attn_kv4_go(const Kv4AttnArgs& k, dim3 grid, int tail, float c, hipStream_t s) {
-    if (tail == 0) hipLaunchKernelGGL((k_attn_kv4<HD, JT, 0>), grid, dim3(64 * KV4_WAVES), 0, s, k, c);
-    else if (tail == 1) hipLaunchKernelGGL((k_attn_kv4<HD, JT, 1>), grid, dim3(64 * KV4_WAVES), 0, s, k, c);
-    else hipLaunchKernelGGL((k_attn_kv4<HD, JT, 2>), grid, dim3(64 * KV4_WAVES), 0, s, k, c);
-    return hipGetLastError();
+    return kv4_launch(tail == 0   ? k_attn_kv4<HD, JT, 0>
+                      : tail == 1 ? k_attn_kv4<HD, JT, 1>
+                                  : k_attn_kv4<HD, JT, 2>,
+                      grid, 64 * KV4_WAVES, s, k, c);
 }
 
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s) {
