@@ -439,11 +439,11 @@ hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
 // see their slot.
 //
 // What bounds it: for few rows the bytes (one row of 8B heads over 131072
-// slots: 142.6 MB in 26 us, and 4 to join); for many the vector unit, which a step keeps busy
+// slots: 142.6 MB in 27 us, and 4 to join); for many the vector unit, which a step keeps busy
 // for all but a tenth of its time: per tile and query tile 8 exponentials a
 // lane at twice an instruction's cost, 4 conversions of P, and at hd 128 32 of
 // the values' codes and 32 to bring the two d tiles apart, shared by JT (128
-// rows of 8B heads over 16001 slots: 33.7 GFLOP in 40.3 us, 840 TFLOP/s); for short calls the
+// rows of 8B heads over 16001 slots: 33.7 GFLOP in 39.7 us, 850 TFLOP/s); for short calls the
 // launch, the query's conversion and the two joins.
 
 template <int HD> struct Kv4Tile {  // a lane's share of a record
