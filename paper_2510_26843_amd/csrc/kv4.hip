@@ -439,12 +439,13 @@ hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
 // see their slot.
 //
 // What bounds it: for few rows the bytes (one row of 8B heads over 131072
-// slots: 142.6 MB in 27 us, and 4 to join); for many the vector unit, which a step keeps busy
-// for all but a tenth of its time: per tile and query tile 8 exponentials a
-// lane at twice an instruction's cost, 4 conversions of P, and at hd 128 32 of
-// the values' codes and 32 to bring the two d tiles apart, shared by JT (128
-// rows of 8B heads over 16001 slots: 33.7 GFLOP in 39.7 us, 850 TFLOP/s); for short calls the
-// launch, the query's conversion and the two joins.
+// slots: 142.6 MB in 27 us, and 4 to join); for many the vector unit and the
+// matrix cores, which take turns (128 rows of 8B heads over 16001 slots: 33.7
+// GFLOP in 39.7 us, 850 TFLOP/s, 69% and 34% busy): per tile and query tile 8
+// exponentials a lane at twice an instruction's cost, 4 conversions of P, and
+// at hd 128 32 of the values' codes and 32 to bring the two d tiles apart,
+// shared by JT; for short calls the launch, the query's conversion and the two
+// joins.
 
 template <int HD> struct Kv4Tile {  // a lane's share of a record
     uint32_t k[2][HD / 32];
@@ -461,7 +462,8 @@ template <int HD> struct Kv4Records {
     int key, val, ks, vs;
     __device__ __forceinline__ Kv4Records(const uint8_t* head, int tiles, int lane) {
         const int r = lane & 15, g = lane >> 4;
-        rec = __builtin_amdgcn_make_buffer_rsrc((void*)head, 0, tiles * (34 * HD), 0x27000);  // (32-bit data, untyped loads)
+        // (the last word: 32-bit data, which untyped loads ignore but for its being valid)
+        rec = __builtin_amdgcn_make_buffer_rsrc((void*)head, 0, tiles * (34 * HD), 0x27000);
         key = lane * (HD / 8);
         val = 16 * HD + lane * 16;
         ks = 32 * HD + ((HD == 128 ? g : g >> 1) * 16 + r) * 2;
