@@ -327,6 +327,25 @@ def test_same_bits_again_and_on_another_stream():
     assert torch.equal(a, b) and torch.equal(a, c.run())
 
 
+@pytest.mark.parametrize("split", [3, 13, 16, 30])
+def test_two_streams_append_to_the_same_records(split):
+    """No byte belongs to two slots: appends to different slots need no order."""
+    Hkv, hd, n = 8, 128, 64
+    r = _rng(split)
+    k, v = (R.bf16(r.normal(0, 1.28, (n, Hkv, hd))) for _ in "kv")
+    kd, vd = (_dev_bf16(x).reshape(n, -1) for x in (k, v))
+    rec = torch.zeros((Hkv, 2, 34 * hd), dtype=torch.uint8, device=DEV)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    cuts = [0, split, 32 + split, n]
+    torch.cuda.synchronize()
+    for s, a, b in zip(streams, cuts, cuts[1:]):
+        cas.op_kv4_append(kd[a:b], vd[a:b], b - a, Hkv, hd, rec, 64, a, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    got_k, got_v = _read(rec, 64, 0, n, Hkv, hd)
+    assert _same(got_k, R.values(*R.quantise(k.transpose(1, 0, 2))))
+    assert _same(got_v, R.values(*R.quantise(v.transpose(1, 0, 2))))
+
+
 def test_captured_and_replayed():
     """Append and attention in one graph, replayed over changed inputs."""
     c = _Case(8, 2, 64, 4, 4, 131, None)

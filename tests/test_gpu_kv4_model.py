@@ -202,6 +202,23 @@ def test_graphs_and_direct_launches_give_the_same_bits(weights):
     m.close()
 
 
+def test_profiled_and_gemv_calls(weights):
+    """Launches timed one by one give the same bits, and the one-row tiles of
+    cas_set_gemv a result within the bar."""
+    shape = MHA
+    m = _model(shape, weights["mha_small"], _prompt(shape, 200), quant=False)
+    a = m.forward([5], [-1], kv4=True)
+    m.profile(True)
+    b = m.forward([5], [-1], kv4=True)
+    m.profile(False)
+    assert np.array_equal(_bits(a), _bits(b))
+    m.set_gemv(True)
+    assert _row_err(m.forward([5], [-1], kv4=True), a) < TOL
+    m.set_gemv(False)
+    assert np.array_equal(_bits(a), _bits(m.forward([5], [-1], kv4=True)))
+    m.close()
+
+
 def test_the_target_is_untouched(weights):
     """A 4-bit draft is no verify call, and verify calls around it keep their bits."""
     shape = MHA
