@@ -605,9 +605,11 @@ template <int HD> __device__ __forceinline__ Kv4Query<HD> kv4_query_get(const Kv
 // its MFMA run while this one's probabilities and values are converted.
 // MASKED: vm has the visibility of the lane's 8 slots to its row of each query
 // tile; CARE: values of unseen slots may not be finite.
-// The maximum follows the scores only where one passes it by KV4_SLACK (in
+// A row's maximum follows its scores only where one passes it by KV4_SLACK (in
 // log2 units): probabilities are then at most 2^KV4_SLACK, which neither bf16
 // nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
+// maximum scales the probabilities before their rounding, so it takes the
+// row's own scores only: what a row gives does not hang on its neighbours.  The
 // sum of the (rounded) probabilities is one more row of the PV product.
 static constexpr float KV4_SLACK = 8.f;
 template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
@@ -633,7 +635,8 @@ __device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][
         mfma_result_pad();
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
-            const float mn = fmaxf(st[j].m, pair_max32(pair_max16(mt[j])));
+            const float mr = pair_max32(pair_max16(mt[j]));
+            const float mn = mr > st[j].top ? mr : st[j].m;  // (other rows' scores do not move it)
             const float f = __builtin_amdgcn_exp2f((st[j].m - mn) * c);
             st[j].l *= f;
 #pragma unroll
