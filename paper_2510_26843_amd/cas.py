@@ -393,15 +393,21 @@ def _ochk(st: int, what: str) -> None:
         raise CasError(st, what)
 
 
-def _work(nbytes: int):
+def _work(nbytes: int, stream=None):
+    """Scratch of one call, from the memory of the stream that the call runs
+    on: once the call lets go of it, only that stream's later work gets it."""
     import torch
-    return torch.empty(max(int(nbytes), 16), dtype=torch.uint8, device="cuda")
+    n = max(int(nbytes), 16)
+    if stream is None or int(stream) == torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()):
+        return torch.empty(n, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()):
+        return torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
 def op_gemm(wtype: int, W, X, N: int, K: int, T: int, out, ldo: int, epi: int = EPI_STORE,
             xs=None, ws=None, stream=None, work=None) -> None:
     need = int(lib().cas_op_gemm_work_bytes(wtype, N, K, T))
-    work = _work(need) if work is None else work
+    work = _work(need, stream) if work is None else work
     _ochk(lib().cas_op_gemm(wtype, _dp(W), _dp(X), N, K, T, _dp(xs), _dp(ws), epi, _dp(out), ldo, _dp(work),
                             int(work.numel() * work.element_size()), _stream(stream)), "cas_op_gemm")
 
@@ -417,7 +423,7 @@ def op_quant_rows(atype: int, x, T: int, K: int, q, s, stream=None, qmax: int = 
 def op_quant_weight(wtype: int, W, N: int, K: int, q, s, stream=None, qmax: int = 127) -> None:
     """Per-output-channel copy of W; qmax 127 (int8) or 7 (int4, packed by the
     library and returned unpacked)."""
-    work = _work(lib().cas_op_quant_weight_work_bytes(wtype, N, K))
+    work = _work(lib().cas_op_quant_weight_work_bytes(wtype, N, K), stream)
     fn = lib().cas_op_quant_weight if qmax == 127 else lib().cas_op_quant_weight_i4
     _ochk(fn(wtype, _dp(W), N, K, _dp(q), _dp(s), _dp(work), int(work.numel()), _stream(stream)),
           "cas_op_quant_weight" if qmax == 127 else "cas_op_quant_weight_i4")
@@ -426,7 +432,7 @@ def op_quant_weight(wtype: int, W, N: int, K: int, q, s, stream=None, qmax: int 
 def op_attention(q, k, v, ctx_cap: int, Lc: int, n_tree: int, T: int, H: int, Hkv: int, hd: int, anc, out,
                  stream=None) -> None:
     """k, v: [Hkv][ctx_cap][hd] bf16 row-major device tensors."""
-    work = _work(lib().cas_op_attention_work_bytes(Lc, n_tree, T, H, hd, Hkv, ctx_cap))
+    work = _work(lib().cas_op_attention_work_bytes(Lc, n_tree, T, H, hd, Hkv, ctx_cap), stream)
     _ochk(lib().cas_op_attention(_dp(q), _dp(k), _dp(v), ctx_cap, Lc, n_tree, T, H, Hkv, hd, _dp(anc), _dp(out),
                                  _dp(work), int(work.numel()), _stream(stream)), "cas_op_attention")
 
@@ -448,7 +454,7 @@ def op_rmsnorm(atype: int, h, gain, T: int, d: int, eps: float, out=None, q=None
     """RMSNorm of the residual rows h [T][d] (updated in place by pending
     split-K sums when nparts > 0): the normalised rows in the model type
     (qmax 0) or their per-token codes and scales (qmax 127 or 7)."""
-    work = _work(lib().cas_op_rmsnorm_work_bytes(atype, T, d, qmax))
+    work = _work(lib().cas_op_rmsnorm_work_bytes(atype, T, d, qmax), stream)
     _ochk(lib().cas_op_rmsnorm(atype, _dp(h), _dp(gain), T, d, float(eps), _dp(parts), int(nparts), int(qmax),
                                _dp(out), _dp(q), _dp(qs), _dp(work), int(work.numel()), _stream(stream)),
           "cas_op_rmsnorm")
@@ -458,7 +464,7 @@ def op_attn_merge(part_o, part_ml, S: int, T: int, H: int, hd: int, out=None, q=
                   stream=None) -> None:
     """Merge of S attention split partials into bf16 rows (qmax 0) or their
     per-token codes and scales (qmax 127 or 7)."""
-    work = _work(lib().cas_op_attn_merge_work_bytes(T, H, hd, qmax))
+    work = _work(lib().cas_op_attn_merge_work_bytes(T, H, hd, qmax), stream)
     _ochk(lib().cas_op_attn_merge(_dp(part_o), _dp(part_ml), S, T, H, hd, int(qmax), _dp(out), _dp(q), _dp(qs),
                                   _dp(work), int(work.numel()), _stream(stream)), "cas_op_attn_merge")
 
@@ -477,7 +483,7 @@ def op_prefill_block(wtype: int, N: int, K: int, T: int, resid: bool) -> Tuple[i
 def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, stream=None) -> None:
     """Split-K integer projection that quantises its bf16 rows on load; parts
     [splits][T][N] fp32 receives each split's dequantised sums."""
-    work = _work(lib().cas_op_gemm_qx_work_bytes(wtype, N, K, T))
+    work = _work(lib().cas_op_gemm_qx_work_bytes(wtype, N, K, T), stream)
     _ochk(lib().cas_op_gemm_qx(wtype, _dp(W), _dp(ws), _dp(x), N, K, T, int(qmax), _dp(parts), _dp(work),
                                int(work.numel()), _stream(stream)), "cas_op_gemm_qx")
 
@@ -533,7 +539,7 @@ def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int
     L = lib()
     if work is None:
         need = L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)
-        work = _work(need) if need else None
+        work = _work(need, stream) if need else None
     s, (qa, at, aa, oa, ka, va, wa) = _call_at(stream, "cas_op_attention_kv4", q, kv4, anc, out, k, v, work)
     if kv_cap is None:
         kv_cap = 0 if k is None else int(k.shape[1])
