@@ -262,8 +262,8 @@ cas_status cas_tree_info(const int32_t* tree_parent, int32_t n, int32_t* depth, 
  * or launch kernel by kernel (0). */
 cas_status cas_set_graphs(cas_ctx* ctx, int32_t enable);
 
-/* Draft calls of one row (a skip mask, quantised activations or an attention
- * window) with bf16 or int8 weights run their wide GEMMs (QKV, gate/up, LM
+/* Draft calls of one row (a skip mask, quantised activations, an attention
+ * window or 4-bit KV) with bf16 or int8 weights run their wide GEMMs (QKV, gate/up, LM
  * head) as GEMV-style tiles (1: VALU dot products per lane, summed across
  * the k-group lanes) or as the MFMA tiles every other call uses (0,
  * default).  The GEMV tiles stream a little faster (7B 16-layer one-row

@@ -360,13 +360,13 @@ hipError_t enqueue_forward(cas_ctx* c, int T, const uint8_t* skip, int aq) {
     // attention merge, no separate quantiser of the SwiGLU output); the QKV
     // and gate/up inputs keep the codes their RMSNorm writes
     const bool qxs = aq && et == ET_BF16;
-    // drafts of one row (a layer skipped, quantised activations or an
-    // attention window) take the GEMV-style tiles in the wide GEMMs when the
+    // drafts of one row (a layer skipped, quantised activations, an attention
+    // window or 4-bit KV) take the GEMV-style tiles in the wide GEMMs when the
     // caller asks for them (cas_set_gemv); verify calls always keep the MFMA
     // form, whose row sums do not depend on the tree size
     bool skips = false;
     for (int l = 0; skip && l < f.n_layers; ++l) skips = skips || skip[l];
-    const int gv = c->gemv && T == 1 && (skips || aq || c->win_len > 0) ? 1 : 0;
+    const int gv = c->gemv && T == 1 && (skips || aq || c->win_len > 0 || c->kv4_call) ? 1 : 0;
     const int ks_o = gemm_parts_count(wq, d, c->kq_q, T), ks_d = gemm_parts_count(wq, d, c->kq_f, T);
     const bool qx_o = qxs && gemm_qx_ok(wq, d, c->kq_q, T, ks_o);
     const bool qx_d = qxs && gemm_qx_ok(wq, d, c->kq_f, T, ks_d);
