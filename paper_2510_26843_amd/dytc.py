@@ -192,16 +192,22 @@ def pld_propose(seq: Sequence[int], k: int, n_max: int = 3, n_min: int = 1) -> T
 # latency prediction (cost coefficients)
 # ----------------------------------------------------------------------------
 
-def roofline_features(shape, run_layers: int, n_rows: int, ctx: int, act_quant: int = 0) -> np.ndarray:
+def roofline_features(shape, run_layers: int, n_rows: int, ctx: int, act_quant: int = 0,
+                      window: Optional[Tuple[int, int]] = None, kv4: bool = False) -> np.ndarray:
     """Roofline features of one forward: [1, weight GB of the layers that run
     (+ LM head), KV GB read, dense TFLOP, layers run].  The constant and the
     layer count absorb launch and latency floors, the byte terms the HBM
     time, the FLOP term the matrix-core time.  act_quant 1 (W8A8) reads one
-    byte per weight of the run layers, 2 (W4A4) half a byte."""
+    byte per weight of the run layers, 2 (W4A4) half a byte; window (sink,
+    window) bounds the committed slots that are read, kv4 reads whole records
+    of 32 of them at 17/64 of their bytes."""
     es = 2 if shape.dtype == "bf16" else 4
     wb = {0: es, 1: 1, 2: 0.5}[int(act_quant)]
     wbytes = run_layers * shape.layer_params() * wb + shape.vocab * shape.d_model * es
-    kv = run_layers * 2 * shape.n_kv_heads * shape.head_dim * es * (ctx + n_rows)
+    if window and window[1] > 0:
+        ctx = min(ctx, window[0] + window[1])
+    slots = ctx + n_rows - (ctx // 32 * 32 * 47 / 64 if kv4 else 0)
+    kv = run_layers * 2 * shape.n_kv_heads * shape.head_dim * es * slots
     flops = 2.0 * n_rows * (run_layers * shape.layer_params() + shape.vocab * shape.d_model)
     return np.array([1.0, wbytes / 1e9, kv / 1e9, flops / 1e12, float(run_layers)])
 

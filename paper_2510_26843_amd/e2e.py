@@ -28,6 +28,7 @@ that the two decodings produced the same tokens.
 from __future__ import annotations
 
 import argparse
+import dataclasses
 import json
 import sys
 import time
@@ -46,37 +47,39 @@ def calibrate(model, shape, ctx: int, levels: List[dytc.DraftConfig], log) -> Di
     F, y, pts = [], [], []
     model.set_committed(ctx)
 
-    def timed(tokens, parents, skip, aq, reps=6):
+    def timed(tokens, parents, reps=6, **draft):
         for _ in range(2):
-            model.forward(tokens, parents, 0, skip=skip, act_quant=aq, logits=False)
+            model.forward(tokens, parents, 0, logits=False, **draft)
         model.sync()
         t0 = time.perf_counter()
         for _ in range(reps):
-            model.forward(tokens, parents, 0, skip=skip, act_quant=aq, logits=False)
+            model.forward(tokens, parents, 0, logits=False, **draft)
         model.sync()
         return (time.perf_counter() - t0) / reps * 1e3
+
+    def features(c, n):
+        return dytc.roofline_features(shape, len(c.run_layers(L)), n, ctx, c.act_quant, c.window, c.kv4)
 
     for n in (1, 4, 16, 32, 64):
         par = synth.balanced_tree(n)
         toks = synth.gen_tree_tokens(par, shape.vocab, seed=n)
-        ms = timed(toks, par, None, False)
+        ms = timed(toks, par)
         F.append(dytc.roofline_features(shape, L, n, ctx))
         y.append(ms)
         pts.append(("verify", n, ms))
     for c in levels:
-        run = len(c.run_layers(L))
+        draft = dict(skip=list(c.skip) if c.skip else None, act_quant=c.act_quant, attn_window=c.window, kv4=c.kv4)
         for n in (1, 2, 4, 8):
             par = synth.balanced_tree(n)
             toks = synth.gen_tree_tokens(par, shape.vocab, seed=n)
-            ms = timed(toks, par, list(c.skip), c.act_quant)
-            F.append(dytc.roofline_features(shape, run, n, ctx, c.act_quant))
+            ms = timed(toks, par, **draft)
+            F.append(features(c, n))
             y.append(ms)
             pts.append((c.name, n, ms))
     model.set_committed(0)
     lm = dytc.LatencyModel(prior_precision=1e-3, noise_precision=1e2).fit(np.array(F), np.array(y))
     base = lm.predict(dytc.roofline_features(shape, L, 1, ctx))[0]
-    cost = {c.name: lm.predict(dytc.roofline_features(shape, len(c.run_layers(L)), 1, ctx, c.act_quant))[0] / base
-            for c in levels}
+    cost = {c.name: lm.predict(features(c, 1))[0] / base for c in levels}
     resid = float(np.sqrt(np.mean((np.array(F) @ lm.mean - np.array(y)) ** 2)))
     log(f"[e2e] latency model: rms residual {resid:.3f} ms over {len(y)} points; c-hat {cost}")
     return {"cost": cost, "points": pts, "rms_residual_ms": resid, "target_ms": base}
@@ -138,6 +141,7 @@ def main(argv=None) -> None:
                     help="scale the odd layers' W_o and W_down by this factor (unset: unchanged)")
     ap.add_argument("--gemv", type=int, choices=(0, 1), default=None,
                     help="GEMV-style tiles for one-row drafts (default: the library's)")
+    ap.add_argument("--kv4", action="store_true", help="the draft levels read the 4-bit copy of the KV cache")
     ap.add_argument("--out", default="")
     args = ap.parse_args(argv)
     log = lambda *a: print(*a, file=sys.stderr, flush=True)
@@ -156,6 +160,8 @@ def main(argv=None) -> None:
     m.load_weights(w)
     m.build_int8()
     m.build_int4()
+    if args.kv4:
+        m.build_kv4()
     if args.gemv is not None:
         m.set_gemv(bool(args.gemv))
     del w
@@ -166,6 +172,8 @@ def main(argv=None) -> None:
     odd = tuple(skip_mask(L, "odd"))
     levels = [dytc.DraftConfig("skip25", q3), dytc.DraftConfig("skip50", odd),
               dytc.DraftConfig("skip50_int8", odd, 1), dytc.DraftConfig("skip50_int4", odd, 2)]
+    if args.kv4:
+        levels = [dataclasses.replace(c, kv4=True) for c in levels]
     pld = dytc.DraftConfig("pld", pld=True)
     m.prefill(prompt[:-1])
     cal = calibrate(m, shape, len(prompt) - 1, levels, log)
@@ -211,7 +219,7 @@ def main(argv=None) -> None:
         "expansions": stats.get("expansions", {}), "alpha_final": {k: round(v, 4) for k, v in est.a.items()},
         "c_hat": {k: round(v, 4) for k, v in cost.items()}, "latency_model_rms_ms": round(cal["rms_residual_ms"], 4),
         "params": vars(params),
-        "damp_odd": args.damp_odd, "gemv": args.gemv, "prior": prior, "ties": ties,
+        "damp_odd": args.damp_odd, "gemv": args.gemv, "kv4": args.kv4, "prior": prior, "ties": ties,
         "data": ("synthetic: random N(0,0.02^2) bf16 weights" +
                  (f", odd layers' W_o and W_down scaled by {args.damp_odd}" if args.damp_odd is not None else "") +
                  ", uniform-random prompt"),
