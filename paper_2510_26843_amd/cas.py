@@ -490,20 +490,86 @@ def op_gemm_qx(wtype: int, W, ws, x, N: int, K: int, T: int, qmax: int, parts, s
 
 # the 4-bit KV cache (device byte tensors of kv4_bytes(...) bytes)
 
-def _call_at(stream, what: str, *tensors):
-    """The stream of a call and the addresses of its tensors (None: none),
-    which have to be on the current device."""
-    import torch
+class _KV4:
+    """Element types of the calls' tensors, in the order of _call_at."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        # (bf16 values or their bits)
+        self.b16 = b16 = (torch.bfloat16, torch.int16, torch.uint16)
+        u8, i64, i32, f32 = (torch.uint8,), (torch.int64, torch.uint64), (torch.int32,), (torch.float32,)
+        self.append = (b16, b16, u8, i32, f32, f32)
+        self.read = (u8, b16, b16)
+        self.attend = (b16, u8, i64, b16, b16, b16, u8)
+
+
+_kv4_types = None
+
+
+def _kv4() -> _KV4:
+    global _kv4_types
+    if _kv4_types is None:
+        _kv4_types = _KV4()
+    return _kv4_types
+
+
+def _refuse(what: str, why: str):
+    raise CasError(ERR_ARG, f"{what}: {why}")
+
+
+def _call_at(torch, stream, what: str, names: str, tensors, types, sizes):
+    """The stream of a call and the addresses of its tensors, which have to be
+    on the current device and to be that many bytes of one of the types, one
+    after another (0 bytes: seen to by the caller).  A tensor that is None is
+    the library's to refuse."""
     dev = torch.cuda.current_device()
     at = []
-    for t in tensors:
+    for t, ty, n in zip(tensors, types, sizes):
         if t is None:
             at.append(None)
-        elif t.get_device() == dev:
-            at.append(t.data_ptr())
+        elif t.get_device() != dev:
+            _refuse(what, "the tensors are not on the current device")
+        elif n > 0 and not (t.nbytes >= n and t.dtype in ty and t.is_contiguous()):
+            _refuse(what, f"{names.split()[len(at)]} needs {n} contiguous bytes of {ty[0]}")
         else:
-            raise CasError(ERR_ARG, what + ": the tensors are not on the current device")
+            at.append(t.data_ptr())
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream), at
+
+
+def _row_stride(what: str, name: str, x, T: int, width: int, ld: Optional[int], types) -> int:
+    """Elements from one to the next of T rows of `width` in x: ld, or those of
+    x's own layout.  The rows have to lie within x."""
+    if x is None:
+        return width if ld is None else ld
+    n, st = x.shape, x.stride()
+    if x.dtype in types:
+        # rows (of heads) of a wider matrix
+        if (n and st[-1] == 1 and n[0] >= T and (ld is None or ld == st[0]) and
+                (len(n) == 2 and n[1] >= width or len(n) == 3 and st[1] == n[2] and n[1] * n[2] >= width)):
+            return st[0]
+        if x.is_contiguous() and x.numel() >= (T - 1) * (width if ld is None else ld) + width:
+            return width if ld is None else ld
+    _refuse(what, f"{name} does not hold {T} rows of {width} contiguous elements of {types[0]}, ldk or ldv apart")
+
+
+def _head_rows(what: str, name: str, x, Hkv: int, hd: int, rows: int, cap: Optional[int], types) -> int:
+    """Rows from one head to the next in x, of [Hkv][rows or more][hd] elements:
+    cap, or those of x's own layout (a slice of a longer cache has its rows)."""
+    if x is None:
+        return 0 if cap is None else cap
+    n = x.shape
+    if x.dtype in types:
+        packed = x.is_contiguous()
+        if len(n) == 3 and n[0] >= Hkv and n[1] >= rows and n[2] == hd:
+            if packed and (cap is None or cap == n[1] or Hkv == 1):
+                return n[1] if cap is None else cap
+            st = x.stride()
+            if st[2] == 1 and st[1] == hd and (st[0] == cap * hd if cap is not None else st[0] % hd == 0):
+                return st[0] // hd
+        elif len(n) != 3 and packed and cap is not None and x.numel() >= ((Hkv - 1) * cap + rows) * hd:
+            return cap
+    _refuse(what, f"{name} does not hold {rows} rows of {hd} elements of {types[0]} of each of {Hkv} heads, kv_cap apart")
 
 
 def kv4_bytes(Hkv: int, hd: int, ctx_cap: int) -> int:
@@ -514,34 +580,54 @@ def kv4_bytes(Hkv: int, hd: int, ctx_cap: int) -> int:
 def op_kv4_append(k, v, T: int, Hkv: int, hd: int, kv4, ctx_cap: int, slot0: int, pos=None, cos=None, sin=None,
                   ldk: Optional[int] = None, ldv: Optional[int] = None, stream=None) -> None:
     """Quantise T rows of keys and values (bf16, Hkv * hd elements, ldk and
-    ldv elements apart) into slots slot0 .. slot0 + T - 1.  With cos and sin
-    ([positions][hd/2] fp32) the keys are rotated by pos ([T] int32; None:
-    their slots) first."""
-    s, (ka, va, at, pa, ca, sa) = _call_at(stream, "cas_op_kv4_append", k, v, kv4, pos, cos, sin)
-    ld = Hkv * hd
-    _ochk(lib().cas_op_kv4_append(ka, va, ld if ldk is None else ldk, ld if ldv is None else ldv, T, slot0, pa, ca, sa,
-                                  0 if cos is None else int(cos.shape[0]), Hkv, hd, at, ctx_cap, s),
-          "cas_op_kv4_append")
+    ldv elements apart; by default packed, or as the view's rows lie) into
+    slots slot0 .. slot0 + T - 1.  With cos and sin ([positions][hd/2] fp32)
+    the keys are rotated by pos ([T] int32; None: their slots) first."""
+    what, kv = "cas_op_kv4_append", _kv4_types or _kv4()
+    w, n_pos, packed = Hkv * hd, 0, 0
+    if ldk == w and ldv == w:
+        packed = 2 * T * w
+    else:
+        ldk = _row_stride(what, "k", k, T, w, ldk, kv.b16)
+        ldv = _row_stride(what, "v", v, T, w, ldv, kv.b16)
+    if cos is not None:
+        shape = cos.shape
+        if len(shape) != 2 or 2 * shape[1] != hd:
+            _refuse(what, "cos is not [positions][hd / 2]")
+        n_pos = shape[0]
+    angles = 2 * n_pos * hd
+    s, (ka, va, at, pa, ca, sa) = _call_at(
+        kv.torch, stream, what, "k v kv4 pos cos sin", (k, v, kv4, pos, cos, sin), kv.append,
+        (packed, packed, w * (ctx_cap // 32) * 34, 4 * T if n_pos else 0, angles, angles))
+    _ochk(lib().cas_op_kv4_append(ka, va, ldk, ldv, T, slot0, pa, ca, sa, n_pos, Hkv, hd, at, ctx_cap, s), what)
 
 
 def op_kv4_read(kv4, ctx_cap: int, slot0: int, n: int, Hkv: int, hd: int, k, v, stream=None) -> None:
     """The values of slots slot0 .. slot0 + n - 1 into k, v [Hkv][n][hd] bf16."""
-    s, (at, ka, va) = _call_at(stream, "cas_op_kv4_read", kv4, k, v)
-    _ochk(lib().cas_op_kv4_read(at, ctx_cap, slot0, n, Hkv, hd, ka, va, s), "cas_op_kv4_read")
+    what, kv = "cas_op_kv4_read", _kv4_types or _kv4()
+    rows = 2 * Hkv * n * hd
+    s, (at, ka, va) = _call_at(kv.torch, stream, what, "kv4 k v", (kv4, k, v), kv.read,
+                               (Hkv * (ctx_cap // 32) * 34 * hd, rows, rows))
+    _ochk(lib().cas_op_kv4_read(at, ctx_cap, slot0, n, Hkv, hd, ka, va, s), what)
 
 
 def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int, H: int, Hkv: int, hd: int, anc, out,
                      k=None, v=None, kv_cap: Optional[int] = None, sink: int = 0, window: int = 0, stream=None,
                      work=None) -> None:
     """Tree attention with slots [0, n4) from the 4-bit cache and the others
-    from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap: k's second
-    dimension by default)."""
-    L = lib()
+    from k, v [Hkv][kv_cap][hd] bf16 (row 0: slot n4; kv_cap by default as k
+    lies: its second dimension, or that of the cache that it is a slice of)."""
+    what, kv, L = "cas_op_attention_kv4", _kv4_types or _kv4(), lib()
+    rest = Lc + n_tree - n4
+    if rest > 0:
+        kv_cap = _head_rows(what, "k", k, Hkv, hd, rest, kv_cap, kv.b16)
+        _head_rows(what, "v", v, Hkv, hd, rest, kv_cap, kv.b16)
     if work is None:
         need = L.cas_op_attention_kv4_work_bytes(Lc, n_tree, T, H, Hkv, hd, sink, window)
         work = _work(need, stream) if need else None
-    s, (qa, at, aa, oa, ka, va, wa) = _call_at(stream, "cas_op_attention_kv4", q, kv4, anc, out, k, v, work)
-    if kv_cap is None:
-        kv_cap = 0 if k is None else int(k.shape[1])
-    _ochk(L.cas_op_attention_kv4(qa, at, ctx_cap, n4, ka, va, kv_cap, Lc, n_tree, T, H, Hkv, hd, sink, window, aa, oa,
-                                 wa, 0 if work is None else work.nbytes, s), "cas_op_attention_kv4")
+    rows = 2 * T * H * hd
+    s, (qa, at, aa, oa, ka, va, wa) = _call_at(
+        kv.torch, stream, what, "q kv4 anc out k v work", (q, kv4, anc, out, k, v, work), kv.attend,
+        (rows, Hkv * (ctx_cap // 32) * 34 * hd if n4 > 0 else 0, 16 * T, rows, 0, 0, 0))
+    _ochk(L.cas_op_attention_kv4(qa, at, ctx_cap, n4, ka, va, kv_cap or 0, Lc, n_tree, T, H, Hkv, hd, sink, window, aa,
+                                 oa, wa, 0 if work is None else work.nbytes, s), what)

@@ -99,3 +99,22 @@ def test_a_row_does_not_depend_on_the_queries_beside_it(H, Hkv, hd, T, Lc):
         got = other.run()
         assert torch.equal(got[0::2], want[0::2]), (scale, int((got[0::2] != want[0::2]).sum()))
         assert not torch.equal(got[1::2], want[1::2])
+
+
+def test_views_of_wider_rows_and_longer_caches():
+    """Tensors passed as views give the bits of their packed copies: rows of a
+    fused product without ldk and ldv, the last slots of a bf16 cache without
+    kv_cap."""
+    c = _Call(8, 2, 64, 5, 200, tail=True)
+    want = c.run()
+    c.check(want)
+    long = torch.full((2, 2, 300, 64), float("nan"), dtype=torch.bfloat16, device=DEV)
+    long[0, :, c.n4 : c.n4 + 13], long[1, :, c.n4 : c.n4 + 13] = c.kr, c.vr
+    c.kr, c.vr = long[0, :, c.n4 : c.n4 + 13], long[1, :, c.n4 : c.n4 + 13]
+    assert torch.equal(c.run(), want)
+    rows = torch.randn((7, 3 * 128), device=DEV).to(torch.bfloat16)
+    k, v = rows[:, 128:256], rows[:, 256:]
+    recs = [torch.zeros((2, 1, 34 * 64), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    cas.op_kv4_append(k, v, 7, 2, 64, recs[0], 32, 5)
+    cas.op_kv4_append(k.contiguous(), v.contiguous(), 7, 2, 64, recs[1], 32, 5)
+    assert torch.equal(*recs) and bool(recs[0].any())

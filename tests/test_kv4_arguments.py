@@ -1,0 +1,137 @@
+"""What the tensor calls of the 4-bit KV cache make of their tensors' types,
+sizes and strides, before anything is launched.  CPU: the library notes the
+arguments that reach it, host tensors stand in for the device's."""
+import pytest
+import torch
+
+from paper_2510_26843_amd import cas
+
+B, F, U, I, A = torch.bfloat16, torch.float32, torch.uint8, torch.int32, torch.int64
+HKV, HD, CAP, T, H = 2, 64, 64, 3, 4
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    seen = []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name.endswith("_work_bytes"):
+                return lambda *a: 0
+            return lambda *a: seen.append(a) or 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)  # (what a host tensor's get_device says)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    monkeypatch.setattr(cas, "lib", lambda debug=False: Lib())
+    return seen
+
+
+def _z(*shape, dtype=B):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def _rec(heads=HKV):
+    return _z(heads, CAP // 32, 34 * HD, dtype=U)
+
+
+def _append(**kw):
+    a = dict(k=_z(T, HKV * HD), v=_z(T, HKV * HD), kv4=_rec(), T=T, pos=_z(T, dtype=I), cos=_z(50, HD // 2, dtype=F),
+             sin=_z(50, HD // 2, dtype=F))
+    a.update(kw)
+    cas.op_kv4_append(a.pop("k"), a.pop("v"), a.pop("T"), HKV, HD, a.pop("kv4"), CAP, 0, **a)
+
+
+WIDE = 3 * HKV * HD
+
+
+@pytest.mark.parametrize("change,ld", [
+    ({}, HKV * HD), (dict(ldk=HKV * HD, ldv=HKV * HD), HKV * HD), (dict(k=_z(T, HKV, HD)), HKV * HD),
+    (dict(k=_z(T * HKV * HD)), HKV * HD), (dict(k=_z(T * HKV, HD)), HKV * HD), (dict(k=_z(T, WIDE)[:, HD : HD * 3]), WIDE),
+    (dict(k=_z(T, WIDE)[:, HD : HD * 3], ldk=WIDE), WIDE), (dict(k=_z(T, 6, HD)[:, 2:4]), WIDE),
+    (dict(k=_z(T * WIDE), ldk=WIDE), WIDE), (dict(k=_z(T * WIDE - 100)[HD:], ldk=WIDE), WIDE),
+    (dict(k=_z(T + 2, HKV * HD)), HKV * HD), (dict(k=_z(T, HKV * HD, dtype=torch.int16)), HKV * HD),
+    (dict(pos=None), HKV * HD), (dict(pos=None, cos=None, sin=None), HKV * HD)])
+def test_append_takes(calls, change, ld):
+    _append(**change)
+    assert len(calls) == 1 and calls[0][2] == ld and calls[0][3] == HKV * HD
+
+
+@pytest.mark.parametrize("change,name", [
+    (dict(k=_z(T, HKV * HD, dtype=F)), "k"), (dict(v=_z(T, HKV * HD, dtype=torch.float16)), "v"),
+    (dict(k=_z(T - 1, HKV * HD)), "k"), (dict(k=_z(T, WIDE)[:, :HD]), "k"), (dict(k=_z(T, WIDE)[:, :128], ldk=WIDE + 8), "k"),
+    (dict(k=_z(HKV * HD, T).t()), "k"), (dict(v=_z(T, 2 * HKV * HD)[:, ::2]), "v"), (dict(v=_z(T * WIDE - 300), ldv=WIDE), "v"),
+    (dict(v=_z(T - 1, WIDE)[:, :128], ldv=WIDE), "v"), (dict(kv4=_rec(1)), "kv4"), (dict(kv4=_rec()[:, :1]), "kv4"),
+    (dict(kv4=_rec().view(torch.int8)), "kv4"), (dict(kv4=_rec()[..., ::2]), "kv4"), (dict(pos=_z(T, dtype=A)), "pos"),
+    (dict(pos=_z(T - 1, dtype=I)), "pos"), (dict(pos=_z(2 * T, dtype=I)[::2]), "pos"), (dict(cos=_z(50, HD, dtype=F)), "cos"),
+    (dict(cos=_z(50 * HD // 2, dtype=F)), "cos"), (dict(sin=_z(49, HD // 2, dtype=F)), "sin"),
+    (dict(sin=_z(50, HD // 2, dtype=torch.float64)), "sin"), (dict(cos=_z(50, HD // 2)), "cos"),
+    (dict(cos=_z(50, HD, dtype=F)[:, ::2]), "cos")])
+def test_append_refuses(calls, change, name):
+    for packed in ([{}, dict(ldk=HKV * HD, ldv=HKV * HD)] if not {"ldk", "ldv"} & set(change) else [{}]):
+        with pytest.raises(cas.CasError, match=rf"CAS_ERR_ARG.*: {name} "):
+            _append(**packed, **change)
+    assert not calls
+
+
+def _read(**kw):
+    a = dict(kv4=_rec(), k=_z(HKV, 5, HD), v=_z(HKV, 5, HD))
+    a.update(kw)
+    cas.op_kv4_read(a["kv4"], CAP, 3, 5, HKV, HD, a["k"], a["v"])
+
+
+def test_read_takes(calls):
+    _read()
+    _read(k=_z(HKV * 5 * HD + 7), v=_z(5, HKV, HD, dtype=torch.int16))
+    assert len(calls) == 2
+
+
+@pytest.mark.parametrize("change,name", [
+    (dict(kv4=_rec(1)), "kv4"), (dict(k=_z(HKV, 4, HD)), "k"), (dict(v=_z(HKV, 5, HD, dtype=F)), "v"),
+    (dict(v=_z(HKV, 6, HD)[:, :5]), "v"), (dict(k=_z(5, HKV, HD).transpose(0, 1)), "k")])
+def test_read_refuses(calls, change, name):
+    with pytest.raises(cas.CasError, match=rf"CAS_ERR_ARG.*: {name} "):
+        _read(**change)
+    assert not calls
+
+
+def _attend(n4=32, **kw):  # 40 committed slots and 5 nodes: 13 of them in bf16
+    a = dict(q=_z(T, H, HD), kv4=_rec(), anc=_z(T, 2, dtype=A), out=_z(T, H * HD), k=_z(HKV, 13, HD), v=_z(HKV, 13, HD))
+    a.update(kw)
+    cas.op_attention_kv4(a.pop("q"), a.pop("kv4"), CAP, n4, 40, 5, T, H, HKV, HD, a.pop("anc"), a.pop("out"), **a)
+
+
+CACHE = _z(HKV, 100, HD)  # 45 slots and more: k, v are its rows from slot 32 on
+
+
+@pytest.mark.parametrize("change,cap", [
+    ({}, 13), (dict(k=_z(HKV, 20, HD), v=_z(HKV, 20, HD)), 20), (dict(k=CACHE[:, 32:45], v=CACHE[:, 32:45]), 100),
+    (dict(k=CACHE[:, 32:], v=CACHE[:, 32:45], kv_cap=100), 100), (dict(k=_z(HKV * 13 * HD), v=_z(HKV * 13, HD), kv_cap=13), 13),
+    (dict(n4=45, k=None, v=None), 0), (dict(n4=0, kv4=None, k=_z(HKV, 45, HD), v=_z(HKV, 45, HD)), 45),
+    (dict(q=_z(T, H * HD, dtype=torch.int16), anc=_z(2 * T, dtype=A)), 13)])
+def test_attention_takes(calls, change, cap):
+    _attend(**change)
+    assert len(calls) == 1 and calls[0][6] == cap
+
+
+@pytest.mark.parametrize("change,name", [
+    (dict(q=_z(T, H, HD, dtype=F)), "q"), (dict(q=_z(T - 1, H, HD)), "q"), (dict(q=_z(H, T, HD).transpose(0, 1)), "q"),
+    (dict(out=_z(T, H * HD, dtype=F)), "out"), (dict(out=_z(T, HD)), "out"), (dict(out=_z(T, 2 * H * HD)[:, : H * HD]), "out"),
+    (dict(anc=_z(T, 2, dtype=I)), "anc"), (dict(anc=_z(T, dtype=A)), "anc"), (dict(anc=_z(T, 4, dtype=A)[:, :2]), "anc"),
+    (dict(kv4=_rec(1)), "kv4"), (dict(kv4=_rec()[:, :1]), "kv4"), (dict(k=_z(HKV, 12, HD)), "k"),
+    (dict(v=_z(HKV, 12, HD)), "v"), (dict(v=_z(HKV, 14, HD)), "v"), (dict(k=_z(1, 13, HD)), "k"),
+    (dict(k=_z(HKV, 13, HD, dtype=F)), "k"), (dict(k=_z(13, HKV, HD).transpose(0, 1)), "k"),
+    (dict(k=CACHE[:, 32:45]), "v"), (dict(k=_z(HKV, 13, HD), v=CACHE[:, 32:45]), "v"),
+    (dict(k=CACHE[:, 32:44], v=CACHE[:, 32:44]), "k"), (dict(k=_z(HKV, 20, HD), v=_z(HKV, 20, HD), kv_cap=13), "k"),
+    (dict(k=_z(HKV, 13, HD), kv_cap=20), "k"), (dict(k=_z(HKV * 13 * HD)), "k"), (dict(k=_z(HKV * 13 * HD - 1), kv_cap=13), "k")])
+def test_attention_refuses(calls, change, name):
+    with pytest.raises(cas.CasError, match=rf"CAS_ERR_ARG.*: {name} "):
+        _attend(**change)
+    assert not calls
+
+
+def test_another_device(calls, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in (_append, _read, _attend):
+        with pytest.raises(cas.CasError, match="not on the current device"):
+            call()
+    assert not calls
