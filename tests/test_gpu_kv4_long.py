@@ -118,3 +118,26 @@ def test_views_of_wider_rows_and_longer_caches():
     cas.op_kv4_append(k, v, 7, 2, 64, recs[0], 32, 5)
     cas.op_kv4_append(k.contiguous(), v.contiguous(), 7, 2, 64, recs[1], 32, 5)
     assert torch.equal(*recs) and bool(recs[0].any())
+
+
+# (splits: the runs of key tiles that the plan gives each, which work_bytes
+# tells; the first two and the last are 128 or 256 tiles of query rows, whose
+# splits fill the card's 256 places with two tiles per workgroup)
+@pytest.mark.parametrize("H,Hkv,hd,T,Lc,sink,window,splits", [
+    (16, 4, 128, 128, 7000, 0, 0, 4), (32, 8, 128, 128, 16001, 0, 0, 2),
+    (8, 8, 128, 128, 8190, 0, 0, 4), (8, 8, 128, 64, 8190, 0, 0, 7), (4, 2, 64, 128, 8190, 0, 0, 7),
+    (32, 32, 128, 32, 8190, 0, 0, 4), (8, 2, 64, 20, 6000, 0, 0, 12), (4, 4, 128, 1, 8190, 0, 0, 32),
+    (8, 2, 64, 3, 9000, 40, 3000, 16), (4, 4, 128, 20, 9000, 40, 3000, 16), (8, 2, 64, 1, 9000, 4, 5000, 20),
+    (16, 4, 128, 128, 9000, 100, 7000, 4)])
+@pytest.mark.parametrize("tail", [False, True], ids=["4-bit", "bf16 tail"])
+def test_splits(H, Hkv, hd, T, Lc, tail, sink, window, splits):
+    c = _Call(H, Hkv, hd, T, Lc, tail, sink, window)
+    assert c.splits() == splits
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("H,Hkv,hd", [(8, 2, 64), (4, 4, 128)])
+@pytest.mark.parametrize("T,Lc", [(1, 0), (1, 30), (1, 31), (9, 11), (32, 0)])
+def test_a_cache_of_one_record(H, Hkv, hd, T, Lc):
+    c = _Call(H, Hkv, hd, T, Lc, cap=32)
+    c.check(c.run())
