@@ -254,8 +254,9 @@ cas_status cas_op_kv4_read(const void* kv4, int32_t ctx_cap, int32_t slot0, int3
  * A row that sees no slot gives zeros; one that sees a key that is not finite
  * gives NaN, and one that sees such a value NaN at its element.
  * Probabilities are rounded to bf16 for the product with the values (each by
- * at most 2^-8 of itself).  The result does not depend on earlier calls or on
- * timing; it may depend in the last bits on T.
+ * at most 2^-8 of itself; cas_op_attention, over slots read back, by 2^-16).
+ * The result does not depend on earlier calls or on timing; it may depend in
+ * the last bits on T.
  * 1 <= T <= 128, 1 <= n_tree <= 128, 0 <= Lc, Lc + n_tree <= 1048576, n4 <=
  * ctx_cap (the bf16 rows need no record), n_heads <= 4096.
  * work: device scratch of cas_op_attention_kv4_work_bytes(...) bytes (0: none

@@ -427,7 +427,12 @@ hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
 // k-order of P in the PV product (on bf16 MFMA, its values converted in
 // registers), so probabilities stay in registers.  They enter that product as
 // bf16, each off by at most 2^-8 of itself; their sum, which is of the rounded
-// ones, and the output stay in fp32.
+// ones, and the output stay in fp32.  The output's error is 0.0023 of its norm
+// (0.0017 is its own rounding), the cache's quantisation 0.1.  With the rest of
+// each as a second bf16 term, as in k_attn_bf16, it is 0.0017, and 128 rows of
+// 8B heads over 16001 slots take 48.3 us for 38.5, 64 rows of 13B heads over
+// 2048 10.8 for 9.6, one row over 131071 31.8 for 31.1.  One fp16 term (2^-11)
+// ends at 2^-31 of a row's largest, and the sums over the others would miss it.
 //
 // Whole tiles, which every row sees, are a wave's main loop: a ring of three
 // tiles' codes in registers, loaded two steps ahead, the next tile's scores
