@@ -545,7 +545,7 @@ def _row_stride(what: str, name: str, x, T: int, width: int, ld: Optional[int], 
     n, st = x.shape, x.stride()
     if x.dtype in types:
         # rows (of heads) of a wider matrix
-        if (n and st[-1] == 1 and n[0] >= T and (ld is None or ld == st[0]) and
+        if (n and st[-1] == 1 and n[0] >= T and (ld == st[0] or ld is None and st[0] >= width) and
                 (len(n) == 2 and n[1] >= width or len(n) == 3 and st[1] == n[2] and n[1] * n[2] >= width)):
             return st[0]
         if x.is_contiguous() and x.numel() >= (T - 1) * (width if ld is None else ld) + width:

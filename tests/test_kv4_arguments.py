@@ -56,6 +56,15 @@ def test_append_takes(calls, change, ld):
     assert len(calls) == 1 and calls[0][2] == ld and calls[0][3] == HKV * HD
 
 
+def test_append_takes_one_row_whatever_its_stride(calls):
+    """(A dimension of one element may have any stride.)"""
+    column = _z(HKV * HD, 1).t()
+    assert column.stride(0) == 1
+    for x in (column, _z(1, HKV * HD).expand(1, -1), _z(1, WIDE)[:, : HKV * HD], _z(1, 1, HKV, HD)[0]):
+        _append(k=x, v=x, T=1, pos=None)
+    assert all(c[2] >= HKV * HD and c[3] >= HKV * HD for c in calls) and len(calls) == 4
+
+
 @pytest.mark.parametrize("change,name", [
     (dict(k=_z(T, HKV * HD, dtype=F)), "k"), (dict(v=_z(T, HKV * HD, dtype=torch.float16)), "v"),
     (dict(k=_z(T - 1, HKV * HD)), "k"), (dict(k=_z(T, WIDE)[:, :HD]), "k"), (dict(k=_z(T, WIDE)[:, :128], ldk=WIDE + 8), "k"),
