@@ -1,0 +1,146 @@
+// The tile step that the attention over the 4-bit cache (kv4.hip) and the one
+// over a paged cache (paged.hip) share: a wave's running softmax state, and one
+// key tile's part of it.
+#pragma once
+#include "kernel_common.h"
+
+namespace cas {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// A launch that reports its own error, not an earlier call's (and without the
+// call-configuration calls of the <<<>>> form: 2.35 us of the host for 2.55).
+template <typename... P>
+static hipError_t launch_checked(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, P... args) {
+    void* at[] = {(void*)&args...};
+    return hipLaunchKernel((const void*)kernel, grid, dim3(threads), at, 0, s);
+}
+
+__device__ __forceinline__ uint32_t pack_bf(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// Running softmax state of a wave for a query tile: per lane its row's
+// reference score m (before scaling), the score that moves it, the sum l (the
+// same in all four elements) and O.
+template <int HD> struct AttnState {
+    float m, top;
+    f32x4 l, O[HD / 16];
+    __device__ __forceinline__ void clear() {
+        m = top = -1e30f;
+        l = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < HD / 16; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+};
+
+// Values of a pair of d tiles that are not finite, as 1.0 where they are and 0
+// elsewhere; the values themselves become 0.
+__device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
+    i32x4 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = (uint32_t)v[i];
+        const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+        f[i] = (int)(0x3f803f80u & (lo | hi));
+        v[i] = (int)(w & ~(lo | hi));
+    }
+    return f;
+}
+
+// One key tile: S are the scores of its 32 slots, V(m, f) gives the value
+// fragments of d tiles 2m and 2m + 1.  next() computes the next tile's scores:
+// its MFMA run while this one's probabilities and values are converted.
+// MASKED: vm has the visibility of the lane's 8 slots to its row of each query
+// tile; CARE: values of unseen slots may not be finite.
+// A row's maximum follows its scores only where one passes it by ATTN_SLACK (in
+// log2 units): probabilities are then at most 2^ATTN_SLACK, which neither bf16
+// nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
+// maximum scales the probabilities before their rounding, so it takes the
+// row's own scores only: what a row gives does not hang on its neighbours.  The
+// sum of the (rounded) probabilities is one more row of the PV product.
+static constexpr float ATTN_SLACK = 8.f;
+template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
+__device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
+                                         const uint32_t (&vm)[JT], NF next) {
+    constexpr int NDT = HD / 16;
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) S[j][e >> 2][e & 3] = (vm[j] >> e) & 1u ? S[j][e >> 2][e & 3] : -INFINITY;
+    }
+    float mt[JT];
+    bool grow = false;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        mt[j] = S[j][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mt[j] = fmaxf(mt[j], S[j][e >> 2][e & 3]);
+        grow = grow || mt[j] > st[j].top;
+    }
+    if (__any(grow)) {
+        mfma_result_pad();
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+            const float mr = pair_max32(pair_max16(mt[j]));
+            const float mn = mr > st[j].top ? mr : st[j].m;  // (other rows' scores do not move it)
+            const float f = __builtin_amdgcn_exp2f((st[j].m - mn) * c);
+            st[j].l *= f;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) st[j].O[dt] *= f;
+            st[j].m = mn;
+            st[j].top = mn + ATTN_SLACK / c;
+        }
+    }
+    next();
+    i32x4 P[JT];
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        const float mc = st[j].m * c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1)], c, -mc));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1) + 1], c, -mc));
+            P[j][i] = (int)pack_bf(p0, p1);
+        }
+        const int one = 0x3f803f80;
+        st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+    }
+#pragma unroll
+    for (int m = 0; m < NDT / 2; ++m) {
+        i32x4 Vf[2];
+        V(m, Vf);
+        if constexpr (CARE) {
+            i32x4 bad[2] = {take_nonfinite(Vf[0]), take_nonfinite(Vf[1])};
+            int any = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) any |= bad[0][i] | bad[1][i];
+            if (__any(any)) {  // rows that see a bad value's slot: NaN
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    i32x4 seen;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        seen[i] = (int)(((vm[j] >> (2 * i)) & 1u ? 0x3f80u : 0u) |
+                                        ((vm[j] >> (2 * i + 1)) & 1u ? 0x3f800000u : 0u));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f32x4 n = mfma_step<ET_BF16>(bad[h], seen, f32x4{0.f, 0.f, 0.f, 0.f});
+                        mfma_result_pad();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (n[i] > 0.f) st[j].O[2 * m + h][i] = NAN;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < JT; ++j) st[j].O[2 * m + h] = mfma_step<ET_BF16>(Vf[h], P[j], st[j].O[2 * m + h]);
+    }
+}
+
+}  // namespace cas

@@ -21,15 +21,13 @@
 //   block r/w (w = 512 / hd) with d % w = r % w: one scale per slot and lane,
 //   and the two d of a byte are w apart, so one conversion (two codes and a
 //   scale to two bf16, one instruction) serves two of the PV product's d tiles.
-#include "kernel_common.h"
+#include "attn_step.h"
 
 namespace cas {
 
 typedef unsigned short uint16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------- the form
 
@@ -48,9 +46,6 @@ template <int B> __device__ __forceinline__ uint32_t kv4_pair(uint32_t w, float 
 __device__ __forceinline__ i32x4 kv4_values8(uint32_t w, float scale) {
     return i32x4{(int)kv4_pair<0>(w, scale), (int)kv4_pair<1>(w, scale), (int)kv4_pair<2>(w, scale),
                  (int)kv4_pair<3>(w, scale)};
-}
-__device__ __forceinline__ uint32_t pack_bf(float a, float b) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 // Low / high halves of two dwords side by side.
 __device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
@@ -126,14 +121,6 @@ __device__ __forceinline__ i32x4 ld8_bf(const uint16_t* p, bool vec) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = (int)((uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16));
     return v;
-}
-
-// A launch that reports its own error, not an earlier call's (and without the
-// call-configuration calls of the <<<>>> form: 2.35 us of the host for 2.55).
-template <typename... P>
-static hipError_t kv4_launch(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, P... args) {
-    void* at[] = {(void*)&args...};
-    return hipLaunchKernel((const void*)kernel, grid, dim3(threads), at, 0, s);
 }
 
 // ---------------------------------------------------------------- append
@@ -331,8 +318,8 @@ template <int HD> __global__ void __launch_bounds__(KV4_THREADS) k_kv4_append(co
 hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s) {
     if (a.T < 1 || a.slot0 < 0 || a.slot0 > a.ctx_cap - a.T || a.Hkv < 1) return hipErrorInvalidValue;
     const dim3 grid(((a.slot0 + a.T - 1) >> 5) - (a.slot0 >> 5) + 1, a.Hkv);
-    if (a.hd == 128) return kv4_launch(k_kv4_append<128>, grid, KV4_THREADS, s, a);
-    if (a.hd == 64) return kv4_launch(k_kv4_append<64>, grid, KV4_THREADS, s, a);
+    if (a.hd == 128) return launch_checked(k_kv4_append<128>, grid, KV4_THREADS, s, a);
+    if (a.hd == 64) return launch_checked(k_kv4_append<64>, grid, KV4_THREADS, s, a);
     return hipErrorInvalidValue;
 }
 
@@ -369,8 +356,8 @@ hipError_t launch_kv4_pack(const void* kc, const void* vt, int heads, int hd, in
     if (tiles < 1 || tile0 < 0 || tile0 + tiles > ctx_cap >> 5 || heads < 1 || heads > 65535) return hipErrorInvalidValue;
     const dim3 grid(tiles, heads);
     const uint16_t *k = (const uint16_t*)kc, *v = (const uint16_t*)vt;
-    if (hd == 128) return kv4_launch(k_kv4_pack<128>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
-    if (hd == 64) return kv4_launch(k_kv4_pack<64>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
+    if (hd == 128) return launch_checked(k_kv4_pack<128>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
+    if (hd == 64) return launch_checked(k_kv4_pack<64>, grid, KV4_THREADS, s, k, v, ctx_cap, tile0, kv4);
     return hipErrorInvalidValue;
 }
 
@@ -413,8 +400,8 @@ template <int HD> __global__ void __launch_bounds__(KV4_THREADS) k_kv4_read(cons
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t s) {
     if (a.n < 1 || a.slot0 < 0 || a.slot0 > a.ctx_cap - a.n || a.Hkv < 1) return hipErrorInvalidValue;
     const dim3 grid(((a.slot0 + a.n - 1) >> 5) - (a.slot0 >> 5) + 1, a.Hkv);
-    if (a.hd == 128) return kv4_launch(k_kv4_read<128>, grid, KV4_THREADS, s, a);
-    if (a.hd == 64) return kv4_launch(k_kv4_read<64>, grid, KV4_THREADS, s, a);
+    if (a.hd == 128) return launch_checked(k_kv4_read<128>, grid, KV4_THREADS, s, a);
+    if (a.hd == 64) return launch_checked(k_kv4_read<64>, grid, KV4_THREADS, s, a);
     return hipErrorInvalidValue;
 }
 
@@ -503,34 +490,6 @@ template <int HD> __device__ __forceinline__ int kv4_out_d(int g, int dt) {
     return HD == 128 ? 32 * g + 4 * dt : 32 * (g >> 1) + 8 * dt + 4 * (g & 1);
 }
 
-// Running softmax state of a wave for a query tile: per lane its row's
-// reference score m (before scaling), the score that moves it, the sum l (the
-// same in all four elements) and O.
-template <int HD> struct Kv4State {
-    float m, top;
-    f32x4 l, O[HD / 16];
-    __device__ __forceinline__ void clear() {
-        m = top = -1e30f;
-        l = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int dt = 0; dt < HD / 16; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-};
-
-// Values of a pair of d tiles that are not finite, as 1.0 where they are and 0
-// elsewhere; the values themselves become 0.
-__device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
-    i32x4 f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w = (uint32_t)v[i];
-        const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-        f[i] = (int)(0x3f803f80u & (lo | hi));
-        v[i] = (int)(w & ~(lo | hi));
-    }
-    return f;
-}
-
 // The query rows of a tile as the B operand of the scaled MFMA, whose A operand
 // a record's key codes and scales are as they stand (16 x 16 x 128; block kg
 // of its k, 32 wide, is d = 32 kg + [0, 32) at hd 128, and d = 16 kg + [0, 16)
@@ -605,100 +564,6 @@ template <int HD> __device__ __forceinline__ Kv4Query<HD> kv4_query_get(const Kv
     return x;
 }
 
-// One key tile: S are the scores of its 32 slots, V(m, f) gives the value
-// fragments of d tiles 2m and 2m + 1.  next() computes the next tile's scores:
-// its MFMA run while this one's probabilities and values are converted.
-// MASKED: vm has the visibility of the lane's 8 slots to its row of each query
-// tile; CARE: values of unseen slots may not be finite.
-// A row's maximum follows its scores only where one passes it by KV4_SLACK (in
-// log2 units): probabilities are then at most 2^KV4_SLACK, which neither bf16
-// nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
-// maximum scales the probabilities before their rounding, so it takes the
-// row's own scores only: what a row gives does not hang on its neighbours.  The
-// sum of the (rounded) probabilities is one more row of the PV product.
-static constexpr float KV4_SLACK = 8.f;
-template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
-__device__ __forceinline__ void kv4_step(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
-                                         const uint32_t (&vm)[JT], NF next) {
-    constexpr int NDT = HD / 16;
-    if constexpr (MASKED) {
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) S[j][e >> 2][e & 3] = (vm[j] >> e) & 1u ? S[j][e >> 2][e & 3] : -INFINITY;
-    }
-    float mt[JT];
-    bool grow = false;
-#pragma unroll
-    for (int j = 0; j < JT; ++j) {
-        mt[j] = S[j][0][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) mt[j] = fmaxf(mt[j], S[j][e >> 2][e & 3]);
-        grow = grow || mt[j] > st[j].top;
-    }
-    if (__any(grow)) {
-        mfma_result_pad();
-#pragma unroll
-        for (int j = 0; j < JT; ++j) {
-            const float mr = pair_max32(pair_max16(mt[j]));
-            const float mn = mr > st[j].top ? mr : st[j].m;  // (other rows' scores do not move it)
-            const float f = __builtin_amdgcn_exp2f((st[j].m - mn) * c);
-            st[j].l *= f;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) st[j].O[dt] *= f;
-            st[j].m = mn;
-            st[j].top = mn + KV4_SLACK / c;
-        }
-    }
-    next();
-    i32x4 P[JT];
-#pragma unroll
-    for (int j = 0; j < JT; ++j) {
-        const float mc = st[j].m * c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1)], c, -mc));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1) + 1], c, -mc));
-            P[j][i] = (int)pack_bf(p0, p1);
-        }
-        const int one = 0x3f803f80;
-        st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
-    }
-#pragma unroll
-    for (int m = 0; m < NDT / 2; ++m) {
-        i32x4 Vf[2];
-        V(m, Vf);
-        if constexpr (CARE) {
-            i32x4 bad[2] = {take_nonfinite(Vf[0]), take_nonfinite(Vf[1])};
-            int any = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) any |= bad[0][i] | bad[1][i];
-            if (__any(any)) {  // rows that see a bad value's slot: NaN
-#pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    i32x4 seen;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        seen[i] = (int)(((vm[j] >> (2 * i)) & 1u ? 0x3f80u : 0u) |
-                                        ((vm[j] >> (2 * i + 1)) & 1u ? 0x3f800000u : 0u));
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const f32x4 n = mfma_step<ET_BF16>(bad[h], seen, f32x4{0.f, 0.f, 0.f, 0.f});
-                        mfma_result_pad();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (n[i] > 0.f) st[j].O[2 * m + h][i] = NAN;
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < JT; ++j) st[j].O[2 * m + h] = mfma_step<ET_BF16>(Vf[h], P[j], st[j].O[2 * m + h]);
-    }
-}
-
 // The scores of a tile of the 4-bit cache, and its step.
 template <int HD, int JT>
 __device__ __forceinline__ void kv4_scores(f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, const Kv4Query<HD> (&Q)[JT]) {
@@ -720,7 +585,7 @@ __device__ __forceinline__ void kv4_scores(f32x4 (&S)[JT][2], const Kv4Tile<HD>&
     }
 }
 template <int HD, int JT, bool MASKED, bool CARE, typename NF>
-__device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, float c,
+__device__ __forceinline__ void kv4_step4(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], const Kv4Tile<HD>& t, float c,
                                           const uint32_t (&vm)[JT], NF next) {
     float vs[8];
 #pragma unroll
@@ -736,7 +601,7 @@ __device__ __forceinline__ void kv4_step4(Kv4State<HD> (&st)[JT], f32x4 (&S)[JT]
             f[1][i] = (int)halves_hi(p[2 * i], p[2 * i + 1]);
         }
     };
-    kv4_step<HD, JT, MASKED, CARE>(st, S, c, V, vm, next);
+    attn_step<HD, JT, MASKED, CARE>(st, S, c, V, vm, next);
 }
 
 static constexpr int KV4_WAVES = 8;
@@ -832,7 +697,7 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
     __syncthreads();
 
     // the edge tiles, over the splits and the waves of each query tile
-    Kv4State<HD> es[1];
+    AttnState<HD> es[1];
     es[0].clear();
     for (int e = split + S * (WJ - 1 - wave / JT); e < tl.n_edge; e += workers) {
         const int pt = tl.edge(e);
@@ -908,13 +773,13 @@ __global__ void __launch_bounds__(64 * KV4_WAVES, 2) k_attn_kv4(const Kv4AttnArg
                     }
                 }
             };
-            if (__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) kv4_step<HD, 1, true, true>(es, Sc, c, V, vm, [] {});
-            else kv4_step<HD, 1, true, false>(es, Sc, c, V, vm, [] {});
+            if (__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) attn_step<HD, 1, true, true>(es, Sc, c, V, vm, [] {});
+            else attn_step<HD, 1, true, false>(es, Sc, c, V, vm, [] {});
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
     mfma_result_pad();
-    Kv4State<HD> st[JT];
+    AttnState<HD> st[JT];
     Kv4Query<HD> Q[JT];
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
@@ -1051,7 +916,7 @@ template <int HD> static hipError_t kv4_merge_go(const AttnArgs& a, int S, hipSt
     int SG = 1;
     while (SG < NG && SG * 2 <= S) SG *= 2;
     const unsigned wgs = ((unsigned)(a.H * a.T) + NG / SG - 1) / (NG / SG);
-    return kv4_launch(k_kv4_merge<HD>, dim3(wgs), KV4_MERGE_THREADS, s, a, S, SG);
+    return launch_checked(k_kv4_merge<HD>, dim3(wgs), KV4_MERGE_THREADS, s, a, S, SG);
 }
 
 // Query tiles per workgroup (jt) and splits of the key tiles (S), by the time
@@ -1089,7 +954,7 @@ Kv4Plan kv4_plan(int Lc, int n_tree, int T, int H, int Hkv, int hd, int win_sink
 }
 
 template <int HD, int JT> static hipError_t attn_kv4_go(const Kv4AttnArgs& k, dim3 grid, int tail, float c, hipStream_t s) {
-    return kv4_launch(tail == 0   ? k_attn_kv4<HD, JT, 0>
+    return launch_checked(tail == 0   ? k_attn_kv4<HD, JT, 0>
                       : tail == 1 ? k_attn_kv4<HD, JT, 1>
                                   : k_attn_kv4<HD, JT, 2>,
                       grid, 64 * KV4_WAVES, s, k, c);

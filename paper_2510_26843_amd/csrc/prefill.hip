@@ -7,26 +7,6 @@ namespace cas {
 
 // ---------------------------------------------------------------- GEMM of many rows
 
-// Direct-to-LDS load of one wave: 16 bytes per lane from base + voff (base
-// uniform, voff per lane) to LDS byte lds + 16 lane.  Written out because the
-// compiler, which cannot tell the ring's stages apart, would wait for every
-// load in flight before each LDS read; stage_wait() below is the wait.  (No
-// register is written; s_nop: the wait state between m0 and its use.)
-__device__ __forceinline__ void lds_load16(const char* base, uint32_t voff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds)
-                 : "memory");
-}
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
-// All but the last N of this wave's direct-to-LDS loads have landed and its
-// LDS reads are done; then the same holds for every wave of the workgroup.
-template <int N>
-__device__ __forceinline__ void stage_wait() {
-    static_assert(N >= 0 && N <= 63, "vmcnt");
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
 // 4 x 4 transpose over the lane groups g = lane / 16: lane group g's v[j]
 // becomes v[g] of lane group j.
 __device__ __forceinline__ void lane_transpose4(uint32_t (&v)[4]) {
