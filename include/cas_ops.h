@@ -271,6 +271,120 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
                                 void* stream);
 
 /*
+ * The paged KV cache: the new rows of several sequences appended to pages of a
+ * common pool, with their rotation, and attention of those rows over the
+ * sequences' pages.  One cas_paged describes the cache of a layer and the batch
+ * of a step; both calls take it (a host struct, read during the call; its
+ * arrays are on the device and are read by the kernels, so that a captured call
+ * replays with the lengths and pages that they hold then).
+ *   pages:     cas_op_paged_bytes(...) bytes, 16-byte aligned: bf16 [n_pages][2]
+ *              [n_kv_heads][page_size * head_dim], keys then values.  A head's
+ *              run is page_size / 32 tiles of 32 slots, the last index fastest:
+ *                keys    [2 h][hd/32 u][4 g][4 i][4 j][8 e]: slot 8i + 4h + j,
+ *                        element g hd/4 + 8u + e
+ *                values  [hd/16 m][4 g][16 r][8 e]: slot 8g + e, element 16m + r
+ *   table:     [n_seqs][table_len] page numbers; slot s of sequence b is slot
+ *              s % page_size of page table[b][s / page_size].  Entries past a
+ *              sequence's slots are not read.  Sequences may share pages
+ *   seq_start: [n_seqs + 1]: sequence b's rows are the rows seq_start[b] ..
+ *              seq_start[b + 1] - 1 of the call (none: it takes no part)
+ *   ctx_len:   [n_seqs] committed slots
+ *   nodes:     NULL, or [n_seqs] slots of the sequence's round behind the
+ *              committed ones, appended by earlier calls.  Row i of sequence b
+ *              lies in slot ctx_len[b] + nodes[b] + i
+ *   n_rows:    rows of the calls' tensors; rows behind the last sequence's are
+ *              not read and not written
+ *   max_rows:  rows of the longest sequence as far as the caller knows (0: may
+ *              be all): a hint by which a kernel is chosen, results are right
+ *              whatever it says
+ * A sequence whose slots do not fit its table row stores nothing, and its
+ * attention rows are NaN; so are rows that see a slot of a page outside [0,
+ * n_pages), and such a page is not written.
+ * Limits: head_dim 64 or 128; page_size a power of two from 32 to 4096;
+ * table_len * page_size at most 1048576; n_kv_heads at most 4096; n_seqs at most
+ * 65536; n_rows * n_heads / n_kv_heads below 2^24.
+ */
+typedef struct {
+    void* pages;
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+    const int32_t* table;
+    int32_t table_len, n_seqs;
+    const int32_t* seq_start;
+    const int32_t* ctx_len;
+    const int32_t* nodes;
+    int32_t n_rows, max_rows;
+} cas_paged;
+size_t cas_op_paged_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/*
+ * Write the rows' keys and values into their slots, and their queries to q_out.
+ * Other slots' bytes are not touched; two rows given the same slot (through
+ * shared pages) leave either.
+ *   k, v:  bf16 rows of n_kv_heads * head_dim elements, ldk and ldv elements
+ *          apart (at least that many: rows of a fused product in place)
+ *   q, q_out: NULL, or bf16 rows of n_heads * head_dim elements, ldq apart, and
+ *          [n_rows][n_heads][head_dim], 16-byte aligned.  q_out may be q (then
+ *          ldq = n_heads * head_dim)
+ *   rope_cos, rope_sin: NULL (nothing is rotated), or [n_pos][head_dim/2] fp32,
+ *          16-byte aligned: keys and queries are rotated, pairs (i, i +
+ *          head_dim/2) as in cas.h, in fp32, and rounded to bf16 once
+ *   pos:   [n_rows] positions, or NULL: a row's position is its slot.  A
+ *          position outside [0, n_pos) gives a key and query of NaN
+ */
+cas_status cas_op_paged_append(const cas_paged* cache, const void* q, int64_t ldq, int32_t n_heads, const void* k,
+                               int64_t ldk, const void* v, int64_t ldv, const int32_t* pos, const float* rope_cos,
+                               const float* rope_sin, int32_t n_pos, void* q_out, void* stream);
+
+/*
+ * Attention of the rows over their sequences' slots (fp32 softmax, scale 1 /
+ * sqrt(head_dim)).
+ *   q:    bf16 [n_rows][n_heads][head_dim]; out: bf16 [n_rows][n_heads * head_dim]
+ *   anc:  NULL: causal, a row sees the slots up to its own; or [n_rows][2]
+ *         ancestor-or-self masks: a row sees the committed slots, and slot
+ *         ctx_len + j where bit j of its mask is set (nodes + rows of a sequence
+ *         at most 128, else its rows are NaN)
+ *   attn_sink, attn_window: attn_window > 0 limits the slots before a causal
+ *         row's own, or a tree row's committed slots, to the first attn_sink and
+ *         the last attn_window ones (0: all)
+ * Slots and rows that a row does not see never reach it, whatever they hold.  A
+ * row that sees no slot gives zeros; one that sees a key that is not finite
+ * gives NaN, and one that sees such a value no finite one at its element.
+ * Probabilities are rounded to bf16 for the product with the values (each by at
+ * most 2^-8 of itself).  The result does not depend on earlier calls or on timing; it may
+ * depend in the last bits on the batch.
+ * n_heads <= 4096.  work: device scratch of cas_op_attention_paged_work_bytes
+ * (...) bytes (0: none is needed, work may be NULL), 16-byte aligned, used by
+ * one call at a time.  The size rests on the struct's numbers, not on its arrays.
+ */
+size_t cas_op_attention_paged_work_bytes(const cas_paged* cache, int32_t n_heads);
+cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t n_heads, const uint64_t* anc,
+                                  int32_t attn_sink, int32_t attn_window, void* out, void* work, size_t work_bytes,
+                                  void* stream);
+
+/*
+ * Log probabilities of given tokens, entropy and top alternatives of rows of
+ * logits, under the distribution p = softmax(scale * x) (natural logarithms):
+ *   ltype:   CAS_W_F32 or CAS_W_BF16; logits: n rows of V elements, ld (>= V)
+ *            elements apart
+ *   tokens:  [n][m] token ids; logp [n][m] fp32: log p of each, NaN for an id
+ *            outside [0, V) (m may be 0)
+ *   entropy: NULL, or [n] fp32: - sum p log p
+ *   K:       0 to 32; top_ids [n][K] int32 and top_logp [n][K] fp32: the tokens
+ *            of highest logit (decreasing, the lower id on ties; id -1 and
+ *            -infinity past the row's finite entries)
+ * A logit of -infinity has probability 0.  A row that holds a NaN or +infinity,
+ * or nothing but -infinity, has no distribution: NaN, and ids -1.
+ * scale: finite and > 0 (1 / temperature).  V at most 1048576, n * ceil(V /
+ * 8192) below 2^31.  Sums in fp32.
+ * work: device scratch of cas_op_logprobs_work_bytes(...) bytes, 16-byte
+ * aligned, used by one call at a time.
+ */
+size_t cas_op_logprobs_work_bytes(int32_t n, int32_t V, int32_t K);
+cas_status cas_op_logprobs(int32_t ltype, const void* logits, int64_t ld, int32_t n, int32_t V, float scale,
+                           const int32_t* tokens, int32_t m, float* logp, float* entropy, int32_t K, int32_t* top_ids,
+                           float* top_logp, void* work, size_t work_bytes, void* stream);
+
+/*
  * How a prefill block of T rows (129 to 2048) runs a linear layer; host only.
  *   wtype:  CAS_W_F32 or CAS_W_BF16; W [N][K]
  *   resid:  1 for the O and down projections (added to the residual stream)

@@ -23,7 +23,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcas.so")
 LIB_DEBUG = os.path.join(PKG, "libcas_debug.so")
 RUNTIME_CHECK = os.path.join(PKG, "cas_runtime_check")
-SOURCES = ("kernels.hip", "prefill.hip", "kv4.hip", "runtime.hip")
+SOURCES = ("kernels.hip", "prefill.hip", "kv4.hip", "paged.hip", "logprobs.hip", "runtime.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CLANG = os.environ.get("CAS_CLANG", "/opt/rocm/llvm/bin/clang")
 ROCM_LIB = "/opt/rocm/lib"
@@ -81,7 +81,7 @@ def build_runtime_check(verbose: bool = False) -> str:
     """Only the sanitized runtime check (needs the release kernel objects of a
     previous build())."""
     objdir = os.path.join(PKG, "_build")
-    kobjs = [os.path.join(objdir, k) for k in ("kernels.o", "prefill.o", "kv4.o")]
+    kobjs = [os.path.join(objdir, k) for k in ("kernels.o", "prefill.o", "kv4.o", "paged.o", "logprobs.o")]
     for k in kobjs:
         if not os.path.exists(k):
             raise RuntimeError(f"{k} is missing: run build() first")

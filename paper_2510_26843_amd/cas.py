@@ -51,7 +51,9 @@ EXPORTS = ("cas_create", "cas_destroy", "cas_last_error", "cas_create_error", "c
            "cas_debug_build", "cas_debug_check", "cas_debug_limit_slots",
            "cas_debug_limit_prefill", "cas_set_gemv", "cas_op_prefill_block", "cas_build_kv4",
            "cas_forward_draft_kv4", "cas_op_kv4_bytes", "cas_op_kv4_append", "cas_op_kv4_read",
-           "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes")
+           "cas_op_attention_kv4", "cas_op_attention_kv4_work_bytes", "cas_logprobs", "cas_op_paged_bytes",
+           "cas_op_paged_append", "cas_op_attention_paged", "cas_op_attention_paged_work_bytes", "cas_op_logprobs",
+           "cas_op_logprobs_work_bytes")
 # device check codes (cas_debug_check)
 DEVICE_CHECKS = ["none", "tree size", "token id", "parent order", "slot capacity", "RoPE position",
                  "KV write slot", "attention slots", "compaction path", "acceptance parent"]
@@ -142,6 +144,13 @@ def lib(debug: bool = False):
             "cas_op_kv4_read": ([P, I, I, I, I, I, P, P, P], I),
             "cas_op_attention_kv4": ([P, P, I, I, P, P, I, I, I, I, I, I, I, I, I, P, P, P, Z, P], I),
             "cas_op_attention_kv4_work_bytes": ([I] * 8, Z),
+            "cas_logprobs": ([P, I, ctypes.c_float, P, I, P, P, I, P, P], I),
+            "cas_op_paged_bytes": ([I] * 4, Z),
+            "cas_op_paged_append": ([P, P, ctypes.c_int64, I, P, ctypes.c_int64, P, ctypes.c_int64, P, P, P, I, P, P], I),
+            "cas_op_attention_paged": ([P, P, I, P, I, I, P, P, Z, P], I),
+            "cas_op_attention_paged_work_bytes": ([P, I], Z),
+            "cas_op_logprobs": ([I, P, ctypes.c_int64, I, I, ctypes.c_float, P, I, P, P, I, P, P, P, Z, P], I),
+            "cas_op_logprobs_work_bytes": ([I] * 3, Z),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -319,6 +328,18 @@ class Model:
         probs = np.zeros((n, K), dtype=np.float32)
         self._chk(self._L.cas_topk(self.h, int(n), int(K), _p(ids), _p(probs)))
         return ids, probs
+
+    def logprobs(self, tokens: np.ndarray, K: int = 0, scale: float = 1.0):
+        """Log probabilities of tokens [n][m] (or [n]) under the n rows of the
+        last forward, softmax(scale * logits): (logp of the tokens' shape,
+        entropy [n], top ids [n][K], their log probabilities [n][K])."""
+        t = np.ascontiguousarray(tokens, dtype=np.int32)
+        n, m = t.shape[0], 1 if t.ndim == 1 else t.shape[1]
+        logp, entropy = np.zeros(t.shape, dtype=np.float32), np.zeros(n, dtype=np.float32)
+        ids, best = np.zeros((n, K), dtype=np.int32), np.zeros((n, K), dtype=np.float32)
+        self._chk(self._L.cas_logprobs(self.h, int(n), float(scale), _p(t), int(m), _p(logp), _p(entropy), int(K),
+                                       _p(ids), _p(best)))
+        return logp, entropy, ids, best
 
     def compact(self, accepted: Sequence[int]) -> None:
         a = np.ascontiguousarray(accepted, dtype=np.int32)
@@ -502,6 +523,11 @@ class _KV4:
         self.append = (b16, b16, u8, i32, f32, f32)
         self.read = (u8, b16, b16)
         self.attend = (b16, u8, i64, b16, b16, b16, u8)
+        self.f32 = f32
+        self.paged = (b16, i32, i32, i32, i32)
+        self.append_paged = (b16, b16, b16, b16, i32, f32, f32)
+        self.attend_paged = (b16, b16, i64, u8)
+        self.logprobs = (b16 + f32, i32, f32, f32, i32, f32, u8)
 
 
 _kv4_types = None
@@ -631,3 +657,109 @@ def op_attention_kv4(q, kv4, ctx_cap: int, n4: int, Lc: int, n_tree: int, T: int
         (rows, Hkv * (ctx_cap // 32) * 34 * hd if n4 > 0 else 0, 16 * T, rows, 0, 0, 0))
     _ochk(L.cas_op_attention_kv4(qa, at, ctx_cap, n4, ka, va, kv_cap or 0, Lc, n_tree, T, H, Hkv, hd, sink, window, aa,
                                  oa, wa, 0 if work is None else work.nbytes, s), what)
+
+
+# the paged KV cache (bf16 device tensors [n_pages][2][Hkv][page_size * hd])
+
+class Paged(ctypes.Structure):
+    """The paged cache of a layer and the batch of a step (cas_paged): pages
+    [n_pages][2][Hkv][page_size * hd] bf16, table [B][pages of a sequence],
+    seq_start [B + 1], ctx_len [B] and nodes [B] (None: 0) int32; n_rows rows
+    in all, max_rows (a hint) of the longest sequence."""
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("table_len", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("seq_start", ctypes.c_void_p),
+                ("ctx_len", ctypes.c_void_p), ("nodes", ctypes.c_void_p), ("n_rows", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32)]
+
+    def __init__(self, pages, page_size: int, hd: int, table, seq_start, ctx_len, n_rows: int, max_rows: int = 0,
+                 nodes=None):
+        what, kv, shape, t = "cas_paged", _kv4_types or _kv4(), pages.shape, table.shape
+        if len(shape) != 4 or shape[1] != 2 or shape[3] != page_size * hd:
+            _refuse(what, "pages is not [n_pages][2][kv heads][page_size * hd]")
+        if len(t) != 2:
+            _refuse(what, "table is not [sequences][pages]")
+        B = t[0]
+        _, (pa, ta, sa, ca, na) = _call_at(
+            kv.torch, 0, what, "pages table seq_start ctx_len nodes", (pages, table, seq_start, ctx_len, nodes),
+            kv.paged, (pages.nbytes, table.nbytes, 4 * B + 4, 4 * B, 4 * B))
+        super().__init__(pa, shape[0], page_size, shape[2], hd, ta, t[1], B, sa, ca, na, n_rows, max_rows)
+        self.tensors = (pages, table, seq_start, ctx_len, nodes)  # (kept as long as their addresses)
+
+
+def paged_bytes(n_pages: int, page_size: int, Hkv: int, hd: int) -> int:
+    """Bytes of a pool of pages (0: the shape has none)."""
+    return int(lib().cas_op_paged_bytes(n_pages, page_size, Hkv, hd))
+
+
+def paged_work_bytes(cache: Paged, H: int) -> int:
+    """Bytes of op_attention_paged's scratch for H query heads (0: none)."""
+    return int(lib().cas_op_attention_paged_work_bytes(ctypes.addressof(cache), H))
+
+
+def op_paged_append(cache: Paged, k, v, q=None, q_out=None, pos=None, cos=None, sin=None, stream=None) -> None:
+    """Write the batch's keys and values (bf16 rows of Hkv * hd elements, any
+    row stride) into their slots; with q and q_out ([rows][H][hd]) also the
+    queries.  With cos and sin ([positions][hd/2] fp32) keys and queries are
+    rotated by pos ([rows] int32; None: their slots) first."""
+    what, kv = "cas_op_paged_append", _kv4_types or _kv4()
+    N, hd = cache.n_rows, cache.head_dim
+    w, H, wq, ldq, n_pos = cache.n_kv_heads * hd, 0, 0, 0, 0
+    ldk = _row_stride(what, "k", k, N, w, None, kv.b16)
+    ldv = _row_stride(what, "v", v, N, w, None, kv.b16)
+    if q_out is not None:
+        if len(q_out.shape) != 3 or q_out.shape[2] != hd:
+            _refuse(what, "q_out is not [rows][heads][hd]")
+        H = q_out.shape[1]
+        wq = H * hd
+        ldq = _row_stride(what, "q", q, N, wq, None, kv.b16)
+    if cos is not None:
+        shape = cos.shape
+        if len(shape) != 2 or 2 * shape[1] != hd:
+            _refuse(what, "cos is not [positions][hd / 2]")
+        n_pos = shape[0]
+    angles = 2 * n_pos * hd
+    s, (ka, va, qa, oa, pa, ca, sa) = _call_at(
+        kv.torch, stream, what, "k v q q_out pos cos sin", (k, v, q, q_out, pos, cos, sin), kv.append_paged,
+        (0, 0, 0, 2 * N * wq, 4 * N if n_pos else 0, angles, angles))
+    _ochk(lib().cas_op_paged_append(ctypes.addressof(cache), qa, ldq, H, ka, ldk, va, ldv, pa, ca, sa, n_pos, oa, s), what)
+
+
+def op_attention_paged(cache: Paged, q, out, anc=None, sink: int = 0, window: int = 0, stream=None, work=None) -> None:
+    """Attention of the batch's rows q [rows][H][hd] over their sequences'
+    pages into out [rows][H * hd] (bf16): causal, or by ancestor masks anc
+    [rows][2]; sink and window as in forward."""
+    what, kv, L = "cas_op_attention_paged", _kv4_types or _kv4(), lib()
+    if len(q.shape) != 3 or q.shape[2] != cache.head_dim:
+        _refuse(what, "q is not [rows][heads][hd]")
+    N, H, at = cache.n_rows, q.shape[1], ctypes.addressof(cache)
+    if work is None:
+        need = L.cas_op_attention_paged_work_bytes(at, H)
+        work = _work(need, stream) if need else None
+    rows = 2 * N * H * cache.head_dim
+    s, (qa, oa, aa, wa) = _call_at(kv.torch, stream, what, "q out anc work", (q, out, anc, work), kv.attend_paged,
+                                   (rows, rows, 16 * N, 0))
+    _ochk(L.cas_op_attention_paged(at, qa, H, aa, sink, window, oa, wa, 0 if work is None else work.nbytes, s), what)
+
+
+def op_logprobs(logits, tokens, logp, entropy=None, top_ids=None, top_logp=None, scale: float = 1.0, stream=None,
+                work=None) -> None:
+    """Log probabilities of tokens [n][m] (None: none) under softmax(scale *
+    logits), logits [n][V] fp32 or bf16 rows of any stride, into logp [n][m];
+    entropy [n]; top_ids, top_logp [n][K]: the K most likely tokens."""
+    what, kv, L = "cas_op_logprobs", _kv4_types or _kv4(), lib()
+    if len(logits.shape) != 2:
+        _refuse(what, "logits is not [rows][V]")
+    n, V = logits.shape
+    bf16 = logits.dtype in kv.b16
+    ld = _row_stride(what, "logits", logits, n, V, None, kv.b16 if bf16 else kv.f32)
+    m = 0 if tokens is None else tokens.numel() // n if n else 0
+    K = 0 if top_ids is None else top_ids.numel() // n if n else 0
+    if work is None:
+        work = _work(L.cas_op_logprobs_work_bytes(n, V, K), stream)
+    s, (xa, ta, la, ea, ia, ba, wa) = _call_at(
+        kv.torch, stream, what, "logits tokens logp entropy top_ids top_logp work",
+        (logits, tokens, logp, entropy, top_ids, top_logp, work), kv.logprobs,
+        (0, 4 * n * m, 4 * n * m, 4 * n, 4 * n * K, 4 * n * K, 0))
+    _ochk(L.cas_op_logprobs(W_BF16 if bf16 else W_F32, xa, ld, n, V, scale, ta, m, la, ea, K, ia, ba, wa, work.nbytes, s),
+          what)

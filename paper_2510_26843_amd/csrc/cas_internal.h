@@ -319,6 +319,65 @@ struct Kv4AttnArgs {
 };
 hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s);
 
+// ---- the paged KV cache (paged.hip): [n_pages][2][Hkv][page_size / 32] tiles of 32 * hd bf16
+// A batch of B sequences with N packed rows; all arrays are on the device.
+struct PagedBatch {
+    uint16_t* pages;
+    int n_pages, tshift;   // a page has 1 << tshift tiles of 32 slots
+    const int* table;      // [B][table_len] pages
+    int table_len, cap;    // cap: slots of a table row
+    const int *seq_start, *ctx_len, *nodes;  // [B + 1], [B], [B] or nullptr
+    int B, N, Hkv, hd;
+};
+struct PagedAppendArgs {
+    PagedBatch p;
+    const uint16_t *q, *k, *v;  // rows of heads * hd bf16, ld* elements apart (q may be nullptr)
+    size_t ldq, ldk, ldv;
+    int vec;                    // the rows allow 16-byte loads
+    int H;
+    const int* pos;             // positions of the rows (nullptr: their slots)
+    const float *cos, *sin;     // [n_pos][hd / 2] (nullptr: no rotation)
+    int n_pos;
+    uint16_t* q_out;            // [N][H][hd]
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s);
+struct PagedAttnArgs {
+    PagedBatch p;
+    const uint16_t* q;     // [N][H][hd]
+    const uint64_t* anc;   // [N][2], or nullptr: causal
+    uint16_t* out;         // [N][H * hd]
+    int H, sink, window;
+    float *part_o, *part_ml;  // partial states of the shares of split units
+    // set by the launch
+    int G, target, least;
+    uint32_t inv_G;
+};
+// How a call is launched: rows of a query tile, the most units of a kv head, the
+// shares aimed at beyond them (0: no unit is split), the least tiles of a share,
+// and the bytes of the partial states.
+struct PagedPlan {
+    int R, units, target, least;
+    size_t work;
+};
+PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows);
+hipError_t launch_attention_paged(const PagedAttnArgs& a, const PagedPlan& q, hipStream_t s);
+
+// ---- log probabilities (logprobs.hip)
+struct LogprobArgs {
+    const void* x;         // rows of V logits, ld elements apart
+    size_t ld;
+    int bf16, n, V;
+    float scale;
+    const int* tokens;     // [n][m]
+    int m, K;
+    float *logp, *entropy; // [n][m], [n] (nullptr: not wanted)
+    int* ids;              // [n][K]
+    float* best;           // [n][K]
+    float* work;           // logprob_work_bytes
+};
+size_t logprob_work_bytes(int n, int V, int K);
+hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
+
 // RMSNorm of rows of the fp32 residual stream h [T][d] with gains g:
 // writes the normalised rows as tiled activations of act type (out) or, with
 // q != NULL, their int8 quantisation (tiled int8 q, scales qs [T]) instead.

@@ -1,0 +1,550 @@
+// gfx950 kernels of the paged KV cache: appending the new rows of several
+// sequences with their rotation, and attention of those rows over it.
+//
+// A page holds page_size slots (a power of two of 32-slot tiles) of every kv
+// head, keys then values: [n_pages][2][Hkv][page_size / 32] tiles of 32 * hd
+// bf16 in the decoder's order of MFMA fragments (kv_k_tiled, kv_v_tiled), so a
+// wave reads a fragment as 1 KB in one piece and no tile crosses a page.
+// Sequence b of a batch has the slots [0, first + T): ctx_len[b] committed ones,
+// nodes[b] earlier ones of its round, and the T = seq_start[b + 1] -
+// seq_start[b] rows of the call at the slots from first on.
+//
+// Lengths, tables and positions are read on the device, so that a captured
+// call serves batches of other lengths: nothing they hold makes a kernel leave
+// its buffers.  Pages outside the pool store nothing and read as NaN, sequences
+// whose lengths do not fit get rows of NaN.
+#include "attn_step.h"
+
+#include <algorithm>
+
+namespace cas {
+
+// ---------------------------------------------------------------- sequences
+
+struct PagedSeq {
+    int b, row0, T, Lc, first;
+    bool fits;
+    __device__ __forceinline__ int n_slots() const { return first + T; }
+};
+
+// Sequence b's lengths (T = 0 past the last one, or where its rows are not rows
+// of the call).
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& p, int b, bool tree) {
+    PagedSeq s;
+    const int i = min(b, p.B - 1);
+    const int s0 = p.seq_start[i], s1 = p.seq_start[i + 1], nodes = p.nodes ? p.nodes[i] : 0;
+    s.b = i;
+    s.row0 = s0;
+    s.T = b < p.B && s0 >= 0 && s0 < s1 && s1 <= p.N ? s1 - s0 : 0;
+    s.Lc = p.ctx_len[i];
+    s.fits = s.Lc >= 0 && s.Lc <= p.cap && nodes >= 0 && nodes <= p.cap && s.Lc + nodes <= p.cap - s.T &&
+             (!tree || nodes + s.T <= 128);
+    s.first = s.Lc + nodes;
+    return s;
+}
+
+// ---------------------------------------------------------------- append
+
+// One workgroup = one tile (32 slots) that new rows fall into, for one kv head
+// (keys and values) or for the query heads of its group.  A sequence of T rows
+// touches at most T / 32 + 2 tiles, so those of sequence b are numbered from
+// row0 / 32 + 2 b on: no sum over the sequences before it.
+static constexpr int PAPP_THREADS = 256;
+
+__device__ __forceinline__ i32x4 paged_ld8(const uint16_t* p, bool vec) {
+    if (vec) return *(const i32x4*)p;
+    i32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (int)((uint32_t)p[2 * i] | ((uint32_t)p[2 * i + 1] << 16));
+    return v;
+}
+
+// The pieces x (elements d0 ..) and y (d0 + hd/2 ..) of a head row, rotated in
+// fp32 (each product's error 2^-24 of it) and rounded to bf16 once.
+__device__ __forceinline__ void paged_rotate(const float* cos, const float* sin, size_t at, bool ok, i32x4& x, i32x4& y) {
+    const f32x4 cs[2] = {*(const f32x4*)(cos + at), *(const f32x4*)(cos + at + 4)};
+    const f32x4 sn[2] = {*(const f32x4*)(sin + at), *(const f32x4*)(sin + at + 4)};
+    float lo[8], hi[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float a = piece_val<uint16_t>(x, e), b = piece_val<uint16_t>(y, e);
+        lo[e] = ok ? rope_lo(a, b, cs[e >> 2][e & 3], sn[e >> 2][e & 3]) : NAN;
+        hi[e] = ok ? rope_hi(a, b, cs[e >> 2][e & 3], sn[e >> 2][e & 3]) : NAN;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = (int)pack_bf(lo[2 * i], lo[2 * i + 1]);
+        y[i] = (int)pack_bf(hi[2 * i], hi[2 * i + 1]);
+    }
+}
+
+template <int HD> __global__ void __launch_bounds__(PAPP_THREADS) k_paged_append(const PagedAppendArgs a) {
+    const PagedBatch& p = a.p;
+    const int lane = threadIdx.x & 63;
+    // the last sequence whose tiles start at or before this one
+    int b = -1;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int i = min(b0 + lane, p.B - 1);
+        const uint64_t in = __ballot(b0 + lane < p.B && (int64_t)(p.seq_start[i] >> 5) + 2 * i <= (int64_t)blockIdx.x);
+        if (in) b = b0 + 63 - __builtin_clzll(in);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    if (b < 0) return;
+    const PagedSeq s = paged_seq(p, b, false);
+    if (s.T == 0 || !s.fits) return;
+    const int tile = (s.first >> 5) + (int)blockIdx.x - ((s.row0 >> 5) + 2 * b);
+    const int lo = max(s.first, tile * 32), hi = min(s.first + s.T, tile * 32 + 32);
+    if (lo >= hi) return;
+    const int row = s.row0 + tile * 32 - s.first;  // of the tile's slot 0
+    auto turn = [&](int sl, int d0, i32x4& x, i32x4& y) {
+        if (!a.cos) return;
+        const int pos = a.pos ? a.pos[row + sl] : tile * 32 + sl;
+        const bool ok = pos >= 0 && pos < a.n_pos;
+        paged_rotate(a.cos, a.sin, (size_t)(ok ? pos : 0) * (HD / 2) + d0, ok, x, y);
+    };
+    constexpr int PR = HD / 16;  // pairs of pieces of a head row
+    if ((int)blockIdx.y >= p.Hkv) {  // queries
+        const int G = a.H / p.Hkv, h0 = ((int)blockIdx.y - p.Hkv) * G, n = (hi - lo) * G * PR;
+        for (int it = threadIdx.x; it < n; it += PAPP_THREADS) {
+            const int d0 = it % PR * 8, h = it / PR % G, sl = lo - tile * 32 + it / PR / G;
+            const uint16_t* from = a.q + (size_t)(row + sl) * a.ldq + (size_t)(h0 + h) * HD + d0;
+            i32x4 x = paged_ld8(from, a.vec), y = paged_ld8(from + HD / 2, a.vec);
+            turn(sl, d0, x, y);
+            uint16_t* to = a.q_out + ((size_t)(row + sl) * a.H + h0 + h) * HD + d0;
+            *(i32x4*)to = x;
+            *(i32x4*)(to + HD / 2) = y;
+        }
+        return;
+    }
+    const int pid = p.table[(size_t)b * p.table_len + (tile >> p.tshift)];
+    if ((uint32_t)pid >= (uint32_t)p.n_pages) return;
+    const int h = blockIdx.y;
+    uint16_t* kt = p.pages + ((((size_t)pid * 2 * p.Hkv + h) << p.tshift) + (tile & ((1 << p.tshift) - 1))) * (32 * HD);
+    uint16_t* vt = kt + (((size_t)p.Hkv << p.tshift) * (32 * HD));
+    const int s_lo = lo - tile * 32, s_hi = hi - tile * 32;
+    if (threadIdx.x < 128) {
+        for (int it = threadIdx.x; it < 32 * PR; it += 128) {
+            const int sl = it % 32, d0 = it / 32 * 8;
+            if (sl < s_lo || sl >= s_hi) continue;
+            const uint16_t* from = a.k + (size_t)(row + sl) * a.ldk + (size_t)h * HD + d0;
+            i32x4 x = paged_ld8(from, a.vec), y = paged_ld8(from + HD / 2, a.vec);
+            turn(sl, d0, x, y);
+            *(i32x4*)(kt + kv_k_tiled(sl, d0, HD)) = x;
+            *(i32x4*)(kt + kv_k_tiled(sl, d0 + HD / 2, HD)) = y;
+        }
+    } else {  // four slots of 8 elements, turned: 8 bytes of a value fragment's lane each
+        const int it = threadIdx.x - 128;
+        const int d0 = it % (HD / 8) * 8, s4 = it / (HD / 8) * 4;
+        if (it >= HD || s4 >= s_hi || s4 + 4 <= s_lo) return;
+        i32x4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int sl = min(max(s4 + j, s_lo), s_hi - 1);
+            x[j] = paged_ld8(a.v + (size_t)(row + sl) * a.ldv + (size_t)h * HD + d0, a.vec);
+        }
+        const bool whole = s4 >= s_lo && s4 + 4 <= s_hi;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+            const uint32_t u = __builtin_amdgcn_perm((uint32_t)x[1][e >> 1], (uint32_t)x[0][e >> 1], sel);
+            const uint32_t w = __builtin_amdgcn_perm((uint32_t)x[3][e >> 1], (uint32_t)x[2][e >> 1], sel);
+            uint16_t* to = vt + kv_v_tiled(s4, d0 + e, HD);
+            if (whole) {
+                *(uint2*)to = make_uint2(u, w);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (s4 + j >= s_lo && s4 + j < s_hi) to[j] = (uint16_t)((j & 2 ? w : u) >> (16 * (j & 1)));
+            }
+        }
+    }
+}
+
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
+    const PagedBatch& p = a.p;
+    if (p.N < 1 || p.B < 1 || p.Hkv < 1 || (a.q && a.H % p.Hkv)) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)p.N / 32 + 2u * p.B, (unsigned)p.Hkv * (a.q ? 2 : 1));
+    if (p.hd == 128) return launch_checked(k_paged_append<128>, grid, PAPP_THREADS, s, a);
+    if (p.hd == 64) return launch_checked(k_paged_append<64>, grid, PAPP_THREADS, s, a);
+    return hipErrorInvalidValue;
+}
+
+// ---------------------------------------------------------------- attention: the work and its shares
+
+// Slots that a row sees.  Causal: those up to its own; with a window, of the
+// ones before it the first `sink` and the last `window`.  Tree: committed slots
+// (the first `sink` and the last `window` of them) and the nodes of its mask.
+// A call's tiles for the rows [t0, t1) of a sequence: the sink's, then from pt0.
+struct PagedRange {
+    int st, pt0, n_log;  // tiles [0, st) and [pt0, pt0 + n_log - st)
+    int wlo, whi;        // whole for every row: tiles in [wlo, whi) and below ...
+    int slo;             // ... slo
+    __device__ __forceinline__ int phys(int lt) const { return lt < st ? lt : lt - st + pt0; }
+    __device__ __forceinline__ bool whole(int tile) const { return (tile >= wlo && tile < whi) || tile < slo; }
+    __device__ PagedRange(const PagedSeq& s, int t0, int t1, bool tree, int sink, int window) {
+        // slots every row sees as committed: [0, all), and those any row sees: [0, any)
+        const int all = tree ? s.Lc : s.first + t0 + 1, any = tree ? s.n_slots() : s.first + t1;
+        const int n_tiles = (any + 31) >> 5;
+        st = 0;
+        pt0 = 0;
+        wlo = 0;
+        whi = all >> 5;
+        slo = 0;
+        if (window > 0) {
+            const int w0 = max((tree ? s.Lc : s.first + t0) - window, 0);      // the first row's window starts
+            const int w1 = max((tree ? s.Lc : s.first + t1 - 1) - window, 0);  // the last row's
+            st = min((min(sink, all) + 31) >> 5, n_tiles);
+            pt0 = min(max(w0 >> 5, st), n_tiles);
+            slo = min(sink, all) >> 5;
+            wlo = (w1 + 31) >> 5;
+        }
+        n_log = st + n_tiles - pt0;
+    }
+};
+
+// Visibility of the 8 slots base .. to row t of a sequence.
+__device__ __forceinline__ uint32_t paged_vis8(const PagedSeq& s, int t, int base, bool tree, uint64_t an0, uint64_t an1,
+                                               int sink, int window) {
+    if (tree) return attn_vis8(base, s.Lc, s.n_slots(), AttnWindow(s.Lc, s.n_slots() - s.Lc, sink, window), an0, an1);
+    const int own = s.first + t;
+    if (window == 0) return bits8(0, own + 1 - base);
+    return bits8(0, min(sink, own) - base) | bits8(own - window - base, own + 1 - base);
+}
+
+// How the work is shared out.  A unit is (sequence, query tile of R packed
+// rows, kv head); the split rule gives a sequence of more than C tiles ns =
+// ceil(tiles / C) shares per unit, with C such that the batch has about
+// `target` shares of C tiles, so that one long sequence among short ones is
+// split and equal ones that fill the chip by themselves are not.  Every wave
+// sums the sequences' work and finds its own share, 64 sequences at a time:
+// the kernels need no plan made before them, and a replayed call shares out
+// the lengths of its own time.
+//   shares in all:            sum nq ns <= sum nq + target    (ns - 1 < tiles / C)
+//   shares of split units:    <= 2 target                     (ns < 2 tiles / C)
+//   split units:              <= target
+struct PagedShare {
+    PagedSeq s;
+    int ns, nq, local, part;  // local: place among the sequence's; part: first partial of the sequence's
+    bool found;
+};
+template <bool MERGE>
+__device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R, uint32_t inv_G, int item) {
+    const PagedBatch& p = a.p;
+    const int lane = threadIdx.x & 63, G = a.G;
+    const bool tree = a.anc != nullptr;
+    struct Seq {
+        PagedSeq s;
+        int nq, tiles;
+    };
+    auto seq = [&](int b) {
+        Seq q;
+        q.s = paged_seq(p, b, tree);
+        q.nq = (int)(((int64_t)q.s.T * G + R - 1) / R);
+        q.tiles = !q.s.fits || q.s.T == 0 ? 0 : (q.s.n_slots() + 31) >> 5;
+        if (a.window > 0) {  // (the most that one of its query tiles walks)
+            const int t = tree ? q.s.n_slots() - q.s.Lc : min(q.s.T, R / G + 2);
+            q.tiles = min(q.tiles, ((a.sink + 31) >> 5) + ((min(a.window, p.cap) + t + 31) >> 5) + 1);
+        }
+        return q;
+    };
+    const Seq own = seq(lane);
+    int C = 1 << 30;
+    if (a.target > 0) {
+        uint64_t w = (uint64_t)own.nq * own.tiles;
+        for (int b0 = 64; b0 < p.B; b0 += 64) {
+            const Seq q = seq(b0 + lane);
+            w += (uint64_t)q.nq * q.tiles;
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor(w, o);
+        C = max(a.least, (int)min((uint64_t)1 << 30, (w + a.target - 1) / a.target));
+    }
+    PagedShare r;
+    r.found = false;
+    int before = 0, parts = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const Seq q = b0 ? seq(b0 + lane) : own;
+        const int ns = max((q.tiles + C - 1) / C, 1);
+        int n = MERGE ? (ns > 1 ? q.nq : 0) : q.nq * ns, np = ns > 1 ? q.nq * ns : 0;
+        const int n_own = n, np_own = np;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(n, o), y = __shfl_up(np, o);
+            if (lane >= o) {
+                n += x;
+                np += y;
+            }
+        }
+        const uint64_t past = __ballot(before + n > item);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            r.s = paged_seq(p, b0 + l, tree);
+            r.s.T = __shfl(q.s.T, l);
+            r.ns = __builtin_amdgcn_readlane(ns, l);
+            r.nq = __builtin_amdgcn_readlane(q.nq, l);
+            r.local = item - before - __builtin_amdgcn_readlane(n - n_own, l);
+            r.part = parts + __builtin_amdgcn_readlane(np - np_own, l);
+            r.found = true;
+            return r;
+        }
+        before += __builtin_amdgcn_readlane(n, 63);
+        parts += __builtin_amdgcn_readlane(np, 63);
+    }
+    return r;
+}
+
+// ---------------------------------------------------------------- attention: few rows
+
+// Workgroup = (share of a unit, kv head): JT query tiles of 16 packed rows (row
+// p = token p / G, head p % G of the group), the share's key tiles over eight
+// waves, each with the running maximum and sum of a softmax of its own (attn_step),
+// joined through LDS at the end.  K and V fragments go from memory to the
+// registers that the MFMA reads.
+static constexpr int PAGED_WAVES = 8;
+
+template <int HD> struct PagedTile {
+    i32x4 k[HD / 16], v[HD / 16];  // key fragments (h2, u), value fragments dt
+    bool ok;
+};
+
+template <int HD, int JT>
+__device__ __forceinline__ void paged_scores(f32x4 (&S)[JT][2], const i32x4 (&k)[HD / 16], const i32x4 (&Q)[JT][HD / 32]) {
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            S[j][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < HD / 32; ++u) S[j][h] = mfma_step<ET_BF16>(k[h * (HD / 32) + u], Q[j][u], S[j][h]);
+        }
+}
+
+template <int HD, int JT>
+__global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedAttnArgs a, float c) {
+    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, RS = HD + 4, W = PAGED_WAVES, R = 16 * JT;
+    const PagedBatch& p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4, G = a.G;
+    const int kvh = blockIdx.x % p.Hkv;
+    const PagedShare sh = paged_share<false>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    if (!sh.found) return;
+    const PagedSeq& s = sh.s;
+    const bool tree = a.anc != nullptr;
+    const int qt = sh.local % sh.nq, split = sh.local / sh.nq;
+    auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
+    const int rows = s.T * G, p0 = qt * R;
+    const int t0 = token(p0), t1 = token(min(p0 + R, rows) - 1) + 1;
+
+    __shared__ float sm_m[W][16], sm_l[W][16];
+    __shared__ __attribute__((aligned(16))) float sm_o[W][16][RS];
+    AttnState<HD> st[JT];
+#pragma unroll
+    for (int j = 0; j < JT; ++j) st[j].clear();
+    if (s.fits) {
+        i32x4 Q[JT][UD];
+        int tok[JT];
+        uint64_t an[JT][2];
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+            const int x = min(p0 + 16 * j + r, rows - 1);
+            tok[j] = token(x);
+            const size_t row = (size_t)(s.row0 + tok[j]);
+            const uint16_t* q = a.q + (row * a.H + kvh * G + (x - tok[j] * G)) * HD + g * DG;
+#pragma unroll
+            for (int u = 0; u < UD; ++u) Q[j][u] = *(const i32x4*)(q + u * 8);
+            an[j][0] = tree ? a.anc[2 * row] : 0;
+            an[j][1] = tree ? a.anc[2 * row + 1] : 0;
+        }
+        const PagedRange rg(s, t0, t1, tree, a.sink, a.window);
+        const int lo = (int)((int64_t)rg.n_log * split / sh.ns), n = (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo;
+        const int w0 = lo + n * wave / W, w1 = lo + n * (wave + 1) / W;
+        const int* table = p.table + (size_t)s.b * p.table_len;
+        const size_t vofs = ((size_t)p.Hkv << p.tshift) * (32 * HD);
+        const int tmask = (1 << p.tshift) - 1;
+        auto load = [&](int lt) {
+            PagedTile<HD> t;
+            const int tile = rg.phys(lt);
+            int pid = table[tile >> p.tshift];
+            t.ok = (uint32_t)pid < (uint32_t)p.n_pages;
+            pid = t.ok ? pid : 0;
+            const uint16_t* k = p.pages + ((((size_t)pid * 2 * p.Hkv + kvh) << p.tshift) + (tile & tmask)) * (32 * HD);
+#pragma unroll
+            for (int i = 0; i < NDT; ++i) {
+                t.k[i] = *(const i32x4*)(k + i * 512 + lane * 8);
+                t.v[i] = *(const i32x4*)(k + vofs + i * 512 + lane * 8);
+            }
+            return t;
+        };
+        for (int lt = w0; lt < w1; ++lt) {
+            const int tile = rg.phys(lt);
+            const PagedTile<HD> t = load(lt);
+            f32x4 S[JT][2];
+            paged_scores<HD, JT>(S, t.k, Q);
+            if (!t.ok) {
+#pragma unroll
+                for (int j = 0; j < JT; ++j) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+            }
+            auto V = [&](int m, i32x4 (&f)[2]) {
+                f[0] = t.v[2 * m];
+                f[1] = t.v[2 * m + 1];
+            };
+            uint32_t vm[JT];
+            if (rg.whole(tile)) {
+                attn_step<HD, JT, false, false>(st, S, c, V, vm, [] {});
+            } else {
+#pragma unroll
+                for (int j = 0; j < JT; ++j)
+                    vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < NDT; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t x = (uint32_t)t.v[i][w];
+                        bad = bad || (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+                    }
+                if (__any(bad)) attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
+                else attn_step<HD, JT, true, false>(st, S, c, V, vm, [] {});
+            }
+            mfma_result_pad();
+        }
+    }
+
+    // ---- join the waves, one query tile after another
+    constexpr int D4 = HD / 4;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        if (j) __syncthreads();
+        if (g == 0) {
+            sm_m[wave][r] = st[j].m * c;
+            sm_l[wave][r] = st[j].l[0];
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) *(f32x4*)(&sm_o[wave][r][16 * dt + 4 * g]) = st[j].O[dt];
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < 16 * D4; idx += 64 * W) {
+            const int rr = idx / D4, d4 = (idx % D4) * 4, x = p0 + 16 * j + rr;
+            if (x >= rows) continue;
+            float mw[W], M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                mw[w] = sm_m[w][rr];
+                M = fmaxf(M, mw[w]);
+            }
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            float L = s.fits ? 0.f : NAN;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float f = __builtin_amdgcn_exp2f(mw[w] - M);
+                attn_merge_o(acc, *(const f32x4*)(&sm_o[w][rr][d4]), f);
+                attn_merge_l(L, sm_l[w][rr], f);
+            }
+            if (sh.ns == 1) {
+                const float inv = L != 0.f ? 1.f / L : 0.f;  // no slot seen: 0 (a NaN sum stays one)
+                const int t = token(x);
+                st4(a.out, ((size_t)(s.row0 + t) * a.H + kvh * G + (x - t * G)) * HD + d4, acc[0] * inv, acc[1] * inv,
+                    acc[2] * inv, acc[3] * inv);
+            } else {
+                const size_t o = ((size_t)(sh.part + sh.local) * p.Hkv + kvh) * R + 16 * j + rr;
+                *(f32x4*)(a.part_o + o * HD + d4) = acc;
+                if (d4 == 0) *(float2*)(a.part_ml + o * 2) = make_float2(M, L);
+            }
+        }
+    }
+}
+
+// The join of the shares of split units: hd / 4 threads per row, NS of them
+// taking every NS-th share, then through LDS.
+static constexpr int PMERGE_THREADS = 256, PMERGE_NS = 4;
+template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merge(const PagedAttnArgs a, int R) {
+    constexpr int D4 = HD / 4, NG = PMERGE_THREADS / D4, NS = PMERGE_NS, NR = NG / NS;
+    __shared__ float2 sm_ml[NG];
+    __shared__ f32x4 sm_o[NG][D4];
+    const PagedBatch& p = a.p;
+    const int kvh = blockIdx.x % p.Hkv, G = a.G;
+    const PagedShare sh = paged_share<true>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    if (!sh.found) return;
+    const int gi = threadIdx.x / D4, d4 = threadIdx.x % D4 * 4, sub = gi % NS;
+    const int p0 = sh.local * R, rows = min(sh.s.T * G - p0, R);
+    for (int i0 = blockIdx.y * NR; i0 < rows; i0 += gridDim.y * NR) {  // (the same for every thread)
+        const int i = min(i0 + gi / NS, rows - 1);
+        float M = -1e30f, L = 0.f;
+        f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+        for (int k0 = sub; k0 < sh.ns; k0 += 4 * NS) {
+            float2 ml[4];
+            f32x4 po[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int sp = min(k0 + k * NS, sh.ns - 1);
+                const size_t o = ((size_t)(sh.part + sp * sh.nq + sh.local) * p.Hkv + kvh) * R + i;
+                ml[k] = *(const float2*)(a.part_ml + o * 2);
+                po[k] = *(const f32x4*)(a.part_o + o * HD + d4);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + k * NS < sh.ns) {
+                    const f32x4 o[1] = {po[k]};
+                    attn_merge_split<1>(acc, L, M, o, ml[k].y, ml[k].x);
+                }
+        }
+        if (d4 == 0) sm_ml[gi] = make_float2(M, L);
+        sm_o[gi][d4 / 4] = acc[0];
+        __syncthreads();
+        if (sub == 0 && i0 + gi / NS < rows) {
+            for (int k = 1; k < NS; ++k) {
+                const f32x4 o[1] = {sm_o[gi + k][d4 / 4]};
+                attn_merge_split<1>(acc, L, M, o, sm_ml[gi + k].y, sm_ml[gi + k].x);
+            }
+            const float inv = L != 0.f ? 1.f / L : 0.f;
+            const int x = p0 + i, t = a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x;
+            st4(a.out, ((size_t)(sh.s.row0 + t) * a.H + kvh * G + (x - t * G)) * HD + d4, acc[0][0] * inv,
+                acc[0][1] * inv, acc[0][2] * inv, acc[0][3] * inv);
+        }
+        __syncthreads();
+    }
+}
+
+// Query tiles per workgroup (16-row tiles), and the shares aimed at.
+static constexpr int PAGED_SHARES = 256;  // workgroups of the whole launch: one per CU
+static constexpr int PAGED_LEAST = 16;    // tiles of a share
+
+PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
+    PagedPlan q;
+    const int G = H / p.Hkv;
+    q.R = (int64_t)std::min(max_rows, p.N) * G > 16 ? 32 : 16;
+    q.units = (int)(((int64_t)p.N * G) / q.R) + p.B;
+    q.target = (PAGED_SHARES + p.Hkv - 1) / p.Hkv;
+    q.least = PAGED_LEAST;
+    if ((p.cap >> 5) <= q.least) q.target = 0;  // no sequence can be split
+    q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
+    return q;
+}
+
+template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const PagedPlan& q, float c, hipStream_t s) {
+    const PagedBatch& p = a.p;
+    const dim3 grid((unsigned)(q.units + q.target) * p.Hkv);
+    hipError_t e = q.R == 16 ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
+                             : launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c);
+    if (e != hipSuccess || q.target == 0) return e;
+    constexpr int NR = PMERGE_THREADS / (HD / 4) / PMERGE_NS;
+    const unsigned units = (unsigned)std::min(q.units, q.target);
+    return launch_checked(k_paged_merge<HD>, dim3(units * p.Hkv, q.R / NR), PMERGE_THREADS, s, a, q.R);
+}
+
+hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q, hipStream_t s) {
+    PagedAttnArgs a = args;
+    const PagedBatch& p = a.p;
+    if (p.N < 1 || p.B < 1 || p.Hkv < 1 || a.H % p.Hkv) return hipErrorInvalidValue;
+    a.G = a.H / p.Hkv;
+    // (multiplying by it and taking the high word divides exactly below 2^25)
+    a.inv_G = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
+    a.target = q.target;
+    a.least = q.least;
+    a.part_ml = a.part_o + (size_t)2 * q.target * p.Hkv * q.R * p.hd;
+    const float c = (1.0f / sqrtf((float)p.hd)) * 1.4426950408889634f;
+    if (p.hd == 128) return paged_attn_go<128>(a, q, c, s);
+    if (p.hd == 64) return paged_attn_go<64>(a, q, c, s);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace cas

@@ -139,6 +139,8 @@ struct cas_ctx {
     int* d_acc = nullptr;
     int* h_result = nullptr;  // pinned
     int* h_topk = nullptr;    // pinned: [max_tree][16] ids, [max_tree][16] probabilities, [max_tree] NaN flags
+    int* h_logp = nullptr;    // pinned (cas_logprobs): tokens and logp [max_tree][128], entropy, top ids and logp [max_tree][32]
+    float* d_logp = nullptr;  // its partial sums
 
     Stage stage[kStages];
     int stage_i = 0;
@@ -878,6 +880,7 @@ void free_ctx(cas_ctx* c) {
     }
     if (c->h_result) (void)hipHostFree(c->h_result);
     if (c->h_topk) (void)hipHostFree(c->h_topk);
+    if (c->h_logp) (void)hipHostFree(c->h_logp);
     for (void* p : c->allocs) (void)hipFree(p);
     if (c->own_stream && c->stream) (void)hipStreamDestroy(c->stream);
     delete c;
@@ -1347,6 +1350,65 @@ cas_status cas_topk(cas_ctx* c, int32_t n, int32_t K, int32_t* ids, float* probs
         if (h_flag[i]) return fail(c, CAS_ERR_DEVICE, "NaN in the logits of row " + std::to_string(i));
     memcpy(ids, h_ids, sizeof(int) * (size_t)n * K);
     memcpy(probs, h_p, sizeof(float) * (size_t)n * K);
+    return CAS_OK;
+}
+
+static constexpr int kLogpTokens = 128, kLogpTop = 32;  // most tokens and alternatives of a row
+
+cas_status cas_logprobs(cas_ctx* c, int32_t n, float scale, const int32_t* tokens, int32_t m, float* logp,
+                        float* entropy, int32_t K, int32_t* top_ids, float* top_logp) {
+    if (!c) return CAS_ERR_ARG;
+    if (m < 0 || m > kLogpTokens) return fail(c, CAS_ERR_ARG, "m must be in [0, 128]");
+    if (K < 0 || K > kLogpTop) return fail(c, CAS_ERR_ARG, "K must be in [0, 32]");
+    if ((m && (!tokens || !logp)) || (K && (!top_ids || !top_logp)))
+        return fail(c, CAS_ERR_ARG, "tokens and output pointers must not be NULL");
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(c, CAS_ERR_ARG, "scale must be finite and > 0");
+    if (c->logits_rows < 1) return fail(c, CAS_ERR_STATE, "cas_logprobs needs a forward first");
+    if (n != c->logits_rows)
+        return fail(c, CAS_ERR_ARG, "n must equal the last forward's row count " + std::to_string(c->logits_rows));
+    const size_t cap = (size_t)c->cfg.max_tree;
+    if (!c->h_logp || !c->d_logp) {
+        int cur = -1;
+        HIPCHK(c, hipGetDevice(&cur));
+        if (cur != c->dev) HIPCHK(c, hipSetDevice(c->dev));
+        hipError_t e = hipSuccess;
+        if (!c->h_logp) e = hipHostMalloc((void**)&c->h_logp, cap * (2 * kLogpTokens + 1 + 2 * kLogpTop) * 4, hipHostMallocDefault);
+        if (e != hipSuccess) c->h_logp = nullptr;
+        else if (!c->d_logp) e = dalloc(c, &c->d_logp, logprob_work_bytes((int)cap, c->cfg.vocab, kLogpTop));
+        if (e != hipSuccess) (void)hipGetLastError();  // (the launches after it report the last error)
+        if (cur != c->dev) (void)hipSetDevice(cur);
+        if (e != hipSuccess) return fail(c, CAS_ERR_OOM, "allocation of the log probabilities' buffers");
+    }
+    // (as in cas_topk, the kernels read and write their few words in pinned memory)
+    LogprobArgs a{};
+    int* h_tok = c->h_logp;
+    a.logp = (float*)(h_tok + cap * kLogpTokens);
+    a.entropy = a.logp + cap * kLogpTokens;
+    a.ids = (int*)(a.entropy + cap);
+    a.best = (float*)(a.ids + cap * kLogpTop);
+    if (m) memcpy(h_tok, tokens, sizeof(int) * (size_t)n * m);
+    a.x = c->d_logits;
+    a.ld = (size_t)c->cfg.vocab;
+    a.n = n;
+    a.V = c->cfg.vocab;
+    a.scale = scale;
+    a.tokens = h_tok;
+    a.m = m;
+    a.K = K;
+    a.work = c->d_logp;
+    hipError_t e = timed(c, CAS_K_TOPK, [&]() -> hipError_t { return launch_logprobs(a, c->stream); });
+    if (e != hipSuccess) return hip_fail(c, e, "log probabilities launch");
+    HIPCHK(c, hipStreamSynchronize(c->stream));
+    cas_status cst = poll_checks(c);
+    if (cst != CAS_OK) return cst;
+    for (int i = 0; i < n; ++i)
+        if (a.entropy[i] != a.entropy[i]) return fail(c, CAS_ERR_DEVICE, "NaN in the logits of row " + std::to_string(i));
+    if (m) memcpy(logp, a.logp, sizeof(float) * (size_t)n * m);
+    if (entropy) memcpy(entropy, a.entropy, sizeof(float) * (size_t)n);
+    if (K) {
+        memcpy(top_ids, a.ids, sizeof(int) * (size_t)n * K);
+        memcpy(top_logp, a.best, sizeof(float) * (size_t)n * K);
+    }
     return CAS_OK;
 }
 
@@ -1874,6 +1936,153 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
     a.vr = (const uint16_t*)v;
     a.kv_cap = kv_cap;
     return launch_attention_kv4(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
+// ---- the paged KV cache
+
+static constexpr int PAGED_MAX_HEADS = 4096, PAGED_MAX_SEQS = 65536, PAGED_MAX_WINDOW = 1 << 21;
+static bool paged_shape(int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t hd, cas_status* st) {
+    *st = CAS_ERR_ARG;
+    if (n_pages < 1 || page_size < 32 || page_size > 4096 || (page_size & (page_size - 1)) || Hkv < 1) return false;
+    *st = CAS_ERR_UNSUPPORTED;
+    if ((hd != 64 && hd != 128) || Hkv > PAGED_MAX_HEADS) return false;
+    *st = CAS_OK;
+    return true;
+}
+
+size_t cas_op_paged_bytes(int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t hd) {
+    cas_status st;
+    return paged_shape(n_pages, page_size, Hkv, hd, &st) ? (size_t)n_pages * 2 * Hkv * page_size * hd * 2 : 0;
+}
+
+// The numbers of a batch (its arrays only where `arrays`), H query heads.
+static bool paged_batch(const cas_paged* c, int32_t H, bool arrays, PagedBatch* p, cas_status* st) {
+    *st = CAS_ERR_ARG;
+    if (!c) return false;
+    if (!paged_shape(c->n_pages, c->page_size, c->n_kv_heads, c->head_dim, st)) return false;
+    *st = CAS_ERR_ARG;
+    if (c->n_seqs < 1 || c->n_seqs > PAGED_MAX_SEQS || c->n_rows < 1 || c->max_rows < 0 || c->table_len < 1) return false;
+    if ((int64_t)c->table_len * c->page_size > KV4_MAX_CAP) return false;
+    if (H < 1 || H > PAGED_MAX_HEADS || H % c->n_kv_heads) return false;
+    const int64_t rows = (int64_t)c->n_rows * (H / c->n_kv_heads);  // of a kv head
+    if (rows >= 1 << 24) return false;
+    *st = CAS_ERR_UNSUPPORTED;
+    if ((rows / 16 + c->n_seqs + 4096) * c->n_kv_heads > INT32_MAX) return false;  // (a grid dimension)
+    *st = CAS_ERR_ARG;
+    if (arrays) {
+        if (!c->pages || !c->table || !c->seq_start || !c->ctx_len || !aligned16(c->pages)) return false;
+        if (((uintptr_t)c->table | (uintptr_t)c->seq_start | (uintptr_t)c->ctx_len | (uintptr_t)c->nodes) & 3) return false;
+    }
+    p->pages = (uint16_t*)c->pages;
+    p->n_pages = c->n_pages;
+    p->tshift = __builtin_ctz((unsigned)c->page_size) - 5;
+    p->table = c->table;
+    p->table_len = c->table_len;
+    p->cap = c->table_len * c->page_size;
+    p->seq_start = c->seq_start;
+    p->ctx_len = c->ctx_len;
+    p->nodes = c->nodes;
+    p->B = c->n_seqs;
+    p->N = c->n_rows;
+    p->Hkv = c->n_kv_heads;
+    p->hd = c->head_dim;
+    *st = CAS_OK;
+    return true;
+}
+
+cas_status cas_op_paged_append(const cas_paged* cache, const void* q, int64_t ldq, int32_t H, const void* k, int64_t ldk,
+                               const void* v, int64_t ldv, const int32_t* pos, const float* cos, const float* sin,
+                               int32_t n_pos, void* q_out, void* stream) {
+    cas_status st;
+    PagedAppendArgs a{};
+    if (!k || !v || !cos != !sin || !q != !q_out) return CAS_ERR_ARG;
+    if (!paged_batch(cache, q ? H : cache ? cache->n_kv_heads : 0, true, &a.p, &st)) return st;
+    const int64_t w = (int64_t)a.p.Hkv * a.p.hd;
+    if (ldk < w || ldv < w || (q && ldq < (int64_t)H * a.p.hd) || (q && q == q_out && ldq != (int64_t)H * a.p.hd))
+        return CAS_ERR_ARG;
+    if (cos && n_pos < 1) return CAS_ERR_ARG;
+    if (!aligned16(cos) || !aligned16(sin) || !aligned16(q_out) || ((uintptr_t)pos & 3)) return CAS_ERR_ARG;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) & 1) return CAS_ERR_ARG;
+    a.q = (const uint16_t*)q;
+    a.k = (const uint16_t*)k;
+    a.v = (const uint16_t*)v;
+    a.ldq = (size_t)ldq;
+    a.ldk = (size_t)ldk;
+    a.ldv = (size_t)ldv;
+    a.vec = aligned16(k) && aligned16(v) && aligned16(q) && ldk % 8 == 0 && ldv % 8 == 0 && (!q || ldq % 8 == 0);
+    a.H = H;
+    a.pos = pos;
+    a.cos = cos;
+    a.sin = sin;
+    a.n_pos = n_pos;
+    a.q_out = (uint16_t*)q_out;
+    return launch_paged_append(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
+size_t cas_op_attention_paged_work_bytes(const cas_paged* cache, int32_t H) {
+    cas_status st;
+    PagedBatch p{};
+    if (!paged_batch(cache, H, false, &p, &st)) return 0;
+    return paged_plan(p, H, cache->max_rows ? cache->max_rows : p.N).work;
+}
+
+cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t H, const uint64_t* anc, int32_t sink,
+                                  int32_t window, void* out, void* work, size_t work_bytes, void* stream) {
+    cas_status st;
+    PagedAttnArgs a{};
+    if (!q || !out || sink < 0 || window < 0) return CAS_ERR_ARG;
+    if (!paged_batch(cache, H, true, &a.p, &st)) return st;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(work) || ((uintptr_t)anc & 7)) return CAS_ERR_ARG;
+    const PagedPlan plan = paged_plan(a.p, H, cache->max_rows ? cache->max_rows : a.p.N);
+    if (plan.work && (!work || work_bytes < plan.work)) return CAS_ERR_ARG;
+    a.q = (const uint16_t*)q;
+    a.anc = anc;
+    a.out = (uint16_t*)out;
+    a.H = H;
+    // (no sequence has as many slots: the kernels' sums of them stay in 32 bits)
+    a.window = window < PAGED_MAX_WINDOW ? window : PAGED_MAX_WINDOW;
+    a.sink = !window ? 0 : sink < PAGED_MAX_WINDOW ? sink : PAGED_MAX_WINDOW;
+    a.part_o = (float*)work;
+    return launch_attention_paged(a, plan, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
+}
+
+// ---- log probabilities
+
+static constexpr int LOGP_MAX_V = 1 << 20, LOGP_MAX_K = 32;
+static bool logprobs_shape(int32_t n, int32_t V, int32_t K) {
+    return n >= 1 && V >= 1 && V <= LOGP_MAX_V && K >= 0 && K <= LOGP_MAX_K && (int64_t)n * ((V + 8191) / 8192) < 1ll << 31;
+}
+
+size_t cas_op_logprobs_work_bytes(int32_t n, int32_t V, int32_t K) {
+    return logprobs_shape(n, V, K) ? logprob_work_bytes(n, V, K) : 0;
+}
+
+cas_status cas_op_logprobs(int32_t ltype, const void* logits, int64_t ld, int32_t n, int32_t V, float scale,
+                           const int32_t* tokens, int32_t m, float* logp, float* entropy, int32_t K, int32_t* top_ids,
+                           float* top_logp, void* work, size_t work_bytes, void* stream) {
+    if (ltype != CAS_W_F32 && ltype != CAS_W_BF16) return CAS_ERR_UNSUPPORTED;
+    if (!logits || !work || !logprobs_shape(n, V, K) || ld < V || m < 0) return CAS_ERR_ARG;
+    if ((m && (!tokens || !logp)) || (K && (!top_ids || !top_logp))) return CAS_ERR_ARG;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return CAS_ERR_ARG;
+    if ((uintptr_t)logits & (ltype == CAS_W_F32 ? 3 : 1)) return CAS_ERR_ARG;
+    if (((uintptr_t)tokens | (uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)top_ids | (uintptr_t)top_logp) & 3) return CAS_ERR_ARG;
+    if (!aligned16(work) || work_bytes < logprob_work_bytes(n, V, K)) return CAS_ERR_ARG;
+    LogprobArgs a{};
+    a.x = logits;
+    a.ld = (size_t)ld;
+    a.bf16 = ltype == CAS_W_BF16;
+    a.n = n;
+    a.V = V;
+    a.scale = scale;
+    a.tokens = tokens;
+    a.m = m;
+    a.K = K;
+    a.logp = logp;
+    a.entropy = entropy;
+    a.ids = top_ids;
+    a.best = top_logp;
+    a.work = (float*)work;
+    return launch_logprobs(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
 }
 
 cas_status cas_op_copy(void* dst, const void* src, size_t bytes, void* stream) {
