@@ -43,6 +43,12 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& p, int b, bool t
     return s;
 }
 
+// A page number: the same for the whole wave, by the scalar unit.
+__device__ __forceinline__ int paged_page(const PagedBatch& p, int b, int tile) {
+    typedef const __attribute__((address_space(4))) int* at;
+    return ((at)(p.table + (size_t)b * p.table_len))[tile >> p.tshift];
+}
+
 // ---------------------------------------------------------------- append
 
 // One workgroup = one tile (32 slots) that new rows fall into, for one kv head
@@ -116,7 +122,7 @@ template <int HD> __global__ void __launch_bounds__(PAPP_THREADS) k_paged_append
         }
         return;
     }
-    const int pid = p.table[(size_t)b * p.table_len + (tile >> p.tshift)];
+    const int pid = paged_page(p, b, tile);
     if ((uint32_t)pid >= (uint32_t)p.n_pages) return;
     const int h = blockIdx.y;
     uint16_t* kt = p.pages + ((((size_t)pid * 2 * p.Hkv + h) << p.tshift) + (tile & ((1 << p.tshift) - 1))) * (32 * HD);
@@ -278,12 +284,17 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         const uint64_t past = __ballot(before + n > item);
         if (past) {
             const int l = __builtin_ctzll(past);
-            r.s = paged_seq(p, b0 + l, tree);
-            r.s.T = __shfl(q.s.T, l);
-            r.ns = __builtin_amdgcn_readlane(ns, l);
-            r.nq = __builtin_amdgcn_readlane(q.nq, l);
-            r.local = item - before - __builtin_amdgcn_readlane(n - n_own, l);
-            r.part = parts + __builtin_amdgcn_readlane(np - np_own, l);
+            auto of = [&](int x) { return (int)__builtin_amdgcn_readlane(x, l); };
+            r.s.b = b0 + l;
+            r.s.row0 = of(q.s.row0);
+            r.s.T = of(q.s.T);
+            r.s.Lc = of(q.s.Lc);
+            r.s.first = of(q.s.first);
+            r.s.fits = of(q.s.fits);
+            r.ns = of(ns);
+            r.nq = of(q.nq);
+            r.local = item - before - of(n - n_own);
+            r.part = parts + of(np - np_own);
             r.found = true;
             return r;
         }
@@ -358,13 +369,12 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
         const PagedRange rg(s, t0, t1, tree, a.sink, a.window);
         const int lo = (int)((int64_t)rg.n_log * split / sh.ns), n = (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo;
         const int w0 = lo + n * wave / W, w1 = lo + n * (wave + 1) / W;
-        const int* table = p.table + (size_t)s.b * p.table_len;
         const size_t vofs = ((size_t)p.Hkv << p.tshift) * (32 * HD);
         const int tmask = (1 << p.tshift) - 1;
         auto load = [&](int lt) {
             PagedTile<HD> t;
             const int tile = rg.phys(lt);
-            int pid = table[tile >> p.tshift];
+            int pid = paged_page(p, s.b, tile);
             t.ok = (uint32_t)pid < (uint32_t)p.n_pages;
             pid = t.ok ? pid : 0;
             const uint16_t* k = p.pages + ((((size_t)pid * 2 * p.Hkv + kvh) << p.tshift) + (tile & tmask)) * (32 * HD);
@@ -453,6 +463,168 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
     }
 }
 
+// ---------------------------------------------------------------- attention: many rows
+
+// Workgroup = (share of a unit of 128 packed rows, kv head): four waves of two
+// 16-row query tiles each.  The share's key tiles pass through LDS in a ring of
+// four, keys one tile ahead of the values, with direct-to-LDS loads (the
+// fragments lie in memory as the MFMA reads them: no swizzle, no conflict) that
+// are issued three tiles ahead; one barrier per tile.  attn_step issues the next
+// tile's scores under this one's exponentials.
+static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
+
+template <int HD>
+__global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedAttnArgs a, float c) {
+    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, JT = PROWS_JT, R = PROWS_R, D = PROWS_D, AHEAD = D - 1;
+    constexpr int LP = NDT / PROWS_WAVES;  // a wave's loads of a tile's keys, and of its values
+    __shared__ i32x4 sk[D * NDT * 64], sv[D * NDT * 64];
+    const PagedBatch& p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4, G = a.G;
+    const int kvh = blockIdx.x % p.Hkv;
+    const PagedShare sh = paged_share<false>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    if (!sh.found) return;
+    const PagedSeq& s = sh.s;
+    const bool tree = a.anc != nullptr;
+    // (the last rows see the most slots: their shares start first)
+    const int qt = sh.nq - 1 - sh.local % sh.nq, split = sh.local / sh.nq;
+    auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
+    const int rows = s.T * G, p0 = qt * R, w0 = p0 + wave * 16 * JT;
+    const bool live = w0 < rows && s.fits;
+
+    AttnState<HD> st[JT];
+    i32x4 Q[JT][UD];
+    int tok[JT];
+    uint64_t an[JT][2];
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        st[j].clear();
+        const int x = min(w0 + 16 * j + r, rows - 1);
+        tok[j] = token(x);
+        const size_t row = (size_t)(s.row0 + tok[j]);
+        const uint16_t* q = a.q + (row * a.H + kvh * G + (x - tok[j] * G)) * HD + g * DG;
+#pragma unroll
+        for (int u = 0; u < UD; ++u) Q[j][u] = *(const i32x4*)(q + u * 8);
+        an[j][0] = tree ? a.anc[2 * row] : 0;
+        an[j][1] = tree ? a.anc[2 * row + 1] : 0;
+    }
+    const PagedRange rg(s, token(p0), token(min(p0 + R, rows) - 1) + 1, tree, a.sink, a.window);
+    // the wave's own rows
+    const PagedRange wr(s, token(min(w0, rows - 1)), token(min(w0 + 16 * JT, rows) - 1) + 1, tree, a.sink, a.window);
+    const int w_end = wr.pt0 + wr.n_log - wr.st;
+    auto sees = [&](int tile) { return live && tile < w_end && (tile < wr.st || tile >= wr.pt0); };
+    const int lo = s.fits ? (int)((int64_t)rg.n_log * split / sh.ns) : 0;
+    const int n = s.fits ? (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo : 0;
+    if (n > 0) {
+        const size_t vofs = ((size_t)p.Hkv << p.tshift) * (64 * HD);
+        const int tmask = (1 << p.tshift) - 1;
+        uint32_t bad = 0;  // of the last 32 tiles' pages, by tile
+        auto tile_at = [&](int i) { return rg.phys(lo + min(i, n - 1)); };
+        auto page_at = [&](int i) { return paged_page(p, s.b, tile_at(i)); };
+        auto base_of = [&](int i, int pid) {
+            const bool ok = (uint32_t)pid < (uint32_t)p.n_pages;
+            bad = (bad & ~(1u << (i & 31))) | (ok ? 0u : 1u << (i & 31));
+            const size_t at = ((((size_t)(ok ? pid : 0) * 2 * p.Hkv + kvh) << p.tshift) + (tile_at(i) & tmask)) * (64 * HD);
+            return (const char*)p.pages + at + wave * LP * 1024;
+        };
+        const uint32_t k_lds = lds_addr(sk) + wave * LP * 1024, v_lds = lds_addr(sv) + wave * LP * 1024;
+        auto load = [&](const char* base, uint32_t lds, int i) {
+#pragma unroll
+            for (int l = 0; l < LP; ++l) lds_load16(base + l * 1024, lane * 16, lds + (i % D) * (NDT * 1024) + l * 1024);
+        };
+        const char* next_v;  // the values of the tile whose keys were loaded last
+        {
+            int pid[AHEAD + 1];
+#pragma unroll
+            for (int i = 0; i <= AHEAD; ++i) pid[i] = page_at(i);
+            const char* b = base_of(0, pid[0]);
+            load(b, k_lds, 0);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const char* b1 = base_of(i + 1, pid[i + 1]);
+                load(b1, k_lds, i + 1);
+                load(b + vofs, v_lds, i);
+                b = b1;
+            }
+            next_v = b + vofs;
+        }
+        int pid = page_at(AHEAD + 1);
+        f32x4 S[JT][2], N[JT][2];
+        auto scores = [&](f32x4 (&x)[JT][2], int i) {
+            const i32x4* k = sk + (i % D) * (NDT * 64) + lane;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int u = 0; u < UD; ++u) {
+                    const i32x4 f = k[(h * UD + u) * 64];
+#pragma unroll
+                    for (int j = 0; j < JT; ++j)
+                        x[j][h] = mfma_step<ET_BF16>(f, Q[j][u], u ? x[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
+                }
+        };
+        stage_wait<2 * LP * AHEAD>();
+        scores(S, 0);
+        mfma_result_pad();
+        for (int i = 0; i < n; ++i) {
+            stage_wait<2 * LP * (AHEAD - 1)>();  // keys of i + 1, values of i; what step i - 1 used is free
+            {
+                const char* b = base_of(i + 1 + AHEAD, pid);
+                load(b, k_lds, i + 1 + AHEAD);
+                load(next_v, v_lds, i + AHEAD);
+                next_v = b + vofs;
+                pid = page_at(i + 2 + AHEAD);
+            }
+            const int tile = tile_at(i);
+            const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
+            auto V = [&](int m, i32x4 (&f)[2]) {
+                f[0] = v[2 * m * 64];
+                f[1] = v[(2 * m + 1) * 64];
+            };
+            uint32_t vm[JT];
+            if (__builtin_expect(live && wr.whole(tile) && !((bad >> (i & 31)) & 1u), 1)) {
+                attn_step<HD, JT, false, false>(st, S, c, V, vm, [&] { scores(N, i + 1); });
+            } else {
+                if (sees(tile)) {
+                    if ((bad >> (i & 31)) & 1u) {
+#pragma unroll
+                        for (int j = 0; j < JT; ++j) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+                    }
+#pragma unroll
+                    for (int j = 0; j < JT; ++j)
+                        vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+                    attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
+                    mfma_result_pad();
+                }
+                scores(N, i + 1);
+            }
+            mfma_result_pad();
+#pragma unroll
+            for (int j = 0; j < JT; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) S[j][h] = N[j][h];
+        }
+        stage_wait<0>();  // (no load outlives the workgroup's LDS)
+    }
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        const int x = w0 + 16 * j + r;
+        if (x >= rows) continue;
+        const float L = s.fits ? st[j].l[0] : NAN;
+        if (sh.ns == 1) {
+            const float inv = L != 0.f ? 1.f / L : 0.f;  // no slot seen: 0 (a NaN sum stays one)
+            uint16_t* o = a.out + ((size_t)(s.row0 + tok[j]) * a.H + kvh * G + (x - tok[j] * G)) * HD + 4 * g;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+                st4(o, 16 * dt, st[j].O[dt][0] * inv, st[j].O[dt][1] * inv, st[j].O[dt][2] * inv, st[j].O[dt][3] * inv);
+        } else {
+            const size_t at = ((size_t)(sh.part + split * sh.nq + qt) * p.Hkv + kvh) * R + x - p0;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) *(f32x4*)(a.part_o + at * HD + 16 * dt + 4 * g) = st[j].O[dt];
+            if (g == 0) *(float2*)(a.part_ml + at * 2) = make_float2(st[j].m * c, L);
+        }
+    }
+}
+
 // The join of the shares of split units: hd / 4 threads per row, NS of them
 // taking every NS-th share, then through LDS.
 static constexpr int PMERGE_THREADS = 256, PMERGE_NS = 4;
@@ -504,16 +676,15 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
     }
 }
 
-// Query tiles per workgroup (16-row tiles), and the shares aimed at.
-static constexpr int PAGED_SHARES = 256;  // workgroups of the whole launch: one per CU
-static constexpr int PAGED_LEAST = 16;    // tiles of a share
+// Packed rows of a unit, the shares aimed at and the least tiles of one.
+static constexpr int PAGED_CUS = 256, PAGED_LEAST = 16;
 
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     PagedPlan q;
-    const int G = H / p.Hkv;
-    q.R = (int64_t)std::min(max_rows, p.N) * G > 16 ? 32 : 16;
-    q.units = (int)(((int64_t)p.N * G) / q.R) + p.B;
-    q.target = (PAGED_SHARES + p.Hkv - 1) / p.Hkv;
+    const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
+    q.R = most <= 16 ? 16 : most <= 32 ? 32 : PROWS_R;
+    q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
+    q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
     q.least = PAGED_LEAST;
     if ((p.cap >> 5) <= q.least) q.target = 0;  // no sequence can be split
     q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
@@ -523,8 +694,9 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
 template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const PagedPlan& q, float c, hipStream_t s) {
     const PagedBatch& p = a.p;
     const dim3 grid((unsigned)(q.units + q.target) * p.Hkv);
-    hipError_t e = q.R == 16 ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
-                             : launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c);
+    hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
+                   : q.R == 32 ? launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c)
+                               : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);
     if (e != hipSuccess || q.target == 0) return e;
     constexpr int NR = PMERGE_THREADS / (HD / 4) / PMERGE_NS;
     const unsigned units = (unsigned)std::min(q.units, q.target);
