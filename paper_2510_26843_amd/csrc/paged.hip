@@ -562,46 +562,60 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
                         x[j][h] = mfma_step<ET_BF16>(f, Q[j][u], u ? x[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
         };
-        stage_wait<2 * LP * AHEAD>();
-        scores(S, 0);
-        mfma_result_pad();
-        for (int i = 0; i < n; ++i) {
-            stage_wait<2 * LP * (AHEAD - 1)>();  // keys of i + 1, values of i; what step i - 1 used is free
-            {
-                const char* b = base_of(i + 1 + AHEAD, pid);
-                load(b, k_lds, i + 1 + AHEAD);
-                load(next_v, v_lds, i + AHEAD);
-                next_v = b + vofs;
-                pid = page_at(i + 2 + AHEAD);
-            }
-            const int tile = tile_at(i);
+        // keys of tile i + 1 and values of i are there, what step i - 1 used is free
+        auto advance = [&](int i) {
+            stage_wait<2 * LP * (AHEAD - 1)>();
+            const char* b = base_of(i + 1 + AHEAD, pid);
+            load(b, k_lds, i + 1 + AHEAD);
+            load(next_v, v_lds, i + AHEAD);
+            next_v = b + vofs;
+            pid = page_at(i + 2 + AHEAD);
+        };
+        auto values = [&](int i) {
             const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
-            auto V = [&](int m, i32x4 (&f)[2]) {
+            return [v](int m, i32x4 (&f)[2]) {
                 f[0] = v[2 * m * 64];
                 f[1] = v[(2 * m + 1) * 64];
             };
-            uint32_t vm[JT];
-            if (__builtin_expect(live && wr.whole(tile) && !((bad >> (i & 31)) & 1u), 1)) {
-                attn_step<HD, JT, false, false>(st, S, c, V, vm, [&] { scores(N, i + 1); });
-            } else {
-                if (sees(tile)) {
-                    if ((bad >> (i & 31)) & 1u) {
+        };
+        // (the queries are here: no wait for them, which would be one for the loads in flight, in the loops)
 #pragma unroll
-                        for (int j = 0; j < JT; ++j) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
-                    }
+        for (int j = 0; j < JT; ++j)
 #pragma unroll
-                    for (int j = 0; j < JT; ++j)
-                        vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-                    attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
-                    mfma_result_pad();
-                }
-                scores(N, i + 1);
+            for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
+        stage_wait<2 * LP * AHEAD>();
+        scores(S, 0);
+        mfma_result_pad();
+        auto plain = [&](int i) {  // tile i: whole for every row of the workgroup, its page in the pool
+            return rg.whole(tile_at(i)) && !((bad >> (i & 31)) & 1u);
+        };
+        uint32_t vm[JT];
+        for (int i = 0; i < n;) {
+            // two tiles a turn, their scores in S and N
+            while (i + 1 < n && plain(i) && plain(i + 1)) {
+                advance(i);
+                attn_step<HD, JT, false, false>(st, S, c, values(i), vm, [&] { scores(N, i + 1); });
+                advance(i + 1);
+                attn_step<HD, JT, false, false>(st, N, c, values(i + 1), vm, [&] { scores(S, i + 2); });
+                i += 2;
             }
             mfma_result_pad();
+            if (i >= n) break;
+            advance(i);
+            const int tile = tile_at(i);
+            if (sees(tile)) {
+                const bool ok = !((bad >> (i & 31)) & 1u);
 #pragma unroll
-            for (int j = 0; j < JT; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) S[j][h] = N[j][h];
+                for (int j = 0; j < JT; ++j) {
+                    vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+                    if (!ok) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+                }
+                attn_step<HD, JT, true, true>(st, S, c, values(i), vm, [] {});
+                mfma_result_pad();
+            }
+            ++i;
+            scores(S, i);
+            mfma_result_pad();
         }
         stage_wait<0>();  // (no load outlives the workgroup's LDS)
     }
