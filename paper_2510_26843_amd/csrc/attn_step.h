@@ -49,6 +49,19 @@ __device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
     return f;
 }
 
+// Takes a row's reference score to its largest one, where that moves it (mt: a
+// lane's largest of a tile; other rows' scores do not move it).
+template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st, float mt, float c);
+// The probabilities of a tile's scores (mc: the scaled reference), as the B operand of P V.
+__device__ __forceinline__ void attn_probs(i32x4& P, const f32x4 (&S)[2], float mc, float c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1)], c, -mc));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1) + 1], c, -mc));
+        P[i] = (int)pack_bf(p0, p1);
+    }
+}
+
 // One key tile: S are the scores of its 32 slots, V(m, f) gives the value
 // fragments of d tiles 2m and 2m + 1.  next() computes the next tile's scores:
 // its MFMA run while this one's probabilities and values are converted.
@@ -61,6 +74,16 @@ __device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
 // row's own scores only: what a row gives does not hang on its neighbours.  The
 // sum of the (rounded) probabilities is one more row of the PV product.
 static constexpr float ATTN_SLACK = 8.f;
+template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st, float mt, float c) {
+    const float mr = pair_max32(pair_max16(mt));
+    const float mn = mr > st.top ? mr : st.m;
+    const float f = __builtin_amdgcn_exp2f((st.m - mn) * c);
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) st.O[dt] *= f;
+    st.m = mn;
+    st.top = mn + ATTN_SLACK / c;
+}
 template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
 __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
                                          const uint32_t (&vm)[JT], NF next) {

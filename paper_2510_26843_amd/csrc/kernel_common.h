@@ -136,8 +136,10 @@ __device__ __forceinline__ f32x4 attn_merge_row(const AttnArgs& a, int S, size_t
 // compiler, which cannot tell the ring's stages apart, would wait for every
 // load in flight before each LDS read; stage_wait() below is the wait.  (No
 // register is written; s_nop: the wait state between m0 and its use.)
-__device__ __forceinline__ void lds_load16(const char* base, uint32_t voff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds)
+// OFS: bytes further on, in memory and in LDS.
+template <int OFS = 0> __device__ __forceinline__ void lds_load16(const char* base, uint32_t voff, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(voff), "s"(base),
+                 "s"(lds), "n"(OFS)
                  : "memory");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {

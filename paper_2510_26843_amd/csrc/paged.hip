@@ -471,11 +471,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 // fragments lie in memory as the MFMA reads them: no swizzle, no conflict) that
 // are issued three tiles ahead; one barrier per tile.  attn_step issues the next
 // tile's scores under this one's exponentials.
-static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
+static constexpr int PROWS_WAVES = 4, PROWS_D = 4;
 
-template <int HD>
-__global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedAttnArgs a, float c) {
-    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, JT = PROWS_JT, R = PROWS_R, D = PROWS_D, AHEAD = D - 1;
+template <int HD, int JT>
+__global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows(const PagedAttnArgs a, float c) {
+    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, R = 16 * JT * PROWS_WAVES, D = PROWS_D;
     constexpr int LP = NDT / PROWS_WAVES;  // a wave's loads of a tile's keys, and of its values
     __shared__ i32x4 sk[D * NDT * 64], sv[D * NDT * 64];
     const PagedBatch& p = a.p;
@@ -516,39 +516,43 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
     const int lo = s.fits ? (int)((int64_t)rg.n_log * split / sh.ns) : 0;
     const int n = s.fits ? (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo : 0;
     if (n > 0) {
-        const size_t vofs = ((size_t)p.Hkv << p.tshift) * (64 * HD);
-        const int tmask = (1 << p.tshift) - 1;
+        // A tile's keys are tile (pid 2 Hkv + kvh) 2^tshift + (tile mod 2^tshift) of the
+        // pool, its values Hkv 2^tshift tiles on.
+        const uint32_t vtiles = (uint32_t)p.Hkv << p.tshift, tmask = (1u << p.tshift) - 1;
+        const char* pool = (const char*)p.pages + wave * LP * 1024;
         uint32_t bad = 0;  // of the last 32 tiles' pages, by tile
         auto tile_at = [&](int i) { return rg.phys(lo + min(i, n - 1)); };
         auto page_at = [&](int i) { return paged_page(p, s.b, tile_at(i)); };
-        auto base_of = [&](int i, int pid) {
+        auto place = [&](int i, int pid) {  // of tile i's keys, in tiles
             const bool ok = (uint32_t)pid < (uint32_t)p.n_pages;
             bad = (bad & ~(1u << (i & 31))) | (ok ? 0u : 1u << (i & 31));
-            const size_t at = ((((size_t)(ok ? pid : 0) * 2 * p.Hkv + kvh) << p.tshift) + (tile_at(i) & tmask)) * (64 * HD);
-            return (const char*)p.pages + at + wave * LP * 1024;
+            return (((uint32_t)(ok ? pid : 0) * (2 * p.Hkv) + kvh) << p.tshift) + ((uint32_t)tile_at(i) & tmask);
         };
         const uint32_t k_lds = lds_addr(sk) + wave * LP * 1024, v_lds = lds_addr(sv) + wave * LP * 1024;
-        auto load = [&](const char* base, uint32_t lds, int i) {
-#pragma unroll
-            for (int l = 0; l < LP; ++l) lds_load16(base + l * 1024, lane * 16, lds + (i % D) * (NDT * 1024) + l * 1024);
+        auto load = [&](uint32_t at, uint32_t lds, int i) {
+            const char* from = pool + (size_t)at * (NDT * 1024);
+            const uint32_t to = lds + (uint32_t)(i % D) * (NDT * 1024);
+            lds_load16<0>(from, lane * 16, to);
+            if constexpr (LP > 1) lds_load16<1024>(from, lane * 16, to);
         };
-        const char* next_v;  // the values of the tile whose keys were loaded last
-        {
-            int pid[AHEAD + 1];
-#pragma unroll
-            for (int i = 0; i <= AHEAD; ++i) pid[i] = page_at(i);
-            const char* b = base_of(0, pid[0]);
-            load(b, k_lds, 0);
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const char* b1 = base_of(i + 1, pid[i + 1]);
-                load(b1, k_lds, i + 1);
-                load(b + vofs, v_lds, i);
-                b = b1;
-            }
-            next_v = b + vofs;
-        }
-        int pid = page_at(AHEAD + 1);
+        static_assert(LP <= 2, "loads of a wave");
+        // Two tiles a stage: step i (even) needs the keys of i + 1 and i + 2 and the
+        // values of i and i + 1, loaded a stage before.
+        uint32_t k2, k1 = place(0, page_at(0));  // (places of the keys of i + 2 and i + 1)
+        int pid[2] = {page_at(1), page_at(2)};
+        load(k1, k_lds, 0);
+        auto request = [&](int i) {  // the stage of step i
+            const uint32_t k0 = k1;
+            k1 = place(i + 1, pid[0]);
+            k2 = place(i + 2, pid[1]);
+            load(k1, k_lds, i + 1);
+            load(k0 + vtiles, v_lds, i);
+            load(k2, k_lds, i + 2);
+            load(k1 + vtiles, v_lds, i + 1);
+            k1 = k2;
+            pid[0] = page_at(i + 3);
+            pid[1] = page_at(i + 4);
+        };
         f32x4 S[JT][2], N[JT][2];
         auto scores = [&](f32x4 (&x)[JT][2], int i) {
             const i32x4* k = sk + (i % D) * (NDT * 64) + lane;
@@ -562,14 +566,9 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
                         x[j][h] = mfma_step<ET_BF16>(f, Q[j][u], u ? x[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
         };
-        // keys of tile i + 1 and values of i are there, what step i - 1 used is free
         auto advance = [&](int i) {
-            stage_wait<2 * LP * (AHEAD - 1)>();
-            const char* b = base_of(i + 1 + AHEAD, pid);
-            load(b, k_lds, i + 1 + AHEAD);
-            load(next_v, v_lds, i + AHEAD);
-            next_v = b + vofs;
-            pid = page_at(i + 2 + AHEAD);
+            stage_wait<0>();  // what was loaded is there, what was used is free
+            request(i + 2);
         };
         auto values = [&](int i) {
             const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
@@ -583,39 +582,105 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         for (int j = 0; j < JT; ++j)
 #pragma unroll
             for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
-        stage_wait<2 * LP * AHEAD>();
+        request(0);
+        stage_wait<4 * LP>();
         scores(S, 0);
         mfma_result_pad();
-        auto plain = [&](int i) {  // tile i: whole for every row of the workgroup, its page in the pool
-            return rg.whole(tile_at(i)) && !((bad >> (i & 31)) & 1u);
+        // A lane's largest scores of a tile.
+        auto tops = [&](float (&t)[JT], const f32x4 (&x)[JT][2]) {
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                t[j] = x[j][0][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) t[j] = fmaxf(t[j], x[j][e >> 2][e & 3]);
+            }
+        };
+        // One whole tile: attn_step with the order of its instructions laid down.
+        // The next tile's keys are read under the barrier's wake, its scores run
+        // under this one's exponentials and the reads of the values, and its largest
+        // scores are taken under the product with the values.
+        auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i) {
+            const i32x4* k = sk + ((i + 1) % D) * (NDT * 64) + lane;
+            const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
+            i32x4 kf[NDT], vf[NDT];
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) kf[f] = k[f * 64];
+            bool grow = false;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) grow = grow || t[j] > st[j].top;
+            if (__any(grow)) {
+                mfma_result_pad();
+#pragma unroll
+                for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
+            }
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) vf[f] = v[f * 64];
+#pragma unroll
+            for (int f = 0; f < NDT; ++f)
+#pragma unroll
+                for (int j = 0; j < JT; ++j)
+                    y[j][f / UD] = mfma_step<ET_BF16>(kf[f], Q[j][f % UD], f % UD ? y[j][f / UD] : f32x4{0.f, 0.f, 0.f, 0.f});
+            i32x4 P[JT];
+#pragma unroll
+            for (int j = 0; j < JT; ++j) attn_probs(P[j], x[j], st[j].m * c, c);
+            const int one = 0x3f803f80;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+#pragma unroll
+            for (int f = 0; f < NDT; ++f)
+#pragma unroll
+                for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+            tops(t, y);
+            // scores: an MFMA, an exponential, its scaling and rounding; a read to every JT
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+                }
+            }
+#pragma unroll
+            for (int f = 0; f < (NDT + 1) * JT; ++f) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+            }
+        };
+        // two tiles that every row of the workgroup sees whole
+        auto plain = [&](int i) {
+            return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !((bad >> (i & 31)) & 3u);
         };
         uint32_t vm[JT];
         for (int i = 0; i < n;) {
-            // two tiles a turn, their scores in S and N
-            while (i + 1 < n && plain(i) && plain(i + 1)) {
+            float top[JT];
+            tops(top, S);
+            while (plain(i)) {
                 advance(i);
-                attn_step<HD, JT, false, false>(st, S, c, values(i), vm, [&] { scores(N, i + 1); });
-                advance(i + 1);
-                attn_step<HD, JT, false, false>(st, N, c, values(i + 1), vm, [&] { scores(S, i + 2); });
+                turn(S, N, top, i);
+                turn(N, S, top, i + 1);
                 i += 2;
             }
             mfma_result_pad();
             if (i >= n) break;
             advance(i);
-            const int tile = tile_at(i);
-            if (sees(tile)) {
-                const bool ok = !((bad >> (i & 31)) & 1u);
+#pragma unroll 1
+            for (const int end = i + 2; i < end; ++i) {
+                const int tile = tile_at(i);
+                if (i < n && sees(tile)) {
+                    const bool ok = !((bad >> (i & 31)) & 1u);
 #pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-                    if (!ok) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+                    for (int j = 0; j < JT; ++j) {
+                        vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+                        if (!ok) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+                    }
+                    attn_step<HD, JT, true, true>(st, S, c, values(i), vm, [] {});
+                    mfma_result_pad();
                 }
-                attn_step<HD, JT, true, true>(st, S, c, values(i), vm, [] {});
+                scores(S, i + 1);
                 mfma_result_pad();
             }
-            ++i;
-            scores(S, i);
-            mfma_result_pad();
         }
         stage_wait<0>();  // (no load outlives the workgroup's LDS)
     }
@@ -696,9 +761,9 @@ static constexpr int PAGED_CUS = 256, PAGED_LEAST = 16;
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     PagedPlan q;
     const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
-    q.R = most <= 16 ? 16 : most <= 32 ? 32 : PROWS_R;
+    q.R = most <= 16 ? 16 : most <= 32 ? 32 : getenv("PR") ? atoi(getenv("PR")) : 128;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
-    q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
+    q.target = (PAGED_CUS * (q.R == 128 ? 2 : 1) + p.Hkv - 1) / p.Hkv;
     q.least = PAGED_LEAST;
     if ((p.cap >> 5) <= q.least) q.target = 0;  // no sequence can be split
     q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
@@ -710,7 +775,8 @@ template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const 
     const dim3 grid((unsigned)(q.units + q.target) * p.Hkv);
     hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
                    : q.R == 32 ? launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c)
-                               : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);
+                   : q.R == 128 ? launch_checked(k_paged_rows<HD, 2>, grid, 64 * PROWS_WAVES, s, a, c)
+                                : launch_checked(k_paged_rows<HD, 4>, grid, 64 * PROWS_WAVES, s, a, c);
     if (e != hipSuccess || q.target == 0) return e;
     constexpr int NR = PMERGE_THREADS / (HD / 4) / PMERGE_NS;
     const unsigned units = (unsigned)std::min(q.units, q.target);
