@@ -46,7 +46,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& p, int b, bool t
 // A page number: the same for the whole wave, by the scalar unit.
 __device__ __forceinline__ int paged_page(const PagedBatch& p, int b, int tile) {
     typedef const __attribute__((address_space(4))) int* at;
-    return ((at)(p.table + (size_t)b * p.table_len))[tile >> p.tshift];
+    return ((at)(p.table + (size_t)b * p.table_len))[(uint32_t)tile >> p.tshift];
 }
 
 // ---------------------------------------------------------------- append
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         const uint32_t k_lds = lds_addr(sk) + wave * LP * 1024, v_lds = lds_addr(sv) + wave * LP * 1024;
         auto load = [&](uint32_t at, uint32_t lds, int i) {
             const char* from = pool + (size_t)at * (NDT * 1024);
-            const uint32_t to = lds + (uint32_t)(i % D) * (NDT * 1024);
+            const uint32_t to = lds + ((uint32_t)i % D) * (NDT * 1024);
             lds_load16<0>(from, lane * 16, to);
             if constexpr (LP > 1) lds_load16<1024>(from, lane * 16, to);
         };
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         };
         f32x4 S[JT][2], N[JT][2];
         auto scores = [&](f32x4 (&x)[JT][2], int i) {
-            const i32x4* k = sk + (i % D) * (NDT * 64) + lane;
+            const i32x4* k = sk + ((uint32_t)i % D) * (NDT * 64) + lane;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
             request(i + 2);
         };
         auto values = [&](int i) {
-            const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
+            const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
             return [v](int m, i32x4 (&f)[2]) {
                 f[0] = v[2 * m * 64];
                 f[1] = v[(2 * m + 1) * 64];
@@ -600,8 +600,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         // under this one's exponentials and the reads of the values, and its largest
         // scores are taken under the product with the values.
         auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i) {
-            const i32x4* k = sk + ((i + 1) % D) * (NDT * 64) + lane;
-            const i32x4* v = sv + (i % D) * (NDT * 64) + lane;
+            const i32x4* k = sk + ((uint32_t)(i + 1) % D) * (NDT * 64) + lane;
+            const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
             i32x4 kf[NDT], vf[NDT];
 #pragma unroll
             for (int f = 0; f < NDT; ++f) kf[f] = k[f * 64];
@@ -615,14 +615,24 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
             }
 #pragma unroll
             for (int f = 0; f < NDT; ++f) vf[f] = v[f * 64];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int f = 0; f < NDT; ++f)
+            for (int u = 0; u < UD; ++u)
 #pragma unroll
-                for (int j = 0; j < JT; ++j)
-                    y[j][f / UD] = mfma_step<ET_BF16>(kf[f], Q[j][f % UD], f % UD ? y[j][f / UD] : f32x4{0.f, 0.f, 0.f, 0.f});
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < JT; ++j)
+                        y[j][h] = mfma_step<ET_BF16>(kf[h * UD + u], Q[j][u], u ? y[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
             i32x4 P[JT];
 #pragma unroll
             for (int j = 0; j < JT; ++j) attn_probs(P[j], x[j], st[j].m * c, c);
+#pragma unroll
+            for (int f = 0; f < NDT * JT; ++f) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             const int one = 0x3f803f80;
 #pragma unroll
             for (int j = 0; j < JT; ++j) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
@@ -631,22 +641,12 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
 #pragma unroll
                 for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
             tops(t, y);
-            // scores: an MFMA, an exponential, its scaling and rounding; a read to every JT
-#pragma unroll
-            for (int f = 0; f < NDT; ++f) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-#pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
-                }
-            }
 #pragma unroll
             for (int f = 0; f < (NDT + 1) * JT; ++f) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
         // two tiles that every row of the workgroup sees whole
         auto plain = [&](int i) {
