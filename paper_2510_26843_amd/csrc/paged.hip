@@ -550,6 +550,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
             load(k2, k_lds, i + 2);
             load(k1 + vtiles, v_lds, i + 1);
             k1 = k2;
+        };
+        auto look_up = [&](int i) {  // the pages of the stage after step i's
             pid[0] = page_at(i + 3);
             pid[1] = page_at(i + 4);
         };
@@ -583,6 +585,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
 #pragma unroll
             for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
         request(0);
+        look_up(0);
         stage_wait<4 * LP>();
         scores(S, 0);
         mfma_result_pad();
@@ -599,7 +602,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         // The next tile's keys are read under the barrier's wake, its scores run
         // under this one's exponentials and the reads of the values, and its largest
         // scores are taken under the product with the values.
-        auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i) {
+        auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i, bool last) {
             const i32x4* k = sk + ((uint32_t)(i + 1) % D) * (NDT * 64) + lane;
             const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
             i32x4 kf[NDT], vf[NDT];
@@ -632,6 +635,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
                 __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
             }
+            // (here: a scalar load in flight makes every LDS read's wait one for all of them)
+            if (last) look_up(i + 1);
             __builtin_amdgcn_sched_barrier(0);
             const int one = 0x3f803f80;
 #pragma unroll
@@ -658,8 +663,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
             tops(top, S);
             while (plain(i)) {
                 advance(i);
-                turn(S, N, top, i);
-                turn(N, S, top, i + 1);
+                turn(S, N, top, i, false);
+                turn(N, S, top, i + 1, true);
                 i += 2;
             }
             mfma_result_pad();
@@ -681,6 +686,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
                 scores(S, i + 1);
                 mfma_result_pad();
             }
+            look_up(i);
         }
         stage_wait<0>();  // (no load outlives the workgroup's LDS)
     }
