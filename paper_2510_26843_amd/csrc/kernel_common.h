@@ -136,11 +136,21 @@ __device__ __forceinline__ f32x4 attn_merge_row(const AttnArgs& a, int S, size_t
 // compiler, which cannot tell the ring's stages apart, would wait for every
 // load in flight before each LDS read; stage_wait() below is the wait.  (No
 // register is written; s_nop: the wait state between m0 and its use.)
-// OFS: bytes further on, in memory and in LDS.
-template <int OFS = 0> __device__ __forceinline__ void lds_load16(const char* base, uint32_t voff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(voff), "s"(base),
-                 "s"(lds), "n"(OFS)
+__device__ __forceinline__ void lds_load16(const char* base, uint32_t voff, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds)
                  : "memory");
+}
+// NF KB in one piece, by one wave: NF such loads, 1 KB apart in memory and LDS (an
+// instruction's offset counts for both and ends at 4 KB).
+template <int NF> __device__ __forceinline__ void lds_load_tile(const char* base, uint32_t voff, uint32_t lds) {
+    static_assert(NF % 4 == 0, "four loads at a time");
+#pragma unroll
+    for (int f = 0; f < NF; f += 4)
+        asm volatile(
+            "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024\n\t"
+            "global_load_lds_dwordx4 %0, %1 offset:2048\n\tglobal_load_lds_dwordx4 %0, %1 offset:3072" ::"v"(voff),
+            "s"(base + f * 1024), "s"(lds + f * 1024)
+            : "memory");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;

@@ -476,7 +476,6 @@ static constexpr int PROWS_WAVES = 4, PROWS_D = 4;
 template <int HD, int JT>
 __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows(const PagedAttnArgs a, float c) {
     constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, R = 16 * JT * PROWS_WAVES, D = PROWS_D;
-    constexpr int LP = NDT / PROWS_WAVES;  // a wave's loads of a tile's keys, and of its values
     __shared__ i32x4 sk[D * NDT * 64], sv[D * NDT * 64];
     const PagedBatch& p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -486,8 +485,11 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
     if (!sh.found) return;
     const PagedSeq& s = sh.s;
     const bool tree = a.anc != nullptr;
-    // (the last rows see the most slots: their shares start first)
-    const int qt = sh.nq - 1 - sh.local % sh.nq, split = sh.local / sh.nq;
+    // The last rows see the most slots: their shares start first.  Where all of a
+    // sequence's run at once, two to a CU, the second half goes the other way, so
+    // that a long one shares its CU with a short one.
+    const int split = sh.local / sh.nq, at = sh.local - split * sh.nq, half = (sh.nq + 1) / 2;
+    const int qt = a.fold && at >= half ? at - half : sh.nq - 1 - at;
     auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
     const int rows = s.T * G, p0 = qt * R, w0 = p0 + wave * 16 * JT;
     const bool live = w0 < rows && s.fits;
@@ -516,45 +518,30 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
     const int lo = s.fits ? (int)((int64_t)rg.n_log * split / sh.ns) : 0;
     const int n = s.fits ? (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo : 0;
     if (n > 0) {
-        // A tile's keys are tile (pid 2 Hkv + kvh) 2^tshift + (tile mod 2^tshift) of the
-        // pool, its values Hkv 2^tshift tiles on.
-        const uint32_t vtiles = (uint32_t)p.Hkv << p.tshift, tmask = (1u << p.tshift) - 1;
-        const char* pool = (const char*)p.pages + wave * LP * 1024;
-        uint32_t bad = 0;  // of the last 32 tiles' pages, by tile
+        // Two tiles a stage: the stage of step i (even) has the keys of i + 1 and i + 2
+        // and the values of i and i + 1, a tile for each wave to load, one stage
+        // ahead of its use.  A tile's keys are tile (pid 2 Hkv + kvh) 2^tshift + (tile
+        // mod 2^tshift) of the pool, its values Hkv 2^tshift tiles on.
+        const uint32_t tmask = (1u << p.tshift) - 1, head = (uint32_t)kvh + (wave & 1 ? (uint32_t)p.Hkv : 0u);
         auto tile_at = [&](int i) { return rg.phys(lo + min(i, n - 1)); };
-        auto page_at = [&](int i) { return paged_page(p, s.b, tile_at(i)); };
-        auto place = [&](int i, int pid) {  // of tile i's keys, in tiles
-            const bool ok = (uint32_t)pid < (uint32_t)p.n_pages;
-            bad = (bad & ~(1u << (i & 31))) | (ok ? 0u : 1u << (i & 31));
-            return (((uint32_t)(ok ? pid : 0) * (2 * p.Hkv) + kvh) << p.tshift) + ((uint32_t)tile_at(i) & tmask);
+        const int ahead = (wave & 1 ? 0 : 1) + (wave >> 1);  // the wave's tile of a stage: i + ahead
+        const uint32_t ring = (wave & 1 ? lds_addr(sv) : lds_addr(sk));
+        int mine = tile_at(ahead), pid = paged_page(p, s.b, mine);
+        auto load = [&](int i) {  // tile i, by this wave
+            const uint32_t pg = (uint32_t)pid < (uint32_t)p.n_pages ? (uint32_t)pid : 0u;
+            const uint32_t at = ((pg * (2 * p.Hkv) + head) << p.tshift) + ((uint32_t)mine & tmask);
+            lds_load_tile<NDT>((const char*)p.pages + (size_t)at * (NDT * 1024), lane * 16,
+                               ring + ((uint32_t)i % D) * (NDT * 1024));
         };
-        const uint32_t k_lds = lds_addr(sk) + wave * LP * 1024, v_lds = lds_addr(sv) + wave * LP * 1024;
-        auto load = [&](uint32_t at, uint32_t lds, int i) {
-            const char* from = pool + (size_t)at * (NDT * 1024);
-            const uint32_t to = lds + ((uint32_t)i % D) * (NDT * 1024);
-            lds_load16<0>(from, lane * 16, to);
-            if constexpr (LP > 1) lds_load16<1024>(from, lane * 16, to);
+        auto look_up = [&](int i) {  // the page of the wave's next tile, after step i's stage
+            mine = tile_at(i + 2 + ahead);
+            pid = paged_page(p, s.b, mine);
         };
-        static_assert(LP <= 2, "loads of a wave");
-        // Two tiles a stage: step i (even) needs the keys of i + 1 and i + 2 and the
-        // values of i and i + 1, loaded a stage before.
-        uint32_t k2, k1 = place(0, page_at(0));  // (places of the keys of i + 2 and i + 1)
-        int pid[2] = {page_at(1), page_at(2)};
-        load(k1, k_lds, 0);
-        auto request = [&](int i) {  // the stage of step i
-            const uint32_t k0 = k1;
-            k1 = place(i + 1, pid[0]);
-            k2 = place(i + 2, pid[1]);
-            load(k1, k_lds, i + 1);
-            load(k0 + vtiles, v_lds, i);
-            load(k2, k_lds, i + 2);
-            load(k1 + vtiles, v_lds, i + 1);
-            k1 = k2;
-        };
-        auto look_up = [&](int i) {  // the pages of the stage after step i's
-            pid[0] = page_at(i + 3);
-            pid[1] = page_at(i + 4);
-        };
+        // whether a page of the share lies outside the pool: then every tile is looked at
+        bool strange = false;
+        for (int i = lane; i < n; i += 64)
+            strange = strange || (uint32_t)p.table[(size_t)s.b * p.table_len + (rg.phys(lo + i) >> p.tshift)] >= (uint32_t)p.n_pages;
+        strange = __any(strange);
         f32x4 S[JT][2], N[JT][2];
         auto scores = [&](f32x4 (&x)[JT][2], int i) {
             const i32x4* k = sk + ((uint32_t)i % D) * (NDT * 64) + lane;
@@ -570,7 +557,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         };
         auto advance = [&](int i) {
             stage_wait<0>();  // what was loaded is there, what was used is free
-            request(i + 2);
+            load(i + 2 + ahead);
         };
         auto values = [&](int i) {
             const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
@@ -584,9 +571,15 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         for (int j = 0; j < JT; ++j)
 #pragma unroll
             for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
-        request(0);
+        if (wave == 0) {  // the first keys, which no stage has
+            const int pid0 = paged_page(p, s.b, tile_at(0));
+            const uint32_t pg = (uint32_t)pid0 < (uint32_t)p.n_pages ? (uint32_t)pid0 : 0u;
+            const uint32_t at = ((pg * (2 * p.Hkv) + kvh) << p.tshift) + ((uint32_t)tile_at(0) & tmask);
+            lds_load_tile<NDT>((const char*)p.pages + (size_t)at * (NDT * 1024), lane * 16, lds_addr(sk));
+        }
+        load(ahead);
         look_up(0);
-        stage_wait<4 * LP>();
+        stage_wait<NDT>();  // (the others' loads of the stage stay in flight)
         scores(S, 0);
         mfma_result_pad();
         // A lane's largest scores of a tile.
@@ -655,7 +648,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
         };
         // two tiles that every row of the workgroup sees whole
         auto plain = [&](int i) {
-            return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !((bad >> (i & 31)) & 3u);
+            return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !strange;
         };
         uint32_t vm[JT];
         for (int i = 0; i < n;) {
@@ -674,7 +667,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
             for (const int end = i + 2; i < end; ++i) {
                 const int tile = tile_at(i);
                 if (i < n && sees(tile)) {
-                    const bool ok = !((bad >> (i & 31)) & 1u);
+                    const bool ok = !strange || (uint32_t)paged_page(p, s.b, tile) < (uint32_t)p.n_pages;
 #pragma unroll
                     for (int j = 0; j < JT; ++j) {
                         vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
@@ -798,6 +791,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q,
     a.inv_G = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.target = q.target;
     a.least = q.least;
+    a.fold = (int64_t)(q.units - p.B) * p.Hkv <= 2 * PAGED_CUS;
     a.part_ml = a.part_o + (size_t)2 * q.target * p.Hkv * q.R * p.hd;
     const float c = (1.0f / sqrtf((float)p.hd)) * 1.4426950408889634f;
     if (p.hd == 128) return paged_attn_go<128>(a, q, c, s);
