@@ -313,11 +313,6 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
 // registers that the MFMA reads.
 static constexpr int PAGED_WAVES = 8;
 
-template <int HD> struct PagedTile {
-    i32x4 k[HD / 16], v[HD / 16];  // key fragments (h2, u), value fragments dt
-    bool ok;
-};
-
 template <int HD, int JT>
 __device__ __forceinline__ void paged_scores(f32x4 (&S)[JT][2], const i32x4 (&k)[HD / 16], const i32x4 (&Q)[JT][HD / 32]) {
 #pragma unroll
@@ -369,54 +364,64 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
         const PagedRange rg(s, t0, t1, tree, a.sink, a.window);
         const int lo = (int)((int64_t)rg.n_log * split / sh.ns), n = (int)((int64_t)rg.n_log * (split + 1) / sh.ns) - lo;
         const int w0 = lo + n * wave / W, w1 = lo + n * (wave + 1) / W;
-        const size_t vofs = ((size_t)p.Hkv << p.tshift) * (32 * HD);
-        const int tmask = (1 << p.tshift) - 1;
-        auto load = [&](int lt) {
-            PagedTile<HD> t;
-            const int tile = rg.phys(lt);
-            int pid = paged_page(p, s.b, tile);
-            t.ok = (uint32_t)pid < (uint32_t)p.n_pages;
-            pid = t.ok ? pid : 0;
-            const uint16_t* k = p.pages + ((((size_t)pid * 2 * p.Hkv + kvh) << p.tshift) + (tile & tmask)) * (32 * HD);
-#pragma unroll
-            for (int i = 0; i < NDT; ++i) {
-                t.k[i] = *(const i32x4*)(k + i * 512 + lane * 8);
-                t.v[i] = *(const i32x4*)(k + vofs + i * 512 + lane * 8);
-            }
-            return t;
+        // A tile's fragments, keys and values apart: the next tile's keys are loaded
+        // once this one's scores are there, its values after the product with them.
+        const uint32_t tmask = (1u << p.tshift) - 1, vtiles = (uint32_t)p.Hkv << p.tshift;
+        i32x4 kf[NDT], vf[NDT];
+        int tile, pid;
+        uint32_t at;
+        auto look_up = [&](int lt) {
+            tile = rg.phys(lt);
+            pid = paged_page(p, s.b, tile);
         };
-        for (int lt = w0; lt < w1; ++lt) {
-            const int tile = rg.phys(lt);
-            const PagedTile<HD> t = load(lt);
-            f32x4 S[JT][2];
-            paged_scores<HD, JT>(S, t.k, Q);
-            if (!t.ok) {
+        auto load_k = [&] {
+            const uint32_t pg = (uint32_t)pid < (uint32_t)p.n_pages ? (uint32_t)pid : 0u;
+            at = ((pg * (2 * p.Hkv) + kvh) << p.tshift) + ((uint32_t)tile & tmask);
+            const uint16_t* k = p.pages + (size_t)at * (32 * HD);
 #pragma unroll
-                for (int j = 0; j < JT; ++j) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
-            }
-            auto V = [&](int m, i32x4 (&f)[2]) {
-                f[0] = t.v[2 * m];
-                f[1] = t.v[2 * m + 1];
-            };
-            uint32_t vm[JT];
-            if (rg.whole(tile)) {
+            for (int f = 0; f < NDT; ++f) kf[f] = *(const i32x4*)(k + f * 512 + lane * 8);
+        };
+        auto load_v = [&] {
+            const uint16_t* v = p.pages + (size_t)(at + vtiles) * (32 * HD);
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) vf[f] = *(const i32x4*)(v + f * 512 + lane * 8);
+        };
+        auto V = [&](int m, i32x4 (&f)[2]) {
+            f[0] = vf[2 * m];
+            f[1] = vf[2 * m + 1];
+        };
+        uint32_t vm[JT];
+        f32x4 S[JT][2];
+        if (w0 < w1) {
+            look_up(w0);
+            load_k();
+            load_v();
+        }
+        for (int lt = w0; lt < w1;) {
+            while (rg.whole(tile) && (uint32_t)pid < (uint32_t)p.n_pages) {
+                look_up(min(lt + 1, w1 - 1));
+                paged_scores<HD, JT>(S, kf, Q);
+                load_k();
                 attn_step<HD, JT, false, false>(st, S, c, V, vm, [] {});
-            } else {
-#pragma unroll
-                for (int j = 0; j < JT; ++j)
-                    vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-                bool bad = false;
-#pragma unroll
-                for (int i = 0; i < NDT; ++i)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t x = (uint32_t)t.v[i][w];
-                        bad = bad || (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-                    }
-                if (__any(bad)) attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
-                else attn_step<HD, JT, true, false>(st, S, c, V, vm, [] {});
+                load_v();
+                if (++lt >= w1) break;
             }
             mfma_result_pad();
+            if (lt >= w1) break;
+            paged_scores<HD, JT>(S, kf, Q);
+            mfma_result_pad();
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+                if ((uint32_t)pid >= (uint32_t)p.n_pages) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
+            }
+            attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
+            mfma_result_pad();
+            if (++lt < w1) {
+                look_up(lt);
+                load_k();
+                load_v();
+            }
         }
     }
 
@@ -471,11 +476,11 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 // fragments lie in memory as the MFMA reads them: no swizzle, no conflict) that
 // are issued three tiles ahead; one barrier per tile.  attn_step issues the next
 // tile's scores under this one's exponentials.
-static constexpr int PROWS_WAVES = 4, PROWS_D = 4;
+static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
 
-template <int HD, int JT>
-__global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows(const PagedAttnArgs a, float c) {
-    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, R = 16 * JT * PROWS_WAVES, D = PROWS_D;
+template <int HD>
+__global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedAttnArgs a, float c) {
+    constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, JT = PROWS_JT, R = PROWS_R, D = PROWS_D;
     __shared__ i32x4 sk[D * NDT * 64], sv[D * NDT * 64];
     const PagedBatch& p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -591,10 +596,11 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
                 for (int e = 1; e < 8; ++e) t[j] = fmaxf(t[j], x[j][e >> 2][e & 3]);
             }
         };
-        // One whole tile: attn_step with the order of its instructions laid down.
-        // The next tile's keys are read under the barrier's wake, its scores run
-        // under this one's exponentials and the reads of the values, and its largest
-        // scores are taken under the product with the values.
+        // One whole tile: attn_step with the order of its instructions laid down.  x: its
+        // scores, y: the next one's, t: a lane's largest of x, and then of y.  The
+        // keys are read first, the values under them; the next tile's scores run
+        // under this one's exponentials, its largest scores are taken under the
+        // product with the values.
         auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i, bool last) {
             const i32x4* k = sk + ((uint32_t)(i + 1) % D) * (NDT * 64) + lane;
             const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
@@ -703,54 +709,62 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, JT > 2 ? 1 : 2) k_paged_rows
     }
 }
 
-// The join of the shares of split units: hd / 4 threads per row, NS of them
-// taking every NS-th share, then through LDS.
-static constexpr int PMERGE_THREADS = 256, PMERGE_NS = 4;
+// The join of the shares of split units: hd / 4 threads per row and group; the
+// groups take a row each, or with many shares up to eight take every eighth
+// share of a row, four at a time, and join through LDS.  One large workgroup per
+// unit: most find nothing to do, and each has to look (paged_share; with eight
+// workgroups of 256 threads per unit, of which a 2048-row chunk's 512 need
+// none, this kernel took 8 us, with 64 of them 36).
+static constexpr int PMERGE_THREADS = 1024;
 template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merge(const PagedAttnArgs a, int R) {
-    constexpr int D4 = HD / 4, NG = PMERGE_THREADS / D4, NS = PMERGE_NS, NR = NG / NS;
+    constexpr int D4 = HD / 4, NG = PMERGE_THREADS / D4;
     __shared__ float2 sm_ml[NG];
     __shared__ f32x4 sm_o[NG][D4];
     const PagedBatch& p = a.p;
     const int kvh = blockIdx.x % p.Hkv, G = a.G;
     const PagedShare sh = paged_share<true>(a, R, a.inv_G, blockIdx.x / p.Hkv);
     if (!sh.found) return;
+    const int ns = sh.ns, NS = ns > 16 ? 8 : ns > 8 ? 4 : ns > 4 ? 2 : 1;
     const int gi = threadIdx.x / D4, d4 = threadIdx.x % D4 * 4, sub = gi % NS;
     const int p0 = sh.local * R, rows = min(sh.s.T * G - p0, R);
-    for (int i0 = blockIdx.y * NR; i0 < rows; i0 += gridDim.y * NR) {  // (the same for every thread)
+    for (int i0 = blockIdx.y * (NG / NS); i0 < rows; i0 += gridDim.y * (NG / NS)) {  // (the same for every thread)
         const int i = min(i0 + gi / NS, rows - 1);
         float M = -1e30f, L = 0.f;
         f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
-        for (int k0 = sub; k0 < sh.ns; k0 += 4 * NS) {
+        for (int k0 = sub; k0 < ns; k0 += 4 * NS) {
             float2 ml[4];
             f32x4 po[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int sp = min(k0 + k * NS, sh.ns - 1);
+                const int sp = min(k0 + k * NS, ns - 1);
                 const size_t o = ((size_t)(sh.part + sp * sh.nq + sh.local) * p.Hkv + kvh) * R + i;
                 ml[k] = *(const float2*)(a.part_ml + o * 2);
                 po[k] = *(const f32x4*)(a.part_o + o * HD + d4);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (k0 + k * NS < sh.ns) {
+                if (k0 + k * NS < ns) {
                     const f32x4 o[1] = {po[k]};
                     attn_merge_split<1>(acc, L, M, o, ml[k].y, ml[k].x);
                 }
         }
-        if (d4 == 0) sm_ml[gi] = make_float2(M, L);
-        sm_o[gi][d4 / 4] = acc[0];
-        __syncthreads();
+        if (NS > 1) {
+            if (d4 == 0) sm_ml[gi] = make_float2(M, L);
+            sm_o[gi][d4 / 4] = acc[0];
+            __syncthreads();
+            if (sub == 0)
+                for (int k = 1; k < NS; ++k) {
+                    const f32x4 o[1] = {sm_o[gi + k][d4 / 4]};
+                    attn_merge_split<1>(acc, L, M, o, sm_ml[gi + k].y, sm_ml[gi + k].x);
+                }
+        }
         if (sub == 0 && i0 + gi / NS < rows) {
-            for (int k = 1; k < NS; ++k) {
-                const f32x4 o[1] = {sm_o[gi + k][d4 / 4]};
-                attn_merge_split<1>(acc, L, M, o, sm_ml[gi + k].y, sm_ml[gi + k].x);
-            }
             const float inv = L != 0.f ? 1.f / L : 0.f;
             const int x = p0 + i, t = a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x;
             st4(a.out, ((size_t)(sh.s.row0 + t) * a.H + kvh * G + (x - t * G)) * HD + d4, acc[0][0] * inv,
                 acc[0][1] * inv, acc[0][2] * inv, acc[0][3] * inv);
         }
-        __syncthreads();
+        if (NS > 1) __syncthreads();
     }
 }
 
@@ -760,9 +774,9 @@ static constexpr int PAGED_CUS = 256, PAGED_LEAST = 16;
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     PagedPlan q;
     const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
-    q.R = most <= 16 ? 16 : most <= 32 ? 32 : getenv("PR") ? atoi(getenv("PR")) : 128;
+    q.R = most <= 16 ? 16 : most <= 32 ? 32 : PROWS_R;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
-    q.target = (PAGED_CUS * (q.R == 128 ? 2 : 1) + p.Hkv - 1) / p.Hkv;
+    q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
     q.least = PAGED_LEAST;
     if ((p.cap >> 5) <= q.least) q.target = 0;  // no sequence can be split
     q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
@@ -774,12 +788,12 @@ template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const 
     const dim3 grid((unsigned)(q.units + q.target) * p.Hkv);
     hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
                    : q.R == 32 ? launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c)
-                   : q.R == 128 ? launch_checked(k_paged_rows<HD, 2>, grid, 64 * PROWS_WAVES, s, a, c)
-                                : launch_checked(k_paged_rows<HD, 4>, grid, 64 * PROWS_WAVES, s, a, c);
+                               : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);
     if (e != hipSuccess || q.target == 0) return e;
-    constexpr int NR = PMERGE_THREADS / (HD / 4) / PMERGE_NS;
     const unsigned units = (unsigned)std::min(q.units, q.target);
-    return launch_checked(k_paged_merge<HD>, dim3(units * p.Hkv, q.R / NR), PMERGE_THREADS, s, a, q.R);
+    // (several per unit where a unit is 128 rows and there are few of them)
+    const unsigned y = q.R == PROWS_R ? std::max(1u, std::min(16u, 1024u / (units * p.Hkv))) : 1u;
+    return launch_checked(k_paged_merge<HD>, dim3(units * p.Hkv, y), PMERGE_THREADS, s, a, q.R);
 }
 
 hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q, hipStream_t s) {
