@@ -19,6 +19,8 @@
 
 namespace cas {
 
+typedef unsigned short uint16x2 __attribute__((ext_vector_type(2)));
+
 // ---------------------------------------------------------------- sequences
 
 struct PagedSeq {
@@ -217,6 +219,45 @@ __device__ __forceinline__ uint32_t paged_vis8(const PagedSeq& s, int t, int bas
     return bits8(0, min(sink, own) - base) | bits8(own - window - base, own + 1 - base);
 }
 
+// Inclusive sum over the lanes up to one's own, by cross-lane operands: six adds
+// (through LDS, as shuffles go, each step waits 100 cycles).
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_0(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_0(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)b), hi = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(b >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <typename V> __device__ __forceinline__ V wave_scan(V x) {
+    x += dpp_or_0<0x111, 0xf>(x);  // the row's lane - 1, - 2, - 4, - 8
+    x += dpp_or_0<0x112, 0xf>(x);
+    x += dpp_or_0<0x114, 0xf>(x);
+    x += dpp_or_0<0x118, 0xf>(x);
+    x += dpp_or_0<0x142, 0xa>(x);  // the last lane of the row before, to rows 1 and 3
+    x += dpp_or_0<0x143, 0xc>(x);  // lane 31, to rows 2 and 3
+    return x;
+}
+template <typename V> __device__ __forceinline__ V wave_total(V x) {
+    const V s = wave_scan(x);
+    if constexpr (sizeof(V) == 4) {
+        return (V)__builtin_amdgcn_readlane((int)s, 63);
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, s);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63);
+        return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 | lo);
+    }
+}
+__device__ __forceinline__ int wave_most(int x) {  // of values >= 0
+    x = max(x, dpp_or_0<0x111, 0xf>(x));
+    x = max(x, dpp_or_0<0x112, 0xf>(x));
+    x = max(x, dpp_or_0<0x114, 0xf>(x));
+    x = max(x, dpp_or_0<0x118, 0xf>(x));
+    x = max(x, dpp_or_0<0x142, 0xa>(x));
+    x = max(x, dpp_or_0<0x143, 0xc>(x));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // How the work is shared out.  A unit is (sequence, query tile of R packed
 // rows, kv head); the split rule gives a sequence of more than C tiles ns =
 // ceil(tiles / C) shares per unit, with C such that the batch has about
@@ -256,14 +297,25 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
     const Seq own = seq(lane);
     int C = 1 << 30;
     if (a.target > 0) {
-        uint64_t w = (uint64_t)own.nq * own.tiles;
+        int nq = own.nq, most = own.tiles;
+        double w = (double)own.nq * own.tiles;  // (exact)
         for (int b0 = 64; b0 < p.B; b0 += 64) {
             const Seq q = seq(b0 + lane);
-            w += (uint64_t)q.nq * q.tiles;
+            nq += q.nq;
+            most = max(most, q.tiles);
+            w += (double)q.nq * q.tiles;
         }
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor(w, o);
-        C = max(a.least, (int)min((uint64_t)1 << 30, (w + a.target - 1) / a.target));
+        nq = wave_total<int>(nq);
+        w = wave_total<double>(w);
+        most = wave_most(most);
+        auto share = [&](int n) { return max(a.least, (int)fmin(1073741824.0, ceil(w / n))); };
+        C = share(a.target);
+        // (with room left by the units: as many shares as run at once, if the longest is
+        // then no longer than two rounds of the finer shares)
+        if (nq < a.target) {
+            const int D = share(a.target - nq);
+            if (min(D, most) <= 2 * C) C = D;
+        }
     }
     PagedShare r;
     r.found = false;
@@ -273,14 +325,8 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         const int ns = max((q.tiles + C - 1) / C, 1);
         int n = MERGE ? (ns > 1 ? q.nq : 0) : q.nq * ns, np = ns > 1 ? q.nq * ns : 0;
         const int n_own = n, np_own = np;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(n, o), y = __shfl_up(np, o);
-            if (lane >= o) {
-                n += x;
-                np += y;
-            }
-        }
+        n = wave_scan(n);
+        np = wave_scan(np);
         const uint64_t past = __ballot(before + n > item);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -550,32 +596,22 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         f32x4 S[JT][2], N[JT][2];
         auto scores = [&](f32x4 (&x)[JT][2], int i) {
             const i32x4* k = sk + ((uint32_t)i % D) * (NDT * 64) + lane;
+            i32x4 kf[NDT];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int f = 0; f < NDT; ++f) kf[f] = k[f * 64];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int u = 0; u < UD; ++u) {
-                    const i32x4 f = k[(h * UD + u) * 64];
+            for (int u = 0; u < UD; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int j = 0; j < JT; ++j)
-                        x[j][h] = mfma_step<ET_BF16>(f, Q[j][u], u ? x[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
-                }
+                        x[j][h] = mfma_step<ET_BF16>(kf[h * UD + u], Q[j][u], u ? x[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
         };
         auto advance = [&](int i) {
             stage_wait<0>();  // what was loaded is there, what was used is free
-            load(i + 2 + ahead);
+            if (i + 2 + ahead < n) load(i + 2 + ahead);
         };
-        auto values = [&](int i) {
-            const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
-            return [v](int m, i32x4 (&f)[2]) {
-                f[0] = v[2 * m * 64];
-                f[1] = v[(2 * m + 1) * 64];
-            };
-        };
-        // (the queries are here: no wait for them, which would be one for the loads in flight, in the loops)
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-            for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
         if (wave == 0) {  // the first keys, which no stage has
             const int pid0 = paged_page(p, s.b, tile_at(0));
             const uint32_t pg = (uint32_t)pid0 < (uint32_t)p.n_pages ? (uint32_t)pid0 : 0u;
@@ -584,7 +620,12 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         }
         load(ahead);
         look_up(0);
-        stage_wait<NDT>();  // (the others' loads of the stage stay in flight)
+        // (the queries are here: no wait for them, which would be one for the loads in flight, in the loops)
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int u = 0; u < UD; ++u) asm volatile("" : "+v"(Q[j][u]));
+        stage_wait<0>();
         scores(S, 0);
         mfma_result_pad();
         // A lane's largest scores of a tile.
@@ -596,7 +637,31 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
                 for (int e = 1; e < 8; ++e) t[j] = fmaxf(t[j], x[j][e >> 2][e & 3]);
             }
         };
-        // One whole tile: attn_step with the order of its instructions laid down.  x: its
+        // A tile that some row of the wave does not see whole: the scores of unseen slots
+        // go to -infinity.  True if a value is not finite: a probability of 0 would not
+        // hide it.  (Kept short, as the tiles at the ends of a walk run it cold: with
+        // a step of its own for them, of 900 instructions, such a tile took 2 us.)
+        uint32_t vm[JT];
+        auto hide = [&](f32x4 (&x)[JT][2], float (&t)[JT], const i32x4 (&vf)[NDT], int i) {
+            const int tile = tile_at(i);
+            const bool ok = !strange || (uint32_t)paged_page(p, s.b, tile) < (uint32_t)p.n_pages;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[j][e >> 2][e & 3] = (vm[j] >> e) & 1u ? ok ? x[j][e >> 2][e & 3] : NAN : -INFINITY;
+            }
+            tops(t, x);
+            uint16x2 most = {0, 0};
+#pragma unroll
+            for (int f = 0; f < NDT; ++f)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(uint16x2, (uint32_t)vf[f][w] & 0x7fff7fffu));
+            return (bool)__any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
+        };
+        // A whole tile: attn_step with the order of its instructions laid down.  x: its
         // scores, y: the next one's, t: a lane's largest of x, and then of y.  The
         // keys are read first, the values under them; the next tile's scores run
         // under this one's exponentials, its largest scores are taken under the
@@ -652,11 +717,52 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             }
             __builtin_amdgcn_sched_barrier(0);
         };
-        // two tiles that every row of the workgroup sees whole
-        auto plain = [&](int i) {
-            return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !strange;
+        // A tile at the ends of a walk.
+        auto turn_end = [&](float (&t)[JT], int i) {
+            const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
+            i32x4 vf[NDT];
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) vf[f] = v[f * 64];
+            __builtin_amdgcn_sched_barrier(0);
+            const bool odd = hide(S, t, vf, i);
+            bool grow = false;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) grow = grow || t[j] > st[j].top;
+            if (__any(grow)) {
+                mfma_result_pad();
+#pragma unroll
+                for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
+            }
+            i32x4 P[JT], seen[JT];
+            const int one = 0x3f803f80;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                attn_probs(P[j], S[j], st[j].m * c, c);
+                st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    seen[j][w] = (int)(((vm[j] >> (2 * w)) & 1u ? 0x3f80u : 0u) | ((vm[j] >> (2 * w + 1)) & 1u ? 0x3f800000u : 0u));
+            }
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) {
+                if (odd) {  // values that are not finite: taken out, and given back as NaN to the rows that see them
+                    const i32x4 bad = take_nonfinite(vf[f]);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) {
+                        const f32x4 n = mfma_step<ET_BF16>(bad, seen[j], f32x4{0.f, 0.f, 0.f, 0.f});
+                        mfma_result_pad();
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n[e] > 0.f) st[j].O[f][e] = NAN;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+            }
+            mfma_result_pad();
         };
-        uint32_t vm[JT];
+        // two tiles that every row of the workgroup sees whole
+        auto plain = [&](int i) { return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !strange; };
         for (int i = 0; i < n;) {
             float top[JT];
             tops(top, S);
@@ -671,17 +777,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             advance(i);
 #pragma unroll 1
             for (const int end = i + 2; i < end; ++i) {
-                const int tile = tile_at(i);
-                if (i < n && sees(tile)) {
-                    const bool ok = !strange || (uint32_t)paged_page(p, s.b, tile) < (uint32_t)p.n_pages;
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) {
-                        vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-                        if (!ok) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
-                    }
-                    attn_step<HD, JT, true, true>(st, S, c, values(i), vm, [] {});
-                    mfma_result_pad();
-                }
+                if (i < n && sees(tile_at(i))) turn_end(top, i);
                 scores(S, i + 1);
                 mfma_result_pad();
             }
@@ -699,7 +795,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             uint16_t* o = a.out + ((size_t)(s.row0 + tok[j]) * a.H + kvh * G + (x - tok[j] * G)) * HD + 4 * g;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
-                st4(o, 16 * dt, st[j].O[dt][0] * inv, st[j].O[dt][1] * inv, st[j].O[dt][2] * inv, st[j].O[dt][3] * inv);
+                *(uint2*)(o + 16 * dt) = make_uint2(pack_bf(st[j].O[dt][0] * inv, st[j].O[dt][1] * inv),
+                                                    pack_bf(st[j].O[dt][2] * inv, st[j].O[dt][3] * inv));
         } else {
             const size_t at = ((size_t)(sh.part + split * sh.nq + qt) * p.Hkv + kvh) * R + x - p0;
 #pragma unroll
