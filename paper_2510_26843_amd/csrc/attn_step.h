@@ -1,6 +1,6 @@
-// The tile step that the attention over the 4-bit cache (kv4.hip) and the one
-// over a paged cache (paged.hip) share: a wave's running softmax state, and one
-// key tile's part of it.
+// What kv4.hip, paged.hip and logprobs.hip share: launches, sums and maxima over
+// a wave, and the attention's tile step (a wave's running softmax state, and one
+// key tile's part of it).
 #pragma once
 #include "kernel_common.h"
 
@@ -15,6 +15,59 @@ template <typename... P>
 static hipError_t launch_checked(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, P... args) {
     void* at[] = {(void*)&args...};
     return hipLaunchKernel((const void*)kernel, grid, dim3(threads), at, 0, s);
+}
+
+// Inclusive sum over the lanes up to one's own, by cross-lane operands: six adds
+// (through LDS, as shuffles go, each step waits 100 cycles).
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_0(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_0(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)b), hi = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(b >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <typename V> __device__ __forceinline__ V wave_scan(V x) {
+    x += dpp_or_0<0x111, 0xf>(x);  // the row's lane - 1, - 2, - 4, - 8
+    x += dpp_or_0<0x112, 0xf>(x);
+    x += dpp_or_0<0x114, 0xf>(x);
+    x += dpp_or_0<0x118, 0xf>(x);
+    x += dpp_or_0<0x142, 0xa>(x);  // the last lane of the row before, to rows 1 and 3
+    x += dpp_or_0<0x143, 0xc>(x);  // lane 31, to rows 2 and 3
+    return x;
+}
+template <typename V> __device__ __forceinline__ V wave_total(V x) {
+    const V s = wave_scan(x);
+    if constexpr (sizeof(V) == 4) {
+        return (V)__builtin_amdgcn_readlane((int)s, 63);
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, s);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63);
+        return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 | lo);
+    }
+}
+// The largest of the lanes' values, the same for every lane (no NaN).
+__device__ __forceinline__ float wave_top(float x) {
+    auto up = [&](auto ctrl, auto rows) {
+        const int y = __builtin_amdgcn_update_dpp((int)0xff800000, (int)__float_as_uint(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        x = fmaxf(x, __uint_as_float((uint32_t)y));
+    };
+    up(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    up(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    up(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    up(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    up(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    up(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+}
+__device__ __forceinline__ int wave_most(int x) {  // of values >= 0
+    x = max(x, dpp_or_0<0x111, 0xf>(x));
+    x = max(x, dpp_or_0<0x112, 0xf>(x));
+    x = max(x, dpp_or_0<0x114, 0xf>(x));
+    x = max(x, dpp_or_0<0x118, 0xf>(x));
+    x = max(x, dpp_or_0<0x142, 0xa>(x));
+    x = max(x, dpp_or_0<0x143, 0xc>(x));
+    return __builtin_amdgcn_readlane(x, 63);
 }
 
 __device__ __forceinline__ uint32_t pack_bf(float a, float b) {

@@ -8,25 +8,25 @@
 // next one in flight), each wave with a running maximum, S and U = sum e^l l of
 // its own.  Exponents are in log2 units.
 //
-// The K best: a wave keeps a list (in LDS) of what may be among its K best.  The
-// K-th largest of its 64 lanes' running maxima bounds its K-th best from below,
-// and closely (the 20th lane is about the 24th logit), so after the first chunk
-// few logits pass it; when the list fills up the bound is taken again and the
-// list sifted.  Equal logits can defeat it: then the list is cut to its K best by
-// rank, and a chunk with too many of them gives its K best one after another.
-// The lists are joined by rank, over the waves and then over a row's parts.
-// Every list is sorted by (logit, id), so no order of arrival shows.
+// The K best: the walk notes in LDS each thread's largest logit of each chunk, no
+// more.  The K-th largest of the threads' largest logits bounds the K-th best from
+// below, and closely (of 1024 threads the 20th is about the 20th logit), so that
+// few (thread, chunk) pairs reach it, whose logits are read once more; what
+// reaches the bound is ordered by rank.  (Collecting candidates during the walk,
+// against a bound of the first chunk, cost as much as the sums.)  Equal logits can
+// defeat the bound: where more than LP_LIST reach it, the K best come one after
+// another, each from a pass over the part.  Everything is ordered by (logit, id),
+// so no order of arrival shows.
 //
-// What bounds it: for many rows the bytes (1501 rows of 128256 fp32 logits, 20
-// alternatives); for one row the latency of its two kernels.
+// What bounds it: for many rows the bytes; for one row the latency of a CU's reads.
 #include "attn_step.h"
 
 #include <algorithm>
 
 namespace cas {
 
-static constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64, LP_MAX_K = 32;
-static constexpr int LP_LIST = 256;  // entries of a wave's list
+static constexpr int LP_MAX_K = 32;
+static constexpr int LP_LIST = 512;  // candidates of a workgroup, of which a list holds
 static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ bool lp_better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
@@ -38,7 +38,7 @@ __device__ __forceinline__ float lp_lane(float x, int l) {
 __device__ __forceinline__ float lp_kth(float x, int K) {
     const int lane = threadIdx.x & 63;
     int above = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int l = 0; l < 64; ++l) {
         const float o = lp_lane(x, l);
         above += o > x || (o == x && l < lane) ? 1 : 0;
@@ -46,56 +46,26 @@ __device__ __forceinline__ float lp_kth(float x, int K) {
     return lp_lane(x, __builtin_ctzll(__ballot(above == K - 1)));
 }
 
-// The K best of a wave's list of n, in order, to its front (fewer: all, in
-// order); returns their number.
-__device__ __forceinline__ int lp_rank(float* v, int* id, int n, int K) {
-    const int lane = threadIdx.x & 63;
-    float x[LP_LIST / 64];
-    int xi[LP_LIST / 64], rank[LP_LIST / 64];
+// How many of a list's n entries (16-byte aligned; up to three -infinity behind
+// them) are better than (x, xi), four at a time.
+__device__ __forceinline__ int lp_count(const float* v, const int* id, int n, float x, int xi) {
+    int k = 0;
+#pragma unroll 2
+    for (int j = 0; j < n; j += 4) {
+        const f32x4 o = *(const f32x4*)(v + j);
+        const i32x4 oi = *(const i32x4*)(id + j);
 #pragma unroll
-    for (int q = 0; q < LP_LIST / 64; ++q) {
-        const int i = q * 64 + lane;
-        x[q] = i < n ? v[i] : -INFINITY;
-        xi[q] = i < n ? id[i] : 0x7fffffff;
-        rank[q] = 0;
+        for (int e = 0; e < 4; ++e) k += lp_better(o[e], oi[e], x, xi) ? 1 : 0;
     }
-    for (int j = 0; j < n; ++j) {  // (broadcast reads)
-        const float o = v[j];
-        const int oi = id[j];
-#pragma unroll
-        for (int q = 0; q < LP_LIST / 64; ++q) rank[q] += lp_better(o, oi, x[q], xi[q]) ? 1 : 0;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int q = 0; q < LP_LIST / 64; ++q)
-        if (q * 64 + lane < n && rank[q] < K) {
-            v[rank[q]] = x[q];
-            id[rank[q]] = xi[q];
-        }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    return min(n, K);
+    return k;
 }
-
-// Drops what is below tau from a wave's list of n.
-__device__ __forceinline__ int lp_sift(float* v, int* id, int n, float tau) {
+__device__ __forceinline__ void lp_pad(float* v, int* id, int n) {
     const int lane = threadIdx.x & 63;
-    int kept = 0;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = i0 + lane;
-        const float x = i < n ? v[i] : -INFINITY;
-        const int xi = i < n ? id[i] : 0;
-        const bool keep = i < n && x >= tau;
-        const uint64_t m = __ballot(keep);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (keep) {
-            const int to = kept + __popcll(m & (((uint64_t)1 << lane) - 1));
-            v[to] = x;
-            id[to] = xi;
-        }
-        kept += __popcll(m);
+    if (lane < 3) {
+        v[n + lane] = -INFINITY;
+        id[n + lane] = 0x7fffffff;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    return kept;
 }
 
 // A row's running sums relative to its largest logit.
@@ -140,47 +110,56 @@ template <int THREADS> __device__ __forceinline__ void lp_tokens(const LogprobAr
 static int lp_words(int K) { return 4 + 2 * K; }
 
 // Workgroup = (row, part): chunks [part span, (part + 1) span) of EACH logits per
-// thread.  One part: it gives the row's results itself.
-template <bool BF16, int EACH>
-__global__ void __launch_bounds__(LP_THREADS) k_logprob_part(const LogprobArgs a, int parts, int span, int words) {
-    constexpr int E = BF16 ? 8 : 4, NV = EACH / E, CHUNK = LP_THREADS * EACH, W = LP_WAVES;
+// thread.  One part: it gives the row's results itself.  Dynamic LDS: the largest
+// logit of each (chunk, thread) of the part.
+template <bool BF16, int EACH, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, int parts, int span, int words) {
+    constexpr int E = BF16 ? 8 : 4, NV = EACH / E, CHUNK = THREADS * EACH, W = THREADS / 64;
+    constexpr int LIST = THREADS > LP_LIST ? THREADS : LP_LIST;
     struct __attribute__((packed, aligned(BF16 ? 2 : 4))) Piece { i32x4 v; };
-    __shared__ float sm_v[W][LP_LIST], sm_sum[W][3];
-    __shared__ int sm_i[W][LP_LIST], sm_n[W];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    extern __shared__ __attribute__((aligned(16))) float sm_top[];
+    __shared__ __attribute__((aligned(16))) float sm_v[LIST + 4];
+    __shared__ __attribute__((aligned(16))) int sm_i[LIST + 4];
+    __shared__ float sm_sum[W][4];  // m, s, u, and the wave's K-th largest thread
+    __shared__ float sm_tau;
+    __shared__ int sm_n[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % parts, row = blockIdx.x / parts, K = a.K;
     const int begin = part * span * CHUNK, end = min(a.V, begin + span * CHUNK);
     const char* x0 = (const char*)a.x + (size_t)row * a.ld * (BF16 ? 2 : 4);
     const float c = a.scale * LOG2E;
-    float *v = sm_v[wave], lm = -INFINITY, tau = -INFINITY;
-    int *id = sm_i[wave], n = 0;
-    LpSums t = {-INFINITY, 0.f, 0.f};  // (s and u: the lane's)
+    const int odd = end - end % E;  // (a part ends at a chunk's end or the row's) the logits past the last whole piece
     auto load = [&](i32x4 (&r)[NV], int base) {  // pieces that lie in the part as a whole
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int o = base + (i * LP_THREADS + (int)threadIdx.x) * E;
+            const int o = base + (i * THREADS + tid) * E;
             if constexpr (BF16) r[i] = i32x4{(int)0xff80ff80, (int)0xff80ff80, (int)0xff80ff80, (int)0xff80ff80};
             else r[i] = i32x4{(int)0xff800000, (int)0xff800000, (int)0xff800000, (int)0xff800000};
             if (o + E <= end) r[i] = ((const Piece*)(x0 + (size_t)o * (BF16 ? 2 : 4)))->v;
         }
     };
+    // a chunk's logits: its pieces', and one of the odd ones for each of the first threads
+    auto unpack = [&](float (&x)[EACH + 1], const i32x4 (&r)[NV], int base) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) x[e] = piece_val<std::conditional_t<BF16, uint16_t, float>>(r[e / E], e % E);
+        x[EACH] = -INFINITY;
+        if (base + CHUNK >= end && odd + tid < end) x[EACH] = BF16 ? bf2f(((const uint16_t*)x0)[odd + tid]) : ((const float*)x0)[odd + tid];
+    };
+    auto id_of = [&](int base, int e) { return e == EACH ? odd + tid : base + ((e / E) * THREADS + tid) * E + e % E; };
+    LpSums t = {-INFINITY, 0.f, 0.f};  // (s and u: the thread's)
+    float lm = -INFINITY;
     i32x4 raw[NV];
     load(raw, begin);
-    for (int base = begin; base < end; base += CHUNK) {
+    for (int base = begin, k = 0; base < end; base += CHUNK, ++k) {
         float x[EACH + 1];
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) x[e] = piece_val<std::conditional_t<BF16, uint16_t, float>>(raw[e / E], e % E);
-        // the logits past the last whole piece: one for each of the first threads
-        x[EACH] = -INFINITY;
-        const int odd = end - end % E;  // (a part ends at a chunk's end or the row's)
-        if (base + CHUNK >= end && odd + (int)threadIdx.x < end)
-            x[EACH] = BF16 ? bf2f(((const uint16_t*)x0)[odd + threadIdx.x]) : ((const float*)x0)[odd + threadIdx.x];
+        unpack(x, raw, base);
         if (base + CHUNK < end) load(raw, base + CHUNK);
         float cm = -INFINITY;  // (fmaxf passes over NaN: s finds it)
 #pragma unroll
         for (int e = 0; e <= EACH; ++e) cm = fmaxf(cm, x[e]);
+        if (K > 0) sm_top[k * THREADS + tid] = cm;
         lm = fmaxf(lm, cm);
-        const float wm = wave_max(cm);
+        const float wm = wave_top(cm);
         if (wm > t.m) t.lift(wm, c);
         const float ref = t.ref();
 #pragma unroll
@@ -189,99 +168,25 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprob_part(const LogprobArgs a
             t.s += p;
             t.u = fmaf(p, fmaxf(l, -1e30f), t.u);  // (nothing where p is 0)
         }
-        if (K > 0) {
-            if (base == begin) tau = lp_kth(lm, K);
-            if (wm >= tau && wm > -INFINITY) {
-                auto id_of = [&](int e) {
-                    return e == EACH ? odd + (int)threadIdx.x : base + ((e / E) * LP_THREADS + (int)threadIdx.x) * E + e % E;
-                };
-                int mine, upto, all;  // the lane's candidates, those up to its own, the wave's
-                auto count = [&] {
-                    mine = 0;
-                    if (cm >= tau) {
-#pragma unroll
-                        for (int e = 0; e <= EACH; ++e) mine += x[e] >= tau && x[e] > -INFINITY ? 1 : 0;
-                    }
-                    upto = mine;
-#pragma unroll
-                    for (int o = 1; o < 64; o <<= 1) {
-                        const int y = __shfl_up(upto, o);
-                        upto += lane >= o ? y : 0;
-                    }
-                    all = __builtin_amdgcn_readlane(upto, 63);
-                };
-                for (int pass = 0;; ++pass) {
-                    count();
-                    if (n + all <= LP_LIST || pass) break;
-                    tau = lp_kth(lm, K);
-                    n = lp_sift(v, id, n, tau);
-                    if (n > LP_LIST / 2) n = lp_rank(v, id, n, K);
-                }
-                if (n + all <= LP_LIST) {
-                    int to = n + upto - mine;
-                    if (mine) {
-#pragma unroll
-                        for (int e = 0; e <= EACH; ++e)
-                            if (x[e] >= tau && x[e] > -INFINITY) {
-                                v[to] = x[e];
-                                id[to++] = id_of(e);
-                            }
-                    }
-                    n += all;
-                } else {  // the chunk's K best, one after another
-                    if (n > LP_LIST - LP_MAX_K) n = lp_rank(v, id, n, K);
-                    float pv = INFINITY;
-                    int pi = -1;
-                    for (int k = 0; k < K; ++k) {
-                        float bv = -INFINITY;
-                        int bi = 0x7fffffff;
-#pragma unroll
-                        for (int e = 0; e <= EACH; ++e)
-                            if (lp_better(pv, pi, x[e], id_of(e)) && lp_better(x[e], id_of(e), bv, bi)) {
-                                bv = x[e];
-                                bi = id_of(e);
-                            }
-#pragma unroll
-                        for (int o = 32; o >= 1; o >>= 1) {
-                            const float ov = __shfl_xor(bv, o);
-                            const int oi = __shfl_xor(bi, o);
-                            if (lp_better(ov, oi, bv, bi)) {
-                                bv = ov;
-                                bi = oi;
-                            }
-                        }
-                        if (bi == 0x7fffffff) break;
-                        if (lane == 0) {
-                            v[n] = bv;
-                            id[n] = bi;
-                        }
-                        ++n;
-                        pv = bv;
-                        pi = bi;
-                    }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            }
-        }
     }
-    if (K > 0) {
-        n = lp_sift(v, id, n, lp_kth(lm, K));
-        n = lp_rank(v, id, n, K);
-    }
-    // ---- join the waves
+    const float kth = K > 0 ? lp_kth(lm, K) : 0.f;
     t.s = wave_sum(t.s);
     t.u = wave_sum(t.u);
     if (lane == 0) {
         sm_sum[wave][0] = t.m;
         sm_sum[wave][1] = t.s;
         sm_sum[wave][2] = t.u;
-        sm_n[wave] = n;
+        sm_sum[wave][3] = kth;
     }
+    if (tid < 2) sm_n[tid] = 0;
     __syncthreads();
     LpSums r = {-INFINITY, 0.f, 0.f};
-    float m = -INFINITY;
+    float m = -INFINITY, least = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, sm_sum[w][0]);
+    for (int w = 0; w < W; ++w) {
+        m = fmaxf(m, sm_sum[w][0]);
+        least = fmaxf(least, sm_sum[w][3]);
+    }
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         LpSums q = {sm_sum[w][0], sm_sum[w][1], sm_sum[w][2]};
@@ -293,45 +198,143 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprob_part(const LogprobArgs a
     const LpRow out(r);
     float* rec = a.work + (size_t)blockIdx.x * words;
     if (parts == 1) {
-        lp_tokens<LP_THREADS>(a, row, out);
-    } else if (threadIdx.x == 0) {
+        lp_tokens<THREADS>(a, row, out);
+    } else if (tid == 0) {
         rec[0] = r.m;
         rec[1] = r.s;
         rec[2] = r.u;
     }
-    if (K > 0) {
-        float* best = parts == 1 ? a.best + (size_t)row * K : rec + 4;
-        int* ids = parts == 1 ? a.ids + (size_t)row * K : (int*)rec + 4 + K;
-        int total = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) total += sm_n[w];
-        // a wave's entries count those of all lists that are better
-        if (lane < n) {
-            const float y = v[lane];
-            const int yi = id[lane];
-            int rank = 0;
-#pragma unroll
-            for (int w = 0; w < W; ++w)
-                for (int j = 0; j < sm_n[w]; ++j) rank += lp_better(sm_v[w][j], sm_i[w][j], y, yi) ? 1 : 0;
-            if (rank < K) {
-                best[rank] = parts > 1 ? y : out.none ? NAN : out.logp(y, a.scale);
-                ids[rank] = parts == 1 && out.none ? -1 : yi;
-            }
+    if (K == 0) return;
+    float* best = parts == 1 ? a.best + (size_t)row * K : rec + 4;
+    int* ids = parts == 1 ? a.ids + (size_t)row * K : (int*)rec + 4 + K;
+    auto give = [&](int rank, float y, int yi) {
+        best[rank] = parts > 1 ? y : out.none ? NAN : out.logp(y, a.scale);
+        ids[rank] = parts == 1 && out.none ? -1 : yi;
+    };
+    // the K-th largest of all threads' largest logits: of those that are no less than every wave's
+    auto push = [&](bool in, float y, int yi, int* count) {
+        const uint64_t b = __ballot(in);
+        int to = 0;
+        if (lane == 0 && b) to = atomicAdd(count, (int)__popcll(b));
+        to = __builtin_amdgcn_readfirstlane(to) + __popcll(b & (((uint64_t)1 << lane) - 1));
+        if (in && to < LIST) {
+            sm_v[to] = y;
+            sm_i[to] = yi;
         }
-        for (int i = total + (int)threadIdx.x; i < K; i += LP_THREADS) {  // fewer than K finite logits
+    };
+    push(lm >= least, lm, tid, &sm_n[0]);
+    __syncthreads();
+    const int nt = sm_n[0];
+    if (tid < 64) lp_pad(sm_v, sm_i, nt);
+    __syncthreads();
+    if (tid < nt) {
+        const float y = sm_v[tid];
+        if (lp_count(sm_v, sm_i, nt, y, sm_i[tid]) == K - 1) sm_tau = y;
+    }
+    __syncthreads();
+    const float tau = sm_tau;
+    // the logits that reach it
+    for (int base = begin, k = 0; base < end; base += CHUNK, ++k) {
+        const float cm = sm_top[k * THREADS + tid];
+        const bool some = cm >= tau && cm > -INFINITY;
+        if (!__any(some)) continue;
+        float x[EACH + 1];
+        if (some) {
+            load(raw, base);
+            unpack(x, raw, base);
+        }
+#pragma unroll
+        for (int e = 0; e <= EACH; ++e) {
+            const bool in = some && x[e] >= tau && x[e] > -INFINITY;
+            if (__any(in)) push(in, x[e], id_of(base, e), &sm_n[1]);
+        }
+    }
+    __syncthreads();
+    const int n = sm_n[1];
+    if (n <= LP_LIST) {
+        if (tid < 64) lp_pad(sm_v, sm_i, n);
+        __syncthreads();
+        for (int i = tid; i < n; i += THREADS) {
+            const float y = sm_v[i];
+            const int yi = sm_i[i], rank = lp_count(sm_v, sm_i, n, y, yi);
+            if (rank < K) give(rank, y, yi);
+        }
+        for (int i = n + tid; i < K; i += THREADS) {  // fewer than K finite logits
             best[i] = parts == 1 && out.none ? NAN : -INFINITY;
             ids[i] = -1;
         }
+        return;
+    }
+    float pv = INFINITY;
+    int pi = -1;
+    for (int k = 0; k < K; ++k) {
+        float bv = -INFINITY;
+        int bi = 0x7fffffff;
+        for (int base = begin; base < end; base += CHUNK) {
+            float x[EACH + 1];
+            load(raw, base);
+            unpack(x, raw, base);
+#pragma unroll
+            for (int e = 0; e <= EACH; ++e) {
+                const int id = id_of(base, e);
+                if (lp_better(pv, pi, x[e], id) && lp_better(x[e], id, bv, bi)) {
+                    bv = x[e];
+                    bi = id;
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            const float ov = __shfl_xor(bv, o);
+            const int oi = __shfl_xor(bi, o);
+            if (lp_better(ov, oi, bv, bi)) {
+                bv = ov;
+                bi = oi;
+            }
+        }
+        __syncthreads();
+        if (lane == 0) {
+            sm_v[wave] = bv;
+            sm_i[wave] = bi;
+        }
+        __syncthreads();
+        bv = sm_v[0];
+        bi = sm_i[0];
+        for (int w = 1; w < W; ++w)
+            if (lp_better(sm_v[w], sm_i[w], bv, bi)) {
+                bv = sm_v[w];
+                bi = sm_i[w];
+            }
+        if (tid == 0) give(k, bv, bi);  // (more than LP_LIST finite logits: there is one)
+        pv = bv;
+        pi = bi;
     }
 }
 
 // One wave = one row in parts: their sums by a butterfly, the best of their
-// bests, and the tokens asked for.
-__global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int parts, int words) {
-    extern __shared__ float sm[];  // [parts * K] values, then ids
-    const int row = blockIdx.x, lane = threadIdx.x, K = a.K;
+// bests, and the tokens asked for.  All it reads is asked for at the start: what
+// other workgroups wrote takes 2 us to come.
+__global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int parts, int words, uint32_t inv_K) {
+    extern __shared__ __attribute__((aligned(16))) float sm[];  // values, then ids
+    constexpr int AT_ONCE = 8;
+    const int row = blockIdx.x, lane = threadIdx.x, K = a.K, all = parts * K;
     const float* rec = a.work + (size_t)row * parts * words;
     const float c = a.scale * LOG2E;
+    auto part_of = [&](int i) { return inv_K ? (int)__umulhi((uint32_t)i, inv_K) : i; };
+    float cv[AT_ONCE];
+    int ci[AT_ONCE];
+    auto candidates = [&](int i0) {
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+            const int i = min(i0 + q * 64 + lane, all - 1), k = part_of(i);
+            const float* at = rec + (size_t)k * words + 4 + (i - k * K);
+            cv[q] = at[0];
+            ci[q] = ((const int*)at)[K];
+        }
+    };
+    if (K > 0) candidates(0);
+    const int t0 = lane < a.m ? a.tokens[(size_t)row * a.m + lane] : -1;
+    const float x0 = t0 >= 0 && t0 < a.V ? lp_logit(a, row, t0) : NAN;
     LpSums t = {-INFINITY, 0.f, 0.f};
     float tau = -INFINITY;  // every part's K-th best is no better than the row's
     for (int k = lane; k < parts; k += 64) {
@@ -344,36 +347,38 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
         t.s += p.s;
         t.u += p.u;
     }
-    const float m = wave_max(t.m);
-    t.lift(m, c);
+    t.lift(wave_top(t.m), c);
     t.s = wave_sum(t.s);
     t.u = wave_sum(t.u);
     const LpRow out(t);
-    lp_tokens<64>(a, row, out);
-    if (K == 0) return;
-    tau = wave_max(tau);
-    float *best = a.best + (size_t)row * K, *v = sm;
-    int *ids = a.ids + (size_t)row * K, *id = (int*)(sm + (size_t)parts * K), n = 0;
-    for (int i0 = 0; i0 < parts * K; i0 += 64) {
-        const int i = min(i0 + lane, parts * K - 1);
-        const float* q = rec + (size_t)(i / K) * words + 4;
-        const float x = q[i % K];
-        const int xi = ((const int*)q)[K + i % K];
-        const bool keep = i0 + lane < parts * K && x >= tau && x > -INFINITY;
-        const uint64_t in = __ballot(keep);
-        if (keep) {
-            const int to = n + __popcll(in & (((uint64_t)1 << lane) - 1));
-            v[to] = x;
-            id[to] = xi;
-        }
-        n += __popcll(in);
+    if (lane == 0 && a.entropy) a.entropy[row] = out.entropy;
+    for (int j = lane; j < a.m; j += 64) {
+        const int id = j < 64 ? t0 : a.tokens[(size_t)row * a.m + j];
+        const bool ok = id >= 0 && id < a.V;
+        a.logp[(size_t)row * a.m + j] = ok ? out.logp(j < 64 ? x0 : lp_logit(a, row, id), a.scale) : NAN;
     }
-    __syncthreads();
+    if (K == 0) return;
+    tau = wave_top(tau);
+    float *best = a.best + (size_t)row * K, *v = sm;
+    int *ids = a.ids + (size_t)row * K, *id = (int*)(sm + ((all + 7) & ~3)), n = 0;
+    for (int i0 = 0; i0 < all; i0 += AT_ONCE * 64) {
+        if (i0) candidates(i0);
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+            const bool keep = i0 + q * 64 + lane < all && cv[q] >= tau && cv[q] > -INFINITY;
+            const uint64_t in = __ballot(keep);
+            if (keep) {
+                const int to = n + __popcll(in & (((uint64_t)1 << lane) - 1));
+                v[to] = cv[q];
+                id[to] = ci[q];
+            }
+            n += __popcll(in);
+        }
+    }
+    lp_pad(v, id, n);
     for (int i = lane; i < n; i += 64) {
         const float x = v[i];
-        const int xi = id[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += lp_better(v[j], id[j], x, xi) ? 1 : 0;
+        const int xi = id[i], rank = lp_count(v, id, n, x, xi);
         if (rank < K) {
             best[rank] = out.none ? NAN : out.logp(x, a.scale);
             ids[rank] = out.none ? -1 : xi;
@@ -385,38 +390,49 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     }
 }
 
-// Chunks of 8192 logits, or of 2048 where a row's would leave the chip empty, and
-// parts such that there are a few workgroups per CU.
+// A row of up to LP_ROW bytes in a call of up to LP_ROWS rows is one workgroup of
+// 1024 threads: a CU reads it in less time than a second kernel takes.  Others
+// are workgroups of 256 threads: in parts, a few workgroups per CU, where there are
+// too few rows, in chunks of 2048 logits where 8192 would leave the chip empty.
+static constexpr int LP_ROWS = 512, LP_SPAN = 32;  // LP_SPAN: most chunks of a part
+static constexpr int64_t LP_ROW = 640 << 10;
 struct LpPlan {
-    int each, parts, span;
+    int each, threads, parts, span;
 };
-static LpPlan lp_plan(int n, int V) {
+static LpPlan lp_plan(int n, int V, int bf16) {
     LpPlan p;
-    p.each = (int64_t)n * ((V + 8191) / 8192) >= 512 ? 32 : 8;
-    const int chunk = LP_THREADS * p.each, chunks = (V + chunk - 1) / chunk;
-    const int want = (int)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / n));
-    p.span = (chunks + want - 1) / want;
+    const bool whole = n <= LP_ROWS && (int64_t)V * (bf16 ? 2 : 4) <= LP_ROW;
+    p.threads = whole ? 1024 : 256;
+    p.each = whole ? 16 : (int64_t)n * ((V + 8191) / 8192) >= 512 ? 32 : 8;
+    const int chunk = p.threads * p.each, chunks = (V + chunk - 1) / chunk;
+    const int want = whole ? 1 : (int)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / n));
+    p.span = std::min((chunks + want - 1) / want, LP_SPAN);
     p.parts = (chunks + p.span - 1) / p.span;
     return p;
 }
-size_t logprob_work_bytes(int n, int V, int K) {
-    const LpPlan p = lp_plan(n, V);
-    return std::max<size_t>(16, (size_t)n * p.parts * lp_words(K) * 4);
+size_t logprob_work_bytes(int n, int V, int K) {  // (of either type)
+    const LpPlan f = lp_plan(n, V, 0), h = lp_plan(n, V, 1);
+    return std::max<size_t>(16, (size_t)n * std::max(f.parts, h.parts) * lp_words(K) * 4);
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     if (a.n < 1 || a.V < 1 || a.K < 0 || a.K > LP_MAX_K || a.m < 0) return hipErrorInvalidValue;
-    const LpPlan p = lp_plan(a.n, a.V);
+    const LpPlan p = lp_plan(a.n, a.V, a.bf16);
     const int words = lp_words(a.K);
     const dim3 grid((unsigned)a.n * p.parts);
-    auto kernel = p.each == 32 ? (a.bf16 ? k_logprob_part<true, 32> : k_logprob_part<false, 32>)
-                               : (a.bf16 ? k_logprob_part<true, 8> : k_logprob_part<false, 8>);
-    const hipError_t e = launch_checked(kernel, grid, LP_THREADS, s, a, p.parts, p.span, words);
-    if (e != hipSuccess || p.parts == 1) return e;
+    auto kernel = p.each == 16   ? (a.bf16 ? k_logprob_part<true, 16, 1024> : k_logprob_part<false, 16, 1024>)
+                  : p.each == 32 ? (a.bf16 ? k_logprob_part<true, 32, 256> : k_logprob_part<false, 32, 256>)
+                                 : (a.bf16 ? k_logprob_part<true, 8, 256> : k_logprob_part<false, 8, 256>);
     LogprobArgs b = a;
-    int c = p.parts, w = words;
-    void* at[] = {(void*)&b, (void*)&c, (void*)&w};
-    return hipLaunchKernel((const void*)k_logprob_join, dim3(a.n), dim3(64), at, (size_t)p.parts * a.K * 8, s);
+    int c = p.parts, sp = p.span, w = words;
+    void* part_at[] = {(void*)&b, (void*)&c, (void*)&sp, (void*)&w};
+    const hipError_t e = hipLaunchKernel((const void*)kernel, grid, dim3(p.threads), part_at,
+                                         a.K > 0 ? (size_t)p.span * p.threads * 4 : 0, s);
+    if (e != hipSuccess || p.parts == 1) return e;
+    // (multiplying by it and taking the high word divides exactly below 2^25)
+    uint32_t inv_K = a.K > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.K - 1) / a.K) : 0u;
+    void* at[] = {(void*)&b, (void*)&c, (void*)&w, (void*)&inv_K};
+    return hipLaunchKernel((const void*)k_logprob_join, dim3(a.n), dim3(64), at, (size_t)(p.parts * a.K + 8) * 8, s);
 }
 
 }  // namespace cas

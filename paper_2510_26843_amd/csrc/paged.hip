@@ -219,45 +219,6 @@ __device__ __forceinline__ uint32_t paged_vis8(const PagedSeq& s, int t, int bas
     return bits8(0, min(sink, own) - base) | bits8(own - window - base, own + 1 - base);
 }
 
-// Inclusive sum over the lanes up to one's own, by cross-lane operands: six adds
-// (through LDS, as shuffles go, each step waits 100 cycles).
-template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_0(int x) {
-    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_0(double x) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)b), hi = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(b >> 32));
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-template <typename V> __device__ __forceinline__ V wave_scan(V x) {
-    x += dpp_or_0<0x111, 0xf>(x);  // the row's lane - 1, - 2, - 4, - 8
-    x += dpp_or_0<0x112, 0xf>(x);
-    x += dpp_or_0<0x114, 0xf>(x);
-    x += dpp_or_0<0x118, 0xf>(x);
-    x += dpp_or_0<0x142, 0xa>(x);  // the last lane of the row before, to rows 1 and 3
-    x += dpp_or_0<0x143, 0xc>(x);  // lane 31, to rows 2 and 3
-    return x;
-}
-template <typename V> __device__ __forceinline__ V wave_total(V x) {
-    const V s = wave_scan(x);
-    if constexpr (sizeof(V) == 4) {
-        return (V)__builtin_amdgcn_readlane((int)s, 63);
-    } else {
-        const uint64_t b = __builtin_bit_cast(uint64_t, s);
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63);
-        return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 | lo);
-    }
-}
-__device__ __forceinline__ int wave_most(int x) {  // of values >= 0
-    x = max(x, dpp_or_0<0x111, 0xf>(x));
-    x = max(x, dpp_or_0<0x112, 0xf>(x));
-    x = max(x, dpp_or_0<0x114, 0xf>(x));
-    x = max(x, dpp_or_0<0x118, 0xf>(x));
-    x = max(x, dpp_or_0<0x142, 0xa>(x));
-    x = max(x, dpp_or_0<0x143, 0xc>(x));
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
 // How the work is shared out.  A unit is (sequence, query tile of R packed
 // rows, kv head); the split rule gives a sequence of more than C tiles ns =
 // ceil(tiles / C) shares per unit, with C such that the batch has about
