@@ -34,8 +34,8 @@ __device__ __forceinline__ float lp_lane(float x, int l) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), l));
 }
 
-// The K-th largest of the lanes' values (no NaN), the same for every lane.
-__device__ __forceinline__ float lp_kth(float x, int K) {
+// The K-th and the J-th largest of the lanes' values (no NaN), the same for every lane.
+__device__ __forceinline__ void lp_kth(float x, int K, int J, float* kth, float* jth) {
     const int lane = threadIdx.x & 63;
     int above = 0;
 #pragma unroll 4
@@ -43,7 +43,8 @@ __device__ __forceinline__ float lp_kth(float x, int K) {
         const float o = lp_lane(x, l);
         above += o > x || (o == x && l < lane) ? 1 : 0;
     }
-    return lp_lane(x, __builtin_ctzll(__ballot(above == K - 1)));
+    *kth = lp_lane(x, __builtin_ctzll(__ballot(above == K - 1)));
+    *jth = lp_lane(x, __builtin_ctzll(__ballot(above == J - 1)));
 }
 
 // How many of a list's n entries (16-byte aligned; up to three -infinity behind
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
     extern __shared__ __attribute__((aligned(16))) float sm_top[];
     __shared__ __attribute__((aligned(16))) float sm_v[LIST + 4];
     __shared__ __attribute__((aligned(16))) int sm_i[LIST + 4];
-    __shared__ float sm_sum[W][4];  // m, s, u, and the wave's K-th largest thread
+    __shared__ float sm_sum[W][5];  // m, s, u, and the wave's K-th and ceil(K / W)-th largest thread
     __shared__ float sm_tau;
     __shared__ int sm_n[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -169,7 +170,10 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
             t.u = fmaf(p, fmaxf(l, -1e30f), t.u);  // (nothing where p is 0)
         }
     }
-    const float kth = K > 0 ? lp_kth(lm, K) : 0.f;
+    // Of W waves at least K threads reach each of: the K-th largest thread of any
+    // wave, and the smallest of the waves' ceil(K / W)-th.
+    float kth = 0.f, jth = 0.f;
+    if (K > 0) lp_kth(lm, K, (K + W - 1) / W, &kth, &jth);
     t.s = wave_sum(t.s);
     t.u = wave_sum(t.u);
     if (lane == 0) {
@@ -177,16 +181,19 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
         sm_sum[wave][1] = t.s;
         sm_sum[wave][2] = t.u;
         sm_sum[wave][3] = kth;
+        sm_sum[wave][4] = jth;
     }
     if (tid < 2) sm_n[tid] = 0;
     __syncthreads();
     LpSums r = {-INFINITY, 0.f, 0.f};
-    float m = -INFINITY, least = -INFINITY;
+    float m = -INFINITY, least = -INFINITY, low = INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         m = fmaxf(m, sm_sum[w][0]);
         least = fmaxf(least, sm_sum[w][3]);
+        low = fminf(low, sm_sum[w][4]);
     }
+    least = fmaxf(least, low);
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         LpSums q = {sm_sum[w][0], sm_sum[w][1], sm_sum[w][2]};
@@ -211,7 +218,7 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
         best[rank] = parts > 1 ? y : out.none ? NAN : out.logp(y, a.scale);
         ids[rank] = parts == 1 && out.none ? -1 : yi;
     };
-    // the K-th largest of all threads' largest logits: of those that are no less than every wave's
+    // the K-th largest of all threads' largest logits, of those that reach `least`
     auto push = [&](bool in, float y, int yi, int* count) {
         const uint64_t b = __ballot(in);
         int to = 0;
@@ -233,21 +240,27 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
     }
     __syncthreads();
     const float tau = sm_tau;
-    // the logits that reach it
+    // the logits that reach it: each thread's chunks that have some, one after another
+    uint32_t hit = 0;
     for (int base = begin, k = 0; base < end; base += CHUNK, ++k) {
         const float cm = sm_top[k * THREADS + tid];
-        const bool some = cm >= tau && cm > -INFINITY;
-        if (!__any(some)) continue;
+        if (cm >= tau && cm > -INFINITY) hit |= 1u << k;
+    }
+    while (hit) {
+        const int base = begin + __builtin_ctz(hit) * CHUNK;
+        hit &= hit - 1;
         float x[EACH + 1];
-        if (some) {
-            load(raw, base);
-            unpack(x, raw, base);
-        }
+        load(raw, base);
+        unpack(x, raw, base);
 #pragma unroll
-        for (int e = 0; e <= EACH; ++e) {
-            const bool in = some && x[e] >= tau && x[e] > -INFINITY;
-            if (__any(in)) push(in, x[e], id_of(base, e), &sm_n[1]);
-        }
+        for (int e = 0; e <= EACH; ++e)
+            if (x[e] >= tau && x[e] > -INFINITY) {
+                const int to = atomicAdd(&sm_n[1], 1);
+                if (to < LIST) {
+                    sm_v[to] = x[e];
+                    sm_i[to] = id_of(base, e);
+                }
+            }
     }
     __syncthreads();
     const int n = sm_n[1];
@@ -336,11 +349,18 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     const int t0 = lane < a.m ? a.tokens[(size_t)row * a.m + lane] : -1;
     const float x0 = t0 >= 0 && t0 < a.V ? lp_logit(a, row, t0) : NAN;
     LpSums t = {-INFINITY, 0.f, 0.f};
-    float tau = -INFINITY;  // every part's K-th best is no better than the row's
+    // At least K logits reach each of: a part's K-th best, the smallest of the parts'
+    // ceil(K / parts)-th best, and the K-th of the lanes' best.
+    const int J = (K + parts - 1) / parts;
+    float tau = -INFINITY, low = INFINITY, first = -INFINITY;
     for (int k = lane; k < parts; k += 64) {
         const float* q = rec + (size_t)k * words;
         LpSums p = {q[0], q[1], q[2]};
-        if (K > 0) tau = fmaxf(tau, q[3 + K]);
+        if (K > 0) {
+            tau = fmaxf(tau, q[3 + K]);
+            low = fminf(low, q[3 + J]);
+            first = fmaxf(first, q[4]);
+        }
         const float m = fmaxf(t.m, p.m);
         t.lift(m, c);
         p.lift(m, c);
@@ -358,7 +378,9 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
         a.logp[(size_t)row * a.m + j] = ok ? out.logp(j < 64 ? x0 : lp_logit(a, row, id), a.scale) : NAN;
     }
     if (K == 0) return;
-    tau = wave_top(tau);
+    float kth, jth;
+    lp_kth(first, K, 1, &kth, &jth);
+    tau = fmaxf(fmaxf(wave_top(tau), kth), -wave_top(-low));
     float *best = a.best + (size_t)row * K, *v = sm;
     int *ids = a.ids + (size_t)row * K, *id = (int*)(sm + ((all + 7) & ~3)), n = 0;
     for (int i0 = 0; i0 < all; i0 += AT_ONCE * 64) {
@@ -394,16 +416,18 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
 // 1024 threads: a CU reads it in less time than a second kernel takes.  Others
 // are workgroups of 256 threads: in parts, a few workgroups per CU, where there are
 // too few rows, in chunks of 2048 logits where 8192 would leave the chip empty.
-static constexpr int LP_ROWS = 512, LP_SPAN = 32;  // LP_SPAN: most chunks of a part
-static constexpr int64_t LP_ROW = 640 << 10;
+static constexpr int LP_ROWS = 512, LP_SPAN = 32;  // LP_SPAN: most chunks of a part (at most 32: bits of a word)
+static constexpr int LP_FEW = 32;
+static constexpr int64_t LP_ROW = 640 << 10, LP_SHORT = 128 << 10;
 struct LpPlan {
     int each, threads, parts, span;
 };
 static LpPlan lp_plan(int n, int V, int bf16) {
     LpPlan p;
-    const bool whole = n <= LP_ROWS && (int64_t)V * (bf16 ? 2 : 4) <= LP_ROW;
+    const int64_t bytes = (int64_t)V * (bf16 ? 2 : 4);
+    const bool whole = n <= LP_ROWS && bytes <= (n < LP_FEW ? LP_SHORT : LP_ROW);
     p.threads = whole ? 1024 : 256;
-    p.each = whole ? 16 : (int64_t)n * ((V + 8191) / 8192) >= 512 ? 32 : 8;
+    p.each = whole || (int64_t)n * ((V + 8191) / 8192) >= 512 ? 32 : 8;
     const int chunk = p.threads * p.each, chunks = (V + chunk - 1) / chunk;
     const int want = whole ? 1 : (int)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / n));
     p.span = std::min((chunks + want - 1) / want, LP_SPAN);
@@ -420,9 +444,9 @@ hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     const LpPlan p = lp_plan(a.n, a.V, a.bf16);
     const int words = lp_words(a.K);
     const dim3 grid((unsigned)a.n * p.parts);
-    auto kernel = p.each == 16   ? (a.bf16 ? k_logprob_part<true, 16, 1024> : k_logprob_part<false, 16, 1024>)
-                  : p.each == 32 ? (a.bf16 ? k_logprob_part<true, 32, 256> : k_logprob_part<false, 32, 256>)
-                                 : (a.bf16 ? k_logprob_part<true, 8, 256> : k_logprob_part<false, 8, 256>);
+    auto kernel = p.threads == 1024 ? (a.bf16 ? k_logprob_part<true, 32, 1024> : k_logprob_part<false, 32, 1024>)
+                  : p.each == 32      ? (a.bf16 ? k_logprob_part<true, 32, 256> : k_logprob_part<false, 32, 256>)
+                                      : (a.bf16 ? k_logprob_part<true, 8, 256> : k_logprob_part<false, 8, 256>);
     LogprobArgs b = a;
     int c = p.parts, sp = p.span, w = words;
     void* part_at[] = {(void*)&b, (void*)&c, (void*)&sp, (void*)&w};
