@@ -54,9 +54,14 @@ __device__ __forceinline__ int paged_page(const PagedBatch& p, int b, int tile) 
 // ---------------------------------------------------------------- append
 
 // One workgroup = one tile (32 slots) that new rows fall into, for one kv head
-// (keys and values) or for the query heads of its group.  A sequence of T rows
-// touches at most T / 32 + 2 tiles, so those of sequence b are numbered from
-// row0 / 32 + 2 b on: no sum over the sequences before it.
+// and the query heads of its group.  A sequence of T rows touches at most T / 32 +
+// 2 tiles, so those of sequence b are numbered from row0 / 32 + 2 b on: no sum
+// over the sequences before it.
+//
+// A whole tile: all loads run along the rows and are issued first, a thread's
+// angles serve its key and its queries, and the tile is put together in LDS and
+// stored 16 bytes per lane in one piece.  Another tile's few rows are stored in
+// place, a piece of 8 elements per thread.
 static constexpr int PAPP_THREADS = 256;
 
 __device__ __forceinline__ i32x4 paged_ld8(const uint16_t* p, bool vec) {
@@ -69,9 +74,7 @@ __device__ __forceinline__ i32x4 paged_ld8(const uint16_t* p, bool vec) {
 
 // The pieces x (elements d0 ..) and y (d0 + hd/2 ..) of a head row, rotated in
 // fp32 (each product's error 2^-24 of it) and rounded to bf16 once.
-__device__ __forceinline__ void paged_rotate(const float* cos, const float* sin, size_t at, bool ok, i32x4& x, i32x4& y) {
-    const f32x4 cs[2] = {*(const f32x4*)(cos + at), *(const f32x4*)(cos + at + 4)};
-    const f32x4 sn[2] = {*(const f32x4*)(sin + at), *(const f32x4*)(sin + at + 4)};
+__device__ __forceinline__ void paged_rotate(const f32x4 (&cs)[2], const f32x4 (&sn)[2], bool ok, i32x4& x, i32x4& y) {
     float lo[8], hi[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -88,81 +91,150 @@ __device__ __forceinline__ void paged_rotate(const float* cos, const float* sin,
 
 template <int HD> __global__ void __launch_bounds__(PAPP_THREADS) k_paged_append(const PagedAppendArgs a) {
     const PagedBatch& p = a.p;
-    const int lane = threadIdx.x & 63;
+    // (the heads of a tile follow each other: rows are read as a whole)
+    const int lane = threadIdx.x & 63, place = blockIdx.x / p.Hkv;
     // the last sequence whose tiles start at or before this one
     int b = -1;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int i = min(b0 + lane, p.B - 1);
-        const uint64_t in = __ballot(b0 + lane < p.B && (int64_t)(p.seq_start[i] >> 5) + 2 * i <= (int64_t)blockIdx.x);
+        const uint64_t in = __ballot(b0 + lane < p.B && (int64_t)(p.seq_start[i] >> 5) + 2 * i <= (int64_t)place);
         if (in) b = b0 + 63 - __builtin_clzll(in);
     }
     b = __builtin_amdgcn_readfirstlane(b);
     if (b < 0) return;
     const PagedSeq s = paged_seq(p, b, false);
     if (s.T == 0 || !s.fits) return;
-    const int tile = (s.first >> 5) + (int)blockIdx.x - ((s.row0 >> 5) + 2 * b);
+    const int tile = (s.first >> 5) + place - ((s.row0 >> 5) + 2 * b);
     const int lo = max(s.first, tile * 32), hi = min(s.first + s.T, tile * 32 + 32);
     if (lo >= hi) return;
     const int row = s.row0 + tile * 32 - s.first;  // of the tile's slot 0
-    auto turn = [&](int sl, int d0, i32x4& x, i32x4& y) {
-        if (!a.cos) return;
-        const int pos = a.pos ? a.pos[row + sl] : tile * 32 + sl;
-        const bool ok = pos >= 0 && pos < a.n_pos;
-        paged_rotate(a.cos, a.sin, (size_t)(ok ? pos : 0) * (HD / 2) + d0, ok, x, y);
-    };
+    const int h = blockIdx.x % p.Hkv, G = a.q ? a.H / p.Hkv : 0, tid = threadIdx.x;
+    const int pid = paged_page(p, b, tile);
+    const bool paged = (uint32_t)pid < (uint32_t)p.n_pages;  // (else nothing is stored)
+    uint16_t* kt = p.pages + ((((size_t)(paged ? pid : 0) * 2 * p.Hkv + h) << p.tshift) + (tile & ((1 << p.tshift) - 1))) * (32 * HD);
+    uint16_t* vt = kt + (((size_t)p.Hkv << p.tshift) * (32 * HD));
     constexpr int PR = HD / 16;  // pairs of pieces of a head row
-    if ((int)blockIdx.y >= p.Hkv) {  // queries
-        const int G = a.H / p.Hkv, h0 = ((int)blockIdx.y - p.Hkv) * G, n = (hi - lo) * G * PR;
-        for (int it = threadIdx.x; it < n; it += PAPP_THREADS) {
-            const int d0 = it % PR * 8, h = it / PR % G, sl = lo - tile * 32 + it / PR / G;
-            const uint16_t* from = a.q + (size_t)(row + sl) * a.ldq + (size_t)(h0 + h) * HD + d0;
-            i32x4 x = paged_ld8(from, a.vec), y = paged_ld8(from + HD / 2, a.vec);
-            turn(sl, d0, x, y);
-            uint16_t* to = a.q_out + ((size_t)(row + sl) * a.H + h0 + h) * HD + d0;
-            *(i32x4*)to = x;
-            *(i32x4*)(to + HD / 2) = y;
+    auto k_at = [&](int sl, int d0) { return a.k + (size_t)(row + sl) * a.ldk + (size_t)h * HD + d0; };
+    auto q_at = [&](int sl, int g, int d0) { return a.q + (size_t)(row + sl) * a.ldq + (size_t)(h * G + g) * HD + d0; };
+    auto v_at = [&](int sl, int d0) { return a.v + (size_t)(row + sl) * a.ldv + (size_t)h * HD + d0; };
+    auto q_to = [&](int sl, int g, int d0, const i32x4 x, const i32x4 y) {
+        uint16_t* to = a.q_out + ((size_t)(row + sl) * a.H + h * G + g) * HD + d0;
+        *(i32x4*)to = x;
+        *(i32x4*)(to + HD / 2) = y;
+    };
+    // dwords of slots s4, s4 + 1 and s4 + 2, s4 + 3 at element e of four rows' pieces
+    auto turned = [](const i32x4 (&x)[4], int e) {
+        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+        return make_uint2(__builtin_amdgcn_perm((uint32_t)x[1][e >> 1], (uint32_t)x[0][e >> 1], sel),
+                          __builtin_amdgcn_perm((uint32_t)x[3][e >> 1], (uint32_t)x[2][e >> 1], sel));
+    };
+    if (hi - lo == 32) {
+        // (every 256 bytes 16 further on: a row's pieces lie 256 bytes apart)
+        constexpr int PIECES = 32 * HD / 8;
+        __shared__ i32x4 ki[PIECES + PIECES / 16], vi[PIECES + PIECES / 16];
+        auto spread = [](int element) { return element + element / 128 * 8; };
+        constexpr int QB = 4;                                 // query heads at a time
+        const bool kq = tid < 32 * PR;                        // a pair of pieces of a slot: its key's and its queries'
+        const int vt0 = HD == 128 ? 0 : 128;                  // the threads of the values, four slots of 8 elements each
+        const bool vv = tid >= vt0 && tid < vt0 + HD;
+        const int sl = tid / PR % 32, d0 = tid % PR * 8, dv = (tid - vt0) % (HD / 8) * 8, s4 = (tid - vt0) / (HD / 8) * 4;
+        i32x4 kx, ky, v[4], qx[QB], qy[QB];
+        if (kq) {
+            kx = paged_ld8(k_at(sl, d0), a.vec);
+            ky = paged_ld8(k_at(sl, d0 + HD / 2), a.vec);
+        }
+        if (vv) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = paged_ld8(v_at(s4 + j, dv), a.vec);
+        }
+        auto load_q = [&](int g0) {
+#pragma unroll
+            for (int g = 0; g < QB; ++g)
+                if (g0 + g < G) {
+                    qx[g] = paged_ld8(q_at(sl, g0 + g, d0), a.vec);
+                    qy[g] = paged_ld8(q_at(sl, g0 + g, d0 + HD / 2), a.vec);
+                }
+        };
+        if (kq) load_q(0);
+        bool ok = false;
+        f32x4 cs[2], sn[2];
+        if (kq && a.cos) {
+            const int pos = a.pos ? a.pos[row + sl] : tile * 32 + sl;
+            ok = pos >= 0 && pos < a.n_pos;
+            const size_t at = (size_t)(ok ? pos : 0) * (HD / 2) + d0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                cs[i] = *(const f32x4*)(a.cos + at + 4 * i);
+                sn[i] = *(const f32x4*)(a.sin + at + 4 * i);
+            }
+        }
+        if (kq) {
+            if (a.cos) paged_rotate(cs, sn, ok, kx, ky);
+            *(i32x4*)((uint16_t*)ki + spread((int)kv_k_tiled(sl, d0, HD))) = kx;
+            *(i32x4*)((uint16_t*)ki + spread((int)kv_k_tiled(sl, d0 + HD / 2, HD))) = ky;
+        }
+        if (vv) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *(uint2*)((uint16_t*)vi + spread((int)kv_v_tiled(s4, dv + e, HD))) = turned(v, e);
+        }
+        if (kq) {
+            for (int g0 = 0; g0 < G; g0 += QB) {
+                if (g0) load_q(g0);
+#pragma unroll
+                for (int g = 0; g < QB; ++g)
+                    if (g0 + g < G) {
+                        if (a.cos) paged_rotate(cs, sn, ok, qx[g], qy[g]);
+                        q_to(sl, g0 + g, d0, qx[g], qy[g]);
+                    }
+            }
+        }
+        __syncthreads();
+        if (!paged) return;
+        for (int i = tid; i < PIECES; i += PAPP_THREADS) {
+            ((i32x4*)kt)[i] = ki[i + i / 16];
+            ((i32x4*)vt)[i] = vi[i + i / 16];
         }
         return;
     }
-    const int pid = paged_page(p, b, tile);
-    if ((uint32_t)pid >= (uint32_t)p.n_pages) return;
-    const int h = blockIdx.y;
-    uint16_t* kt = p.pages + ((((size_t)pid * 2 * p.Hkv + h) << p.tshift) + (tile & ((1 << p.tshift) - 1))) * (32 * HD);
-    uint16_t* vt = kt + (((size_t)p.Hkv << p.tshift) * (32 * HD));
-    const int s_lo = lo - tile * 32, s_hi = hi - tile * 32;
-    if (threadIdx.x < 128) {
-        for (int it = threadIdx.x; it < 32 * PR; it += 128) {
-            const int sl = it % 32, d0 = it / 32 * 8;
-            if (sl < s_lo || sl >= s_hi) continue;
-            const uint16_t* from = a.k + (size_t)(row + sl) * a.ldk + (size_t)h * HD + d0;
+    const int s_lo = lo - tile * 32, s_hi = hi - tile * 32, n = s_hi - s_lo;
+    const int nk = n * PR, nq = nk * G, g_lo = s_lo >> 2, nv = (((s_hi + 3) >> 2) - g_lo) * (HD / 8);
+    for (int it = tid; it < nk + nq + nv; it += PAPP_THREADS) {
+        if (it < nk + nq) {  // a pair of pieces of a key or query
+            const bool key = it < nk;
+            const int i = key ? it : it - nk, d0 = i % PR * 8, g = key ? 0 : i / PR % G, sl = s_lo + (key ? i / PR : i / PR / G);
+            const uint16_t* from = key ? k_at(sl, d0) : q_at(sl, g, d0);
             i32x4 x = paged_ld8(from, a.vec), y = paged_ld8(from + HD / 2, a.vec);
-            turn(sl, d0, x, y);
-            *(i32x4*)(kt + kv_k_tiled(sl, d0, HD)) = x;
-            *(i32x4*)(kt + kv_k_tiled(sl, d0 + HD / 2, HD)) = y;
-        }
-    } else {  // four slots of 8 elements, turned: 8 bytes of a value fragment's lane each
-        const int it = threadIdx.x - 128;
-        const int d0 = it % (HD / 8) * 8, s4 = it / (HD / 8) * 4;
-        if (it >= HD || s4 >= s_hi || s4 + 4 <= s_lo) return;
-        i32x4 x[4];
+            if (a.cos) {
+                const int pos = a.pos ? a.pos[row + sl] : tile * 32 + sl;
+                const bool ok = pos >= 0 && pos < a.n_pos;
+                const size_t at = (size_t)(ok ? pos : 0) * (HD / 2) + d0;
+                const f32x4 cs[2] = {*(const f32x4*)(a.cos + at), *(const f32x4*)(a.cos + at + 4)};
+                const f32x4 sn[2] = {*(const f32x4*)(a.sin + at), *(const f32x4*)(a.sin + at + 4)};
+                paged_rotate(cs, sn, ok, x, y);
+            }
+            if (!key) {
+                q_to(sl, g, d0, x, y);
+            } else if (paged) {
+                *(i32x4*)(kt + kv_k_tiled(sl, d0, HD)) = x;
+                *(i32x4*)(kt + kv_k_tiled(sl, d0 + HD / 2, HD)) = y;
+            }
+        } else if (paged) {  // four slots' values at 8 elements
+            const int i = it - nk - nq, d0 = i % (HD / 8) * 8, s4 = (g_lo + i / (HD / 8)) * 4;
+            i32x4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int sl = min(max(s4 + j, s_lo), s_hi - 1);
-            x[j] = paged_ld8(a.v + (size_t)(row + sl) * a.ldv + (size_t)h * HD + d0, a.vec);
-        }
-        const bool whole = s4 >= s_lo && s4 + 4 <= s_hi;
+            for (int j = 0; j < 4; ++j) x[j] = paged_ld8(v_at(min(max(s4 + j, s_lo), s_hi - 1), d0), a.vec);
+            const bool whole = s4 >= s_lo && s4 + 4 <= s_hi;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-            const uint32_t u = __builtin_amdgcn_perm((uint32_t)x[1][e >> 1], (uint32_t)x[0][e >> 1], sel);
-            const uint32_t w = __builtin_amdgcn_perm((uint32_t)x[3][e >> 1], (uint32_t)x[2][e >> 1], sel);
-            uint16_t* to = vt + kv_v_tiled(s4, d0 + e, HD);
-            if (whole) {
-                *(uint2*)to = make_uint2(u, w);
-            } else {
+            for (int e = 0; e < 8; ++e) {
+                const uint2 w = turned(x, e);
+                uint16_t* to = vt + kv_v_tiled(s4, d0 + e, HD);
+                if (whole) {
+                    *(uint2*)to = w;
+                } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (s4 + j >= s_lo && s4 + j < s_hi) to[j] = (uint16_t)((j & 2 ? w : u) >> (16 * (j & 1)));
+                    for (int j = 0; j < 4; ++j)
+                        if (s4 + j >= s_lo && s4 + j < s_hi) to[j] = (uint16_t)((j & 2 ? w.y : w.x) >> (16 * (j & 1)));
+                }
             }
         }
     }
@@ -171,7 +243,7 @@ template <int HD> __global__ void __launch_bounds__(PAPP_THREADS) k_paged_append
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
     const PagedBatch& p = a.p;
     if (p.N < 1 || p.B < 1 || p.Hkv < 1 || (a.q && a.H % p.Hkv)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)p.N / 32 + 2u * p.B, (unsigned)p.Hkv * (a.q ? 2 : 1));
+    const dim3 grid(((unsigned)p.N / 32 + 2u * p.B) * p.Hkv);
     if (p.hd == 128) return launch_checked(k_paged_append<128>, grid, PAPP_THREADS, s, a);
     if (p.hd == 64) return launch_checked(k_paged_append<64>, grid, PAPP_THREADS, s, a);
     return hipErrorInvalidValue;

@@ -1967,7 +1967,7 @@ static bool paged_batch(const cas_paged* c, int32_t H, bool arrays, PagedBatch* 
     const int64_t rows = (int64_t)c->n_rows * (H / c->n_kv_heads);  // of a kv head
     if (rows >= 1 << 24) return false;
     *st = CAS_ERR_UNSUPPORTED;
-    if ((rows / 16 + c->n_seqs + 4096) * c->n_kv_heads > INT32_MAX) return false;  // (a grid dimension)
+    if ((rows / 16 + 2 * (int64_t)c->n_seqs + 4096) * c->n_kv_heads > INT32_MAX) return false;  // (a grid dimension)
     *st = CAS_ERR_ARG;
     if (arrays) {
         if (!c->pages || !c->table || !c->seq_start || !c->ctx_len || !aligned16(c->pages)) return false;
