@@ -19,6 +19,7 @@
  * state (committed length, round rules), not numerics.
  * Exit status 0: every check passed.
  */
+#include <math.h>
 #include <stdint.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -163,6 +164,76 @@ static void host_checks(void) {
           CAS_ERR_ARG);
     CHECK(cas_op_attention_kv4(p, p, 64, INT32_MIN, p, p, INT32_MAX, 10, 1, 1, 8, 2, 64, 0, 0, (uint64_t*)p, p, p,
                                1 << 20, NULL) == CAS_ERR_ARG);
+
+    /* the paged KV cache and the log probabilities: the same */
+    cas_paged pg = {p, 10, 64, 2, 64, (int32_t*)p, 5, 3, (int32_t*)p, (int32_t*)p, NULL, 7, 0}, q;
+    float* f = (float*)p;
+    CHECK(cas_op_paged_bytes(10, 64, 2, 64) == (size_t)10 * 2 * 2 * 64 * 64 * 2);
+    CHECK(cas_op_paged_bytes(10, 48, 2, 64) == 0 && cas_op_paged_bytes(10, 16, 2, 64) == 0);
+    CHECK(cas_op_paged_bytes(10, 8192, 2, 64) == 0 && cas_op_paged_bytes(0, 64, 2, 64) == 0);
+    CHECK(cas_op_paged_bytes(10, 64, 2, 96) == 0 && cas_op_paged_bytes(10, 64, INT32_MAX, 64) == 0);
+    CHECK(cas_op_attention_paged_work_bytes(NULL, 4) == 0 && cas_op_attention_paged_work_bytes(&pg, 3) == 0);
+    CHECK(cas_op_attention_paged_work_bytes(&pg, 0) == 0);
+    q = pg; q.table_len = 1 << 14;
+    CHECK(cas_op_attention_paged_work_bytes(&q, 4) > 0);
+    q.table_len = INT32_MAX;
+    CHECK(cas_op_attention_paged_work_bytes(&q, 4) == 0);
+    CHECK(cas_op_paged_append(NULL, NULL, 0, 0, p, 128, p, 128, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, NULL, 128, p, 128, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, p, 127, p, 128, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, p, 128, p, INT64_MIN, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, p, 256, 4, p, 128, p, 128, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, p, 256, 3, p, 128, p, 128, NULL, NULL, NULL, 0, p, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, p, 512, 4, p, 128, p, 128, NULL, NULL, NULL, 0, p, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, p, 128, p, 128, NULL, f, NULL, 4, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, p, 128, p, 128, NULL, f, f, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_paged_append(&pg, NULL, 0, 0, p, 128, p, 128, NULL, f + 1, f, 4, NULL, NULL) == CAS_ERR_ARG);
+    for (int i = 0; i < 12; i++) {
+        q = pg;
+        switch (i) {
+        case 0: q.pages = NULL; break;
+        case 1: q.table = NULL; break;
+        case 2: q.seq_start = NULL; break;
+        case 3: q.ctx_len = NULL; break;
+        case 4: q.n_seqs = 0; break;
+        case 5: q.n_rows = 0; break;
+        case 6: q.max_rows = -1; break;
+        case 7: q.table_len = 0; break;
+        case 8: q.n_rows = 1 << 24; break;
+        case 9: q.n_seqs = INT32_MAX; break;
+        case 10: q.pages = (char*)p + 8; break;
+        default: q.table = (int32_t*)((char*)p + 2); break;
+        }
+        CHECK(cas_op_paged_append(&q, NULL, 0, 0, p, 128, p, 128, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+        CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, p, 1 << 30, NULL) == CAS_ERR_ARG);
+    }
+    q = pg; q.n_kv_heads = 4096; q.n_seqs = 65536; q.n_rows = (1 << 24) - 1;
+    CHECK(cas_op_attention_paged(&q, p, 4096, NULL, 0, 0, p, p, 1 << 30, NULL) == CAS_ERR_UNSUPPORTED);
+    q = pg; q.head_dim = 80;
+    CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, p, 1 << 30, NULL) == CAS_ERR_UNSUPPORTED);
+    CHECK(cas_op_attention_paged(&pg, NULL, 4, NULL, 0, 0, p, NULL, 0, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_attention_paged(&pg, p, 4, NULL, -1, 0, p, NULL, 0, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_attention_paged(&pg, p, 4, NULL, 0, INT32_MIN, p, NULL, 0, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_attention_paged(&pg, p, 4, (uint64_t*)((char*)p + 4), 0, 0, p, NULL, 0, NULL) == CAS_ERR_ARG);
+    q = pg; q.table_len = 1 << 14;
+    CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, p, cas_op_attention_paged_work_bytes(&q, 4) - 1, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, NULL, 1 << 30, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs_work_bytes(3, 32000, 5) > 0);
+    CHECK(cas_op_logprobs_work_bytes(0, 32000, 5) == 0 && cas_op_logprobs_work_bytes(3, (1 << 20) + 1, 5) == 0);
+    CHECK(cas_op_logprobs_work_bytes(3, 32000, 33) == 0 && cas_op_logprobs_work_bytes(INT32_MAX, 1 << 20, 0) == 0);
+    CHECK(cas_op_logprobs(CAS_W_I8, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) ==
+          CAS_ERR_UNSUPPORTED);
+    CHECK(cas_op_logprobs(CAS_W_F32, NULL, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 99, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 0.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, NAN, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, INFINITY, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 1, f, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 2, NULL, f, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 0, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, (char*)p + 2, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) ==
+          CAS_ERR_ARG);
+    CHECK(cas_logprobs(NULL, 1, 1.f, NULL, 0, NULL, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
 }
 
 /* ------------------------------------------------------------ part 2: on a device */
@@ -274,6 +345,13 @@ static void error_paths(cas_ctx* c, const shape_t* s) {
     CHECK(cas_topk(c, 4, 0, ids, probs) == CAS_ERR_ARG);
     CHECK(cas_topk(c, 4, 17, ids, probs) == CAS_ERR_ARG);
     CHECK(cas_topk(c, 4, 2, NULL, probs) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 3, 1.f, ids, 2, probs, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 1.f, ids, 129, probs, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 1.f, ids, -1, probs, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 1.f, NULL, 2, probs, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 1.f, NULL, 0, NULL, NULL, 33, ids, probs) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 1.f, NULL, 0, NULL, NULL, 2, ids, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, -1.f, NULL, 0, NULL, probs, 0, NULL, NULL) == CAS_ERR_ARG);
     CHECK(cas_logits_device(c, NULL, &na) == CAS_ERR_ARG);
     CHECK(committed(c) == Lc);
     OK(c, cas_set_committed(c, Lc));
@@ -373,6 +451,9 @@ static void run_model(const shape_t* s) {
         CHECK(dl != NULL && rows == n);
         OK(c, cas_topk(c, n, 3, ids, probs));
         for (int i = 0; i < n * 3; i++) CHECK(ids[i] >= -1 && ids[i] < s->V && probs[i] >= 0.f && probs[i] <= 1.f);
+        OK(c, cas_logprobs(c, n, 1.f, tok, 1, probs, r % 3 ? probs + n : NULL, r % 2 ? 2 : 0, ids, probs + 2 * n));
+        for (int i = 0; i < n; i++) CHECK(probs[i] <= 1e-5f && (r % 3 == 0 || probs[n + i] >= -1e-5f));
+        for (int i = 0; i < (r % 2 ? 2 * n : 0); i++) CHECK(ids[i] >= 0 && ids[i] < s->V && probs[2 * n + i] <= 1e-5f);
         OK(c, cas_accept_tree(c, 1, acc, &na, &bonus));
         CHECK(na >= 1 && na <= n && acc[0] == 0 && bonus >= 0 && bonus < s->V);
         for (int j = 1; j < na; j++) CHECK(par[acc[j]] == acc[j - 1]);

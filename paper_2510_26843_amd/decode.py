@@ -1,5 +1,6 @@
-"""Host decoding loops over the library: plain greedy decoding and greedy
-speculative decoding with a static token tree drafted by DSIA levels.
+"""Host decoding loops over the library: plain greedy decoding, greedy
+speculative decoding with a static token tree drafted by DSIA levels, and
+scoring of a given text.
 
 Routing (which draft level fills which tree depth, how many children a node
 gets) is host logic; every forward, the acceptance and the KV commit run in
@@ -33,6 +34,23 @@ def ar_decode(model: Model, prompt: Sequence[int], n_new: int) -> List[int]:
         out.append(bonus)
         root = bonus
     return out
+
+
+def score(model: Model, tokens: Sequence[int], K: int = 0, scale: float = 1.0):
+    """Log probability of every token of a text but its first, given those
+    before it: (logp [n - 1], entropy [n - 1], top ids [n - 1][K], their log
+    probabilities).  The text is committed, a chain of up to max_tree tokens per
+    forward, whose rows are scored on the device."""
+    t = np.ascontiguousarray(tokens, dtype=np.int32)
+    model.set_committed(0)
+    parts = []
+    for a in range(0, len(t), model.max_tree):
+        n = min(model.max_tree, len(t) - a)
+        model.forward(t[a:a + n], range(-1, n - 1), 0, logits=False)
+        model.compact(range(n))
+        given = np.append(t[a + 1:a + n + 1], [-1] * (a + n + 1 - len(t)))  # (nothing follows the last token)
+        parts.append(model.logprobs(given, K, scale))
+    return tuple(np.concatenate(p)[:-1] for p in zip(*parts))
 
 
 def cas_decode_static(model: Model, prompt: Sequence[int], n_new: int, tree_parents: Sequence[int],

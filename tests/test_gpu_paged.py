@@ -392,3 +392,60 @@ def test_as_the_contiguous_attention():
     see = P.visible(17, 500, 0, c.masks[0], 0, 0)
     _, err = P.attention(c.q, *c.kv[0], see)
     assert (np.abs(_np(out) - _np(c.run())).reshape(err.shape) <= 2 * err).all()
+
+
+def test_a_serving_step():
+    """Three conversations through one layer: their prompts' chunks, then steps of a
+    token each, chosen among the top alternatives.  Every call against its
+    definition on what the calls before it left."""
+    H, Hkv, hd, V, page = 8, 2, 64, 1000, 32
+    d, w = H * hd, (H + 2 * Hkv) * hd
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    embed, wqkv, head = (torch.randn(s, generator=g, device="cuda") for s in ((V, d), (d, w), (d, V)))
+    cos, sin = _rope(hd, 200)
+    dcos, dsin = torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV)
+    table = _rng(9).permutation(12).reshape(3, 4).astype(np.int32)
+    pages = torch.full((12, 2, Hkv, page * hd), float("nan"), dtype=torch.bfloat16, device=DEV)
+    texts = [list(_rng(9, b).integers(0, V, n)) for b, n in enumerate((37, 1, 64))]
+    past = [0, 0, 0]
+    kp, vp = P.key_places(hd), P.value_places(hd)
+    for step in range(5):
+        rows = [t[c:] for t, c in zip(texts, past)]
+        n = [len(r) for r in rows]
+        ids = np.concatenate(rows).astype(np.int64)
+        x = (embed[torch.from_numpy(ids).to(DEV)] @ wqkv * d**-0.5).to(torch.bfloat16)
+        start = np.concatenate([[0], np.cumsum(n)])
+        cache = cas.Paged(pages, page, hd, _i32(table), _i32(start), _i32(past), len(ids), max(n))
+        q = torch.empty((len(ids), H, hd), dtype=torch.bfloat16, device=DEV)
+        o = torch.empty((len(ids), d), dtype=torch.bfloat16, device=DEV)
+        cas.op_paged_append(cache, x[:, d : d + Hkv * hd], x[:, d + Hkv * hd :], q=x[:, :d], q_out=q, cos=dcos, sin=dsin)
+        cas.op_attention_paged(cache, q, o)
+        last = torch.from_numpy(start[1:] - 1).to(DEV)
+        logits = o[last].float() @ head * (4 * d**-0.5)
+        logp, entropy = torch.empty((3, 1), device=DEV), torch.empty(3, device=DEV)
+        top, best = torch.empty((3, 5), dtype=torch.int32, device=DEV), torch.empty((3, 5), device=DEV)
+        cas.op_logprobs(logits, _i32([[7], [8], [9]]), logp, entropy, top, best)
+        got_q, got_o, pool, xs = _np(q), _np(o).reshape(-1, H, hd), _np(pages), _np(x)
+        for b in range(3):
+            r, slots = slice(start[b], start[b + 1]), np.arange(past[b], past[b] + n[b])
+            for new, h0, h1, got in ((got_q[r], 0, H, None), (None, H, H + Hkv, "k")):
+                raw = xs[r].reshape(n[b], -1, hd)[:, h0:h1]
+                ref = P.rotate(raw, cos, sin, slots)
+                if got:
+                    new = np.stack([pool[table[b, s // page], 0][:, kp[s % 32]] for s in slots])
+                assert (np.abs(new - ref) <= P.rotate_bound(raw, ref)).all(), (step, b)
+            every = np.arange(past[b] + n[b])
+            k = np.stack([pool[table[b, s // page], 0][:, kp[s % 32]] for s in every], 1)
+            v = np.stack([pool[table[b, s // page], 1][:, vp[s % 32]] for s in every], 1)
+            assert np.array_equal(v[:, slots].transpose(1, 0, 2), xs[r].reshape(n[b], -1, hd)[:, H + Hkv :])
+            ref, err = P.attention(got_q[r], k, v, P.visible(n[b], past[b], 0, None, 0, 0))
+            assert (np.abs(got_o[r] - ref) <= err).all(), (step, b)
+        y = _np(logits)
+        lp = y - y.max(1, keepdims=True)
+        lp -= np.log(np.exp(lp).sum(1, keepdims=True))
+        assert np.array_equal(top.cpu().numpy(), np.argsort(-y, axis=1, kind="stable")[:, :5])
+        assert np.abs(_np(best) - np.take_along_axis(lp, top.cpu().numpy().astype(np.int64), 1)).max() < 1e-5
+        assert np.abs(_np(logp)[:, 0] - lp[[0, 1, 2], [7, 8, 9]]).max() < 1e-5
+        past = [len(t) for t in texts]
+        texts = [t + [int(top[b, step])] for b, t in enumerate(texts)]
