@@ -698,7 +698,10 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         // scores, y: the next one's, t: a lane's largest of x, and then of y.  The
         // keys are read first, the values under them; the next tile's scores run
         // under this one's exponentials, its largest scores are taken under the
-        // product with the values.
+        // product with the values.  The scores and exponentials go before the product of
+        // the other workgroup's wave (2048 rows behind 6001 slots 225 -> 211 us: the
+        // waves of a SIMD fall out of step, one's exponentials under the other's
+        // products).
         auto turn = [&](f32x4 (&x)[JT][2], f32x4 (&y)[JT][2], float (&t)[JT], int i, bool last) {
             const i32x4* k = sk + ((uint32_t)(i + 1) % D) * (NDT * 64) + lane;
             const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
@@ -716,6 +719,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
 #pragma unroll
             for (int f = 0; f < NDT; ++f) vf[f] = v[f * 64];
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int u = 0; u < UD; ++u)
 #pragma unroll
@@ -735,6 +739,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             // (here: a scalar load in flight makes every LDS read's wait one for all of them)
             if (last) look_up(i + 1);
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
             const int one = 0x3f803f80;
 #pragma unroll
             for (int j = 0; j < JT; ++j) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
