@@ -846,11 +846,11 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
 
 // The join of the shares of split units: hd / 4 threads per row and group; the
 // groups take a row each, or with many shares up to eight take every eighth
-// share of a row, four at a time, and join through LDS.  One large workgroup per
-// unit: most find nothing to do, and each has to look (paged_share; with eight
-// workgroups of 256 threads per unit, of which a 2048-row chunk's 512 need
-// none, this kernel took 8 us, with 64 of them 36).
-static constexpr int PMERGE_THREADS = 1024;
+// share of a row, four at a time, and join through LDS.  Bound by latency: each
+// workgroup sums the sequences' lengths (paged_share), then reads its rows once.
+// Small workgroups, a unit's over y: with 1024 threads each, units of 16 rows
+// took a microsecond more, and 15 shares of 128 rows 3 us more.
+static constexpr int PMERGE_THREADS = 256;
 template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merge(const PagedAttnArgs a, int R) {
     constexpr int D4 = HD / 4, NG = PMERGE_THREADS / D4;
     __shared__ float2 sm_ml[NG];
@@ -926,8 +926,11 @@ template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const 
                                : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);
     if (e != hipSuccess || q.target == 0) return e;
     const unsigned units = (unsigned)std::min(q.units, q.target);
-    // (several per unit where a unit is 128 rows and there are few of them)
-    const unsigned y = q.R == PROWS_R ? std::max(1u, std::min(16u, 1024u / (units * p.Hkv))) : 1u;
+    // As many workgroups as the chip holds by half, where the units are few (most of
+    // the bound may find nothing to do, and each has to look: with 64 for each of
+    // 512 units this kernel took 36 us); four for 128 rows, where they are many (one:
+    // 80 us instead of 72 for a chunk of 509 rows among 8 decoding sequences).
+    const unsigned y = std::max(q.R == PROWS_R ? 4u : 1u, std::min(std::min(32u, (unsigned)q.R), 1024u / (units * p.Hkv)));
     return launch_checked(k_paged_merge<HD>, dim3(units * p.Hkv, y), PMERGE_THREADS, s, a, q.R);
 }
 
