@@ -672,27 +672,35 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         };
         // A tile that some row of the wave does not see whole: the scores of unseen slots
         // go to -infinity.  True if a value is not finite: a probability of 0 would not
-        // hide it.  (Kept short, as the tiles at the ends of a walk run it cold: with
-        // a step of its own for them, of 900 instructions, such a tile took 2 us.)
+        // hide it (then the products of the values with zeros are NaN).
         uint32_t vm[JT];
         auto hide = [&](f32x4 (&x)[JT][2], float (&t)[JT], const i32x4 (&vf)[NDT], int i) {
+            f32x4 z[2] = {};
+#pragma unroll
+            for (int f = 0; f < NDT; ++f) z[f & 1] = mfma_step<ET_BF16>(vf[f], i32x4{0, 0, 0, 0}, z[f & 1]);
             const int tile = tile_at(i);
-            const bool ok = !strange || (uint32_t)paged_page(p, s.b, tile) < (uint32_t)p.n_pages;
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
                 vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[j][e >> 2][e & 3] = (vm[j] >> e) & 1u ? ok ? x[j][e >> 2][e & 3] : NAN : -INFINITY;
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)vm[j], e, 1);
+                    x[j][e >> 2][e & 3] = __uint_as_float((__float_as_uint(x[j][e >> 2][e & 3]) & m) | (0xff800000u & ~m));
+                }
+            }
+            if (strange && (uint32_t)paged_page(p, s.b, tile) >= (uint32_t)p.n_pages) {
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    asm volatile("" : "+v"(vm[j]));  // (no 16 conditions kept from here on)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((vm[j] >> e) & 1u) x[j][e >> 2][e & 3] = NAN;
+                }
             }
             tops(t, x);
-            uint16x2 most = {0, 0};
-#pragma unroll
-            for (int f = 0; f < NDT; ++f)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    most = __builtin_elementwise_max(most, __builtin_bit_cast(uint16x2, (uint32_t)vf[f][w] & 0x7fff7fffu));
-            return (bool)__any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
+            mfma_result_pad();
+            const f32x4 y = z[0] + z[1];
+            return (bool)__any(y[0] + y[1] + y[2] + y[3] != 0.f);
         };
         // A whole tile: attn_step with the order of its instructions laid down.  x: its
         // scores, y: the next one's, t: a lane's largest of x, and then of y.  The
@@ -771,33 +779,46 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
 #pragma unroll
                 for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
             }
-            i32x4 P[JT], seen[JT];
+            i32x4 P[JT];
             const int one = 0x3f803f80;
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
                 attn_probs(P[j], S[j], st[j].m * c, c);
                 st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    seen[j][w] = (int)(((vm[j] >> (2 * w)) & 1u ? 0x3f80u : 0u) | ((vm[j] >> (2 * w + 1)) & 1u ? 0x3f800000u : 0u));
             }
+            if (!odd) {
 #pragma unroll
-            for (int f = 0; f < NDT; ++f) {
-                if (odd) {  // values that are not finite: taken out, and given back as NaN to the rows that see them
+                for (int f = 0; f < NDT; ++f)
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+            }
+            mfma_result_pad();
+            if (odd) {  // values that are not finite: taken out, and given back as NaN to the rows that see them
+                i32x4 seen[JT];
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    asm volatile("" : "+v"(vm[j]));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        seen[j][w] = (int)(((vm[j] >> (2 * w)) & 1u ? 0x3f80u : 0u) | ((vm[j] >> (2 * w + 1)) & 1u ? 0x3f800000u : 0u));
+                }
+#pragma unroll
+                for (int f = 0; f < NDT; ++f) {
                     const i32x4 bad = take_nonfinite(vf[f]);
 #pragma unroll
                     for (int j = 0; j < JT; ++j) {
                         const f32x4 n = mfma_step<ET_BF16>(bad, seen[j], f32x4{0.f, 0.f, 0.f, 0.f});
+                        st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
                         mfma_result_pad();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n[e] > 0.f) st[j].O[f][e] = NAN;
+                        for (int e = 0; e < 4; ++e) {
+                            float to = n[e] > 0.f ? NAN : 0.f;
+                            asm volatile("" : "+v"(to));  // (here, not as 64 conditions at the end)
+                            st[j].O[f][e] += to;
+                        }
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
             }
-            mfma_result_pad();
         };
         // two tiles that every row of the workgroup sees whole
         auto plain = [&](int i) { return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !strange; };
