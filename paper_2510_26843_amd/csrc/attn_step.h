@@ -102,9 +102,24 @@ __device__ __forceinline__ i32x4 take_nonfinite(i32x4& v) {
     return f;
 }
 
-// Takes a row's reference score to its largest one, where that moves it (mt: a
-// lane's largest of a tile; other rows' scores do not move it).
-template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st, float mt, float c);
+// Takes a row's reference score to its largest one (mt: a lane's largest of a
+// tile), where that passes it by ATTN_SLACK (in log2 units): probabilities are
+// then at most 2^ATTN_SLACK, which neither bf16 nor the fp32 sums mind, and the
+// rescaling of O leaves most tiles' path.  The reference scales the
+// probabilities before their rounding, so it takes the row's own scores only:
+// what a row gives does not hang on its neighbours.
+static constexpr float ATTN_SLACK = 8.f;
+template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st, float mt, float c) {
+    const float mr = pair_max32(pair_max16(mt));
+    const float mn = mr > st.top ? mr : st.m;
+    const float f = __builtin_amdgcn_exp2f((st.m - mn) * c);
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) st.O[dt] *= f;
+    st.m = mn;
+    st.top = mn + ATTN_SLACK / c;
+}
+
 // The probabilities of a tile's scores (mc: the scaled reference), as the B operand of P V.
 __device__ __forceinline__ void attn_probs(i32x4& P, const f32x4 (&S)[2], float mc, float c) {
 #pragma unroll
@@ -120,23 +135,7 @@ __device__ __forceinline__ void attn_probs(i32x4& P, const f32x4 (&S)[2], float 
 // its MFMA run while this one's probabilities and values are converted.
 // MASKED: vm has the visibility of the lane's 8 slots to its row of each query
 // tile; CARE: values of unseen slots may not be finite.
-// A row's maximum follows its scores only where one passes it by ATTN_SLACK (in
-// log2 units): probabilities are then at most 2^ATTN_SLACK, which neither bf16
-// nor the fp32 sums mind, and the rescaling of O leaves most tiles' path.  The
-// maximum scales the probabilities before their rounding, so it takes the
-// row's own scores only: what a row gives does not hang on its neighbours.  The
-// sum of the (rounded) probabilities is one more row of the PV product.
-static constexpr float ATTN_SLACK = 8.f;
-template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st, float mt, float c) {
-    const float mr = pair_max32(pair_max16(mt));
-    const float mn = mr > st.top ? mr : st.m;
-    const float f = __builtin_amdgcn_exp2f((st.m - mn) * c);
-    st.l *= f;
-#pragma unroll
-    for (int dt = 0; dt < HD / 16; ++dt) st.O[dt] *= f;
-    st.m = mn;
-    st.top = mn + ATTN_SLACK / c;
-}
+// The sum of the (rounded) probabilities is one more row of the PV product.
 template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
 __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
                                          const uint32_t (&vm)[JT], NF next) {
@@ -159,28 +158,13 @@ __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
     if (__any(grow)) {
         mfma_result_pad();
 #pragma unroll
-        for (int j = 0; j < JT; ++j) {
-            const float mr = pair_max32(pair_max16(mt[j]));
-            const float mn = mr > st[j].top ? mr : st[j].m;  // (other rows' scores do not move it)
-            const float f = __builtin_amdgcn_exp2f((st[j].m - mn) * c);
-            st[j].l *= f;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) st[j].O[dt] *= f;
-            st[j].m = mn;
-            st[j].top = mn + ATTN_SLACK / c;
-        }
+        for (int j = 0; j < JT; ++j) attn_follow(st[j], mt[j], c);
     }
     next();
     i32x4 P[JT];
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
-        const float mc = st[j].m * c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1)], c, -mc));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(S[j][i >> 1][2 * (i & 1) + 1], c, -mc));
-            P[j][i] = (int)pack_bf(p0, p1);
-        }
+        attn_probs(P[j], S[j], st[j].m * c, c);
         const int one = 0x3f803f80;
         st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
     }
