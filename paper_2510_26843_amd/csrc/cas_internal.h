@@ -349,7 +349,7 @@ struct PagedAttnArgs {
     int H, sink, window;
     float *part_o, *part_ml;  // partial states of the shares of split units
     // set by the launch
-    int G, target, least, fold;
+    int G, target, least, single, fold;
     uint32_t inv_G;
 };
 // How a call is launched: rows of a query tile, the most units of a kv head, the

@@ -319,7 +319,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
     auto seq = [&](int b) {
         Seq q;
         q.s = paged_seq(p, b, tree);
-        q.nq = (int)(((int64_t)q.s.T * G + R - 1) / R);
+        q.nq = (int)(((int64_t)q.s.T * G + R - 1) >> __builtin_ctz(R));
         q.tiles = !q.s.fits || q.s.T == 0 ? 0 : (q.s.n_slots() + 31) >> 5;
         if (a.window > 0) {  // (the most that one of its query tiles walks)
             const int t = tree ? q.s.n_slots() - q.s.Lc : min(q.s.T, R / G + 2);
@@ -341,7 +341,10 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         nq = wave_total<int>(nq);
         w = wave_total<double>(w);
         most = wave_most(most);
-        auto share = [&](int n) { return max(a.least, (int)fmin(1073741824.0, ceil(w / n))); };
+        // (w / n rounded up, or a little more: never below it, as the bounds need)
+        auto share = [&](int n) {
+            return max(a.least, (int)fminf(1073741824.f, ceilf((float)w * __builtin_amdgcn_rcpf((float)n) * 1.000001f)));
+        };
         C = share(a.target);
         // (with room left by the units: as many shares as run at once, if the longest is
         // then no longer than two rounds of the finer shares)
@@ -349,13 +352,22 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
             const int D = share(a.target - nq);
             if (min(D, most) <= 2 * C) C = D;
         }
+        // Where a workgroup has its CU to itself a tile takes it 0.57 us, where two
+        // share one 0.87; the partial states of twice the shares cost 5 us more.
+        if (nq < a.single) {
+            const int A = share(a.single - nq);
+            auto longest = [&](int c) { return (float)most * __builtin_amdgcn_rcpf(ceilf((float)most * __builtin_amdgcn_rcpf((float)c))); };
+            if (0.57f * longest(A) <= 0.87f * longest(C) + 5.f) C = A;
+        }
     }
+    const float rC = __builtin_amdgcn_rcpf((float)C);
     PagedShare r;
     r.found = false;
     int before = 0, parts = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const Seq q = b0 ? seq(b0 + lane) : own;
-        const int ns = max((q.tiles + C - 1) / C, 1);
+        int ns = max((int)((float)q.tiles * rC), 1);  // (never above the quotient rounded up)
+        ns += (int64_t)ns * C < q.tiles ? 1 : 0;
         int n = MERGE ? (ns > 1 ? q.nq : 0) : q.nq * ns, np = ns > 1 ? q.nq * ns : 0;
         const int n_own = n, np_own = np;
         n = wave_scan(n);
@@ -925,16 +937,26 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
 }
 
 // Packed rows of a unit, the shares aimed at and the least tiles of one.
-static constexpr int PAGED_CUS = 256, PAGED_LEAST = 16;
+// 16, 32 or 128 rows.  The caches of 8 sequences at 4000 slots, 32 heads read by 16
+// rows a head: 102 us at 16 as at 128; by 48 rows: 117 at 32, 108 at 128, since the
+// keys and values go to every 32 rows again.  But where the units of 32 rows leave
+// CUs free, the wave that has one key tile in eight is done sooner (64 rows on one
+// sequence of 4000 slots, 8 heads: 14 us at 32, 19 at 128).
+// Least: a share of 32 tiles on 16 rows (one of 1000 slots 8 us, in two shares 9.6),
+// of 8 on more (32 rows at 1000 slots 12.4 us, at least 16 tiles 13.9, 32 tiles 14.6).
+// Sequences that no share of 16 tiles would split are not worth a second kernel that
+// looks for split ones (2.6 us).
+static constexpr int PAGED_CUS = 256;
 
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     PagedPlan q;
     const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
-    q.R = most <= 16 ? 16 : most <= 32 ? 32 : PROWS_R;
+    const bool few = ((int64_t)p.N * (H / p.Hkv) / 32 + p.B) * p.Hkv <= PAGED_CUS;
+    q.R = most <= 16 ? 16 : most <= 32 || (most <= 64 && few) ? 32 : PROWS_R;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
     q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
-    q.least = PAGED_LEAST;
-    if ((p.cap >> 5) <= q.least) q.target = 0;  // no sequence can be split
+    q.least = q.R == 16 ? 32 : 8;
+    if ((p.cap >> 5) <= (q.R == 16 ? 32 : 16)) q.target = 0;  // no sequence is split
     q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
     return q;
 }
@@ -963,6 +985,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q,
     // (multiplying by it and taking the high word divides exactly below 2^25)
     a.inv_G = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.target = q.target;
+    a.single = q.R == PROWS_R ? (PAGED_CUS + p.Hkv - 1) / p.Hkv : 0;
     a.least = q.least;
     a.fold = (int64_t)(q.units - p.B) * p.Hkv <= 2 * PAGED_CUS;
     a.part_ml = a.part_o + (size_t)2 * q.target * p.Hkv * q.R * p.hd;
