@@ -328,6 +328,20 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         return q;
     };
     const Seq own = seq(lane);
+    // tiles / C rounded up, or one less where that is a hair above a whole number
+    auto parts_of = [](int tiles, int C, float rC) {
+        const int ns = max((int)((float)tiles * rC), 1);
+        return ns + ((int64_t)ns * C < tiles ? 1 : 0);
+    };
+    auto shares_of = [&](int C) {
+        const float rC = __builtin_amdgcn_rcpf((float)C);
+        int n = own.nq * parts_of(own.tiles, C, rC);
+        for (int b0 = 64; b0 < p.B; b0 += 64) {
+            const Seq q = seq(b0 + lane);
+            n += q.nq * parts_of(q.tiles, C, rC);
+        }
+        return wave_total<int>(n);
+    };
     int C = 1 << 30;
     if (a.target > 0) {
         int nq = own.nq, most = own.tiles;
@@ -346,11 +360,14 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
             return max(a.least, (int)fminf(1073741824.f, ceilf((float)w * __builtin_amdgcn_rcpf((float)n) * 1.000001f)));
         };
         C = share(a.target);
-        // (with room left by the units: as many shares as run at once, if the longest is
-        // then no longer than two rounds of the finer shares)
+        // With room left by the units: as many shares as run at once, if the longest is
+        // then no longer than two rounds of the finer ones.  On 32 rows only if the
+        // finer ones do not run at once (64 rows, 8 sequences at 16000 slots, 8 heads:
+        // unsplit 160 us, in halves 109); on 16 a share too many costs more than a
+        // CU left over (8 sequences at 4095: three shares each 26 us, four 28).
         if (nq < a.target) {
             const int D = share(a.target - nq);
-            if (min(D, most) <= 2 * C) C = D;
+            if (min(D, most) <= 2 * C && (R != 32 || shares_of(C) > a.target)) C = D;
         }
         // Where a workgroup has its CU to itself a tile takes it 0.57 us, where two
         // share one 0.87; the partial states of twice the shares cost 5 us more.
@@ -366,8 +383,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
     int before = 0, parts = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const Seq q = b0 ? seq(b0 + lane) : own;
-        int ns = max((int)((float)q.tiles * rC), 1);  // (never above the quotient rounded up)
-        ns += (int64_t)ns * C < q.tiles ? 1 : 0;
+        const int ns = parts_of(q.tiles, C, rC);
         int n = MERGE ? (ns > 1 ? q.nq : 0) : q.nq * ns, np = ns > 1 ? q.nq * ns : 0;
         const int n_own = n, np_own = np;
         n = wave_scan(n);
@@ -937,11 +953,12 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
 }
 
 // Packed rows of a unit, the shares aimed at and the least tiles of one.
-// 16, 32 or 128 rows.  The caches of 8 sequences at 4000 slots, 32 heads read by 16
-// rows a head: 102 us at 16 as at 128; by 48 rows: 117 at 32, 108 at 128, since the
-// keys and values go to every 32 rows again.  But where the units of 32 rows leave
-// CUs free, the wave that has one key tile in eight is done sooner (64 rows on one
-// sequence of 4000 slots, 8 heads: 14 us at 32, 19 at 128).
+// 16, 32 or 128 rows.  The caches of 8 sequences at 4000 slots, 32 heads, read by 48
+// rows: 117 us in units of 32, 108 of 128, since the keys and values go to every 32
+// rows again.  But where the units of 32 rows leave CUs free, a workgroup of eight
+// waves, each with every eighth key tile, is done sooner: 64 rows on one sequence of
+// 4000 slots, 8 heads, 14 us of 32 and 19 of 128, at 64000 slots 48 and 57; 256 rows
+// at 1000 slots 14 and 17, at 8000 22 and 27, at 64000 97 and 87.
 // Least: a share of 32 tiles on 16 rows (one of 1000 slots 8 us, in two shares 9.6),
 // of 8 on more (32 rows at 1000 slots 12.4 us, at least 16 tiles 13.9, 32 tiles 14.6).
 // Sequences that no share of 16 tiles would split are not worth a second kernel that
@@ -952,7 +969,7 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     PagedPlan q;
     const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
     const bool few = ((int64_t)p.N * (H / p.Hkv) / 32 + p.B) * p.Hkv <= PAGED_CUS;
-    q.R = most <= 16 ? 16 : most <= 32 || (most <= 64 && few) ? 32 : PROWS_R;
+    q.R = most <= 16 ? 16 : most <= 32 || (few && (most <= 64 || p.cap <= 8192)) ? 32 : PROWS_R;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
     q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
     q.least = q.R == 16 ? 32 : 8;
