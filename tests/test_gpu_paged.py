@@ -51,13 +51,15 @@ class _Batch:
     values, in pages of a shuffled pool.  Everything no row may see holds NaN:
     free pages, slots past a sequence's, and the table past its pages."""
 
+    slots = 0  # the least length of a table
+
     def __init__(self, seqs, H, Hkv, hd, page=32, tree=False, sink=0, window=0, std=1.28, spare_rows=0, seed=0):
         r = _rng(H, hd, page, seed, *[x for s in seqs for x in s])
         self.seqs, self.H, self.Hkv, self.hd, self.page = seqs, H, Hkv, hd, page
         self.sink, self.window = sink, window
         need = [-(-sum(s) // page) if s[0] else -(-s[1] // page) for s in seqs]
         n_pages = sum(need) + 2
-        ids, width = r.permutation(n_pages), max(need + [1]) + 1
+        ids, width = r.permutation(n_pages), max(need + [1, -(-self.slots // page)]) + 1
         self.table = np.full((len(seqs), width), -7, np.int32)
         self.pool = np.full((n_pages, 2, Hkv, page * hd), np.nan)
         self.kv, at = [], 0
@@ -105,6 +107,12 @@ class _Batch:
             assert np.isfinite(got[rows]).all() and over.max() <= 1, (b, np.isfinite(got[rows]).all(), over.max())
 
 
+@pytest.fixture(params=[0, 8193], ids=["short table", "long table"])
+def table(request, monkeypatch):
+    """Few rows go 32 to a unit where no sequence can be long, 128 to one where one can."""
+    monkeypatch.setattr(_Batch, "slots", request.param)
+
+
 HEADS = [(8, 2, 64), (4, 4, 128), (8, 1, 128), (6, 2, 64), (10, 2, 128)]
 BATCHES = {
     "one token": [(1, 0, 0)],
@@ -117,6 +125,7 @@ BATCHES = {
 }
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("H,Hkv,hd", HEADS)
 @pytest.mark.parametrize("seqs", BATCHES.values(), ids=BATCHES)
 def test_causal(H, Hkv, hd, seqs):
@@ -125,6 +134,7 @@ def test_causal(H, Hkv, hd, seqs):
     c.check(c.run(max_rows=max(c.rows)))
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("H,Hkv,hd", HEADS[:3])
 @pytest.mark.parametrize("seqs", [[(1, 0, 0)], [(1, 31, 3), (4, 64, 60), (128, 40, 0)], [(61, 300, 0), (0, 9, 0), (7, 5, 121)],
                                   [(32, 97, 0), (32, 0, 0), (15, 700, 17), (16, 33, 0)]])
@@ -134,6 +144,7 @@ def test_trees(H, Hkv, hd, seqs):
     c.check(c.run(max_rows=max(c.rows)))
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("H,Hkv,hd", HEADS[:2])
 @pytest.mark.parametrize("tree", [False, True])
 @pytest.mark.parametrize("sink,window", [(4, 64), (0, 1), (100, 33), (33, 3), (0, 500), (5000, 7), (2**31 - 1, 1), (4, 2**31 - 1)])
@@ -142,12 +153,14 @@ def test_window(H, Hkv, hd, tree, sink, window):
     c.check(c.run())
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("page", [32, 128, 1024, 4096])
 def test_page_sizes(page):
     c = _Batch([(1, 1500, 0), (40, 1000, 0), (1, 33, 0)], 8, 2, 64, page=page)
     c.check(c.run())
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("H,Hkv,hd", [(8, 1, 128), (4, 2, 64), (4, 4, 128)])
 @pytest.mark.parametrize("seqs", [[(1, 20001, 0)], [(1, 9000, 0), (1, 40, 0), (2, 3000, 0)], [(40, 6000, 0), (1, 5000, 0)]],
                          ids=["one", "ragged", "chunk"])
@@ -160,6 +173,7 @@ def test_split(H, Hkv, hd, seqs):
     assert torch.equal(first, c.run())  # (no order of atomics, no stale share)
 
 
+@pytest.mark.usefixtures("table")
 def test_many_sequences():
     """More sequences than lanes, idle ones among them."""
     r = _rng(77)
@@ -170,6 +184,7 @@ def test_many_sequences():
     c.check(c.run(max_rows=3))
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("std", [1e-20, 0.02, 30.0])
 def test_ranges(std):
     c = _Batch([(9, 200, 0), (50, 100, 0)], 8, 2, 64, std=std)
@@ -185,9 +200,23 @@ def test_a_row_that_sees_nothing_gives_zeros():
     c.check(out)
 
 
+@pytest.mark.usefixtures("table")
+@pytest.mark.parametrize("hd", [64, 128])
+def test_rows_of_a_large_unit_that_see_nothing_give_zeros(hd):
+    seqs = [(60, 0, 0), (40, 5, 0), (50, 0, 70)]
+    c = _Batch(seqs, 4, 1, hd, tree=True)
+    c.masks[0] = [0] * 60
+    c.masks[2][7:30] = [0] * 23
+    c.anc = _words([m for ms in c.masks for m in ms])
+    out = c.run()
+    assert (out[:60] == 0).all() and (out[107:130] == 0).all()
+    c.check(out)
+
+
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("max_rows", [1, 0])
 @pytest.mark.parametrize("seqs,slot", [([(6, 100, 0), (1, 40, 0)], 102), ([(6, 100, 0), (1, 40, 0)], 5),
-                                       ([(80, 60, 0), (1, 40, 0)], 130)])
+                                       ([(80, 60, 0), (1, 40, 0)], 130), ([(80, 60, 0), (1, 40, 0)], 33)])
 def test_values_that_are_not_finite_reach_their_rows_only(seqs, slot, max_rows):
     for what in "kv":
         c = _Batch(seqs, 4, 2, 64)
@@ -203,6 +232,7 @@ def test_values_that_are_not_finite_reach_their_rows_only(seqs, slot, max_rows):
         assert np.array_equal(got[~bad], want[~bad])
 
 
+@pytest.mark.usefixtures("table")
 def test_pages_outside_the_pool_and_lengths_outside_the_table():
     """Rows that see such a page, and sequences that do not fit: NaN.  The others as ever."""
     seqs = [(2, 70, 0), (2, 70, 0), (1, 40, 0), (3, 10, 0), (2, 5, 0)]
@@ -226,6 +256,7 @@ def test_trees_of_more_than_128_nodes_give_nan():
     assert np.isnan(got[:2]).all() and np.isfinite(got[2:]).all()
 
 
+@pytest.mark.usefixtures("table")
 def test_row_numbers_that_are_not_rows():
     """Sequences whose rows do not lie in the call's take no part."""
     c = _Batch([(2, 70, 0), (2, 40, 0), (1, 10, 0)], 4, 2, 64)
@@ -333,6 +364,7 @@ def _step(c, rows, cos, sin, work, q, out):
     cas.op_attention_paged(cache, q, out, work=work)
 
 
+@pytest.mark.usefixtures("table")
 @pytest.mark.parametrize("seqs", [[(1, 5000, 0), (1, 17, 0), (1, 62, 0)], [(90, 100, 0), (1, 2000, 0), (3, 0, 0)]])
 def test_captured_step_replays_with_the_lengths_of_its_time(seqs):
     """Append and attention in one graph, replayed while the lengths grow and a
