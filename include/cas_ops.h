@@ -302,7 +302,8 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
  * n_pages), and such a page is not written.
  * Limits: head_dim 64 or 128; page_size a power of two from 32 to 4096;
  * table_len * page_size at most 1048576; n_kv_heads at most 4096; n_seqs at most
- * 65536; n_rows * n_heads / n_kv_heads below 2^24.
+ * 65536; n_rows * n_heads / n_kv_heads below 2^24; CAS_ERR_UNSUPPORTED where a
+ * call would take more than 2^32 - 1 threads.
  */
 typedef struct {
     void* pages;
@@ -374,8 +375,8 @@ cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t
  *            -infinity past the row's finite entries)
  * A logit of -infinity has probability 0.  A row that holds a NaN or +infinity,
  * or nothing but -infinity, has no distribution: NaN, and ids -1.
- * scale: finite and > 0 (1 / temperature).  V at most 1048576, n * ceil(V /
- * 8192) below 2^31.  Sums in fp32.
+ * scale: finite and > 0 (1 / temperature).  V at most 1048576, n at most
+ * 2097152.  Sums in fp32.
  * work: device scratch of cas_op_logprobs_work_bytes(...) bytes, 16-byte
  * aligned, used by one call at a time.
  */

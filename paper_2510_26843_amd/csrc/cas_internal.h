@@ -360,6 +360,10 @@ struct PagedPlan {
     size_t work;
 };
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows);
+// Workgroups of the launches, of at most PAGED_MOST_THREADS each.
+static constexpr int PAGED_MOST_THREADS = 512;
+static inline int64_t paged_append_grid(const PagedBatch& p) { return ((int64_t)p.N / 32 + 2 * (int64_t)p.B) * p.Hkv; }
+static inline int64_t paged_attn_grid(const PagedBatch& p, const PagedPlan& q) { return ((int64_t)q.units + q.target) * p.Hkv; }
 hipError_t launch_attention_paged(const PagedAttnArgs& a, const PagedPlan& q, hipStream_t s);
 
 // ---- log probabilities (logprobs.hip)

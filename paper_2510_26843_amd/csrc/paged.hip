@@ -243,7 +243,7 @@ template <int HD> __global__ void __launch_bounds__(PAPP_THREADS) k_paged_append
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
     const PagedBatch& p = a.p;
     if (p.N < 1 || p.B < 1 || p.Hkv < 1 || (a.q && a.H % p.Hkv)) return hipErrorInvalidValue;
-    const dim3 grid(((unsigned)p.N / 32 + 2u * p.B) * p.Hkv);
+    const dim3 grid((unsigned)paged_append_grid(p));
     if (p.hd == 128) return launch_checked(k_paged_append<128>, grid, PAPP_THREADS, s, a);
     if (p.hd == 64) return launch_checked(k_paged_append<64>, grid, PAPP_THREADS, s, a);
     return hipErrorInvalidValue;
@@ -344,11 +344,13 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
     };
     int C = 1 << 30;
     if (a.target > 0) {
-        int nq = own.nq, most = own.tiles;
+        // (many: nothing hangs on how many; sequences that overlap could pass 32 bits)
+        constexpr int MANY = 1 << 24;
+        int nq = min(own.nq, MANY), most = own.tiles;
         double w = (double)own.nq * own.tiles;  // (exact)
         for (int b0 = 64; b0 < p.B; b0 += 64) {
             const Seq q = seq(b0 + lane);
-            nq += q.nq;
+            nq = min(nq + min(q.nq, MANY), MANY);
             most = max(most, q.tiles);
             w += (double)q.nq * q.tiles;
         }
@@ -419,6 +421,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
 // joined through LDS at the end.  K and V fragments go from memory to the
 // registers that the MFMA reads.
 static constexpr int PAGED_WAVES = 8;
+static_assert(64 * PAGED_WAVES <= PAGED_MOST_THREADS);
 
 template <int HD, int JT>
 __device__ __forceinline__ void paged_scores(f32x4 (&S)[JT][2], const i32x4 (&k)[HD / 16], const i32x4 (&Q)[JT][HD / 32]) {
@@ -980,7 +983,7 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
 
 template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const PagedPlan& q, float c, hipStream_t s) {
     const PagedBatch& p = a.p;
-    const dim3 grid((unsigned)(q.units + q.target) * p.Hkv);
+    const dim3 grid((unsigned)paged_attn_grid(p, q));
     hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
                    : q.R == 32 ? launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c)
                                : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);

@@ -1941,6 +1941,8 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
 // ---- the paged KV cache
 
 static constexpr int PAGED_MAX_HEADS = 4096, PAGED_MAX_SEQS = 65536, PAGED_MAX_WINDOW = 1 << 21;
+// (a grid's threads are counted in 32 bits)
+static bool grid_fits(int64_t workgroups, int threads) { return workgroups * threads <= UINT32_MAX; }
 static bool paged_shape(int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t hd, cas_status* st) {
     *st = CAS_ERR_ARG;
     if (n_pages < 1 || page_size < 32 || page_size > 4096 || (page_size & (page_size - 1)) || Hkv < 1) return false;
@@ -1964,11 +1966,7 @@ static bool paged_batch(const cas_paged* c, int32_t H, bool arrays, PagedBatch* 
     if (c->n_seqs < 1 || c->n_seqs > PAGED_MAX_SEQS || c->n_rows < 1 || c->max_rows < 0 || c->table_len < 1) return false;
     if ((int64_t)c->table_len * c->page_size > KV4_MAX_CAP) return false;
     if (H < 1 || H > PAGED_MAX_HEADS || H % c->n_kv_heads) return false;
-    const int64_t rows = (int64_t)c->n_rows * (H / c->n_kv_heads);  // of a kv head
-    if (rows >= 1 << 24) return false;
-    *st = CAS_ERR_UNSUPPORTED;
-    if ((rows / 16 + 2 * (int64_t)c->n_seqs + 4096) * c->n_kv_heads > INT32_MAX) return false;  // (a grid dimension)
-    *st = CAS_ERR_ARG;
+    if ((int64_t)c->n_rows * (H / c->n_kv_heads) >= 1 << 24) return false;
     if (arrays) {
         if (!c->pages || !c->table || !c->seq_start || !c->ctx_len || !aligned16(c->pages)) return false;
         if (((uintptr_t)c->table | (uintptr_t)c->seq_start | (uintptr_t)c->ctx_len | (uintptr_t)c->nodes) & 3) return false;
@@ -2016,6 +2014,7 @@ cas_status cas_op_paged_append(const cas_paged* cache, const void* q, int64_t ld
     a.sin = sin;
     a.n_pos = n_pos;
     a.q_out = (uint16_t*)q_out;
+    if (!grid_fits(paged_append_grid(a.p), PAGED_MOST_THREADS)) return CAS_ERR_UNSUPPORTED;
     return launch_paged_append(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
 }
 
@@ -2035,6 +2034,7 @@ cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t
     if (!aligned16(q) || !aligned16(out) || !aligned16(work) || ((uintptr_t)anc & 7)) return CAS_ERR_ARG;
     const PagedPlan plan = paged_plan(a.p, H, cache->max_rows ? cache->max_rows : a.p.N);
     if (plan.work && (!work || work_bytes < plan.work)) return CAS_ERR_ARG;
+    if (!grid_fits(paged_attn_grid(a.p, plan), PAGED_MOST_THREADS)) return CAS_ERR_UNSUPPORTED;
     a.q = (const uint16_t*)q;
     a.anc = anc;
     a.out = (uint16_t*)out;
@@ -2048,9 +2048,9 @@ cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t
 
 // ---- log probabilities
 
-static constexpr int LOGP_MAX_V = 1 << 20, LOGP_MAX_K = 32;
+static constexpr int LOGP_MAX_N = 1 << 21, LOGP_MAX_V = 1 << 20, LOGP_MAX_K = 32;
 static bool logprobs_shape(int32_t n, int32_t V, int32_t K) {
-    return n >= 1 && V >= 1 && V <= LOGP_MAX_V && K >= 0 && K <= LOGP_MAX_K && (int64_t)n * ((V + 8191) / 8192) < 1ll << 31;
+    return n >= 1 && n <= LOGP_MAX_N && V >= 1 && V <= LOGP_MAX_V && K >= 0 && K <= LOGP_MAX_K;
 }
 
 size_t cas_op_logprobs_work_bytes(int32_t n, int32_t V, int32_t K) {

@@ -209,6 +209,7 @@ static void host_checks(void) {
     }
     q = pg; q.n_kv_heads = 4096; q.n_seqs = 65536; q.n_rows = (1 << 24) - 1;
     CHECK(cas_op_attention_paged(&q, p, 4096, NULL, 0, 0, p, p, 1 << 30, NULL) == CAS_ERR_UNSUPPORTED);
+    CHECK(cas_op_paged_append(&q, NULL, 0, 0, p, 4096 * 64, p, 4096 * 64, NULL, NULL, NULL, 0, NULL, NULL) == CAS_ERR_UNSUPPORTED);
     q = pg; q.head_dim = 80;
     CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, p, 1 << 30, NULL) == CAS_ERR_UNSUPPORTED);
     CHECK(cas_op_attention_paged(&pg, NULL, 4, NULL, 0, 0, p, NULL, 0, NULL) == CAS_ERR_ARG);
@@ -220,7 +221,7 @@ static void host_checks(void) {
     CHECK(cas_op_attention_paged(&q, p, 4, NULL, 0, 0, p, NULL, 1 << 30, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs_work_bytes(3, 32000, 5) > 0);
     CHECK(cas_op_logprobs_work_bytes(0, 32000, 5) == 0 && cas_op_logprobs_work_bytes(3, (1 << 20) + 1, 5) == 0);
-    CHECK(cas_op_logprobs_work_bytes(3, 32000, 33) == 0 && cas_op_logprobs_work_bytes(INT32_MAX, 1 << 20, 0) == 0);
+    CHECK(cas_op_logprobs_work_bytes(3, 32000, 33) == 0 && cas_op_logprobs_work_bytes((1 << 21) + 1, 100, 0) == 0);
     CHECK(cas_op_logprobs(CAS_W_I8, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) ==
           CAS_ERR_UNSUPPORTED);
     CHECK(cas_op_logprobs(CAS_W_F32, NULL, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
