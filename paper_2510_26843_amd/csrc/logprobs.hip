@@ -30,21 +30,25 @@ static constexpr int LP_LIST = 512;  // candidates of a workgroup, of which a li
 static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ bool lp_better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
-__device__ __forceinline__ float lp_lane(float x, int l) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), l));
-}
 
-// The K-th and the J-th largest of the lanes' values (no NaN), the same for every lane.
+// Bounds, the same for every lane, that K and J lanes' values reach (no NaN): the
+// K-th and the J-th largest but for the last 12 bits, found from the top by the
+// count of lanes that reach (with every lane's rank, of 64 comparisons, this took
+// 16 waves of a CU 3 us).
 __device__ __forceinline__ void lp_kth(float x, int K, int J, float* kth, float* jth) {
-    const int lane = threadIdx.x & 63;
-    int above = 0;
-#pragma unroll 4
-    for (int l = 0; l < 64; ++l) {
-        const float o = lp_lane(x, l);
-        above += o > x || (o == x && l < lane) ? 1 : 0;
+    const uint32_t b = __float_as_uint(x), key = b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);  // ordered as the values
+    uint32_t k = 0, j = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) {
+        const uint32_t k1 = k | 1u << bit, j1 = j | 1u << bit;
+        k = (int)__popcll(__ballot(key >= k1)) >= K ? k1 : k;
+        j = (int)__popcll(__ballot(key >= j1)) >= J ? j1 : j;
     }
-    *kth = lp_lane(x, __builtin_ctzll(__ballot(above == K - 1)));
-    *jth = lp_lane(x, __builtin_ctzll(__ballot(above == J - 1)));
+    auto value = [](uint32_t o) {  // (below the finite ones: -infinity)
+        return o < 0x00800000u ? -INFINITY : __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+    };
+    *kth = value(k);
+    *jth = value(j);
 }
 
 // How many of a list's n entries (16-byte aligned; up to three -infinity behind
@@ -99,12 +103,16 @@ __device__ __forceinline__ float lp_logit(const LogprobArgs& a, int row, int t) 
     const size_t o = (size_t)row * a.ld + t;
     return a.bf16 ? bf2f(((const uint16_t*)a.x)[o]) : ((const float*)a.x)[o];
 }
-template <int THREADS> __device__ __forceinline__ void lp_tokens(const LogprobArgs& a, int row, const LpRow& r) {
+// The logit of a row's j-th token: NaN for an id outside the row.
+__device__ __forceinline__ float lp_token(const LogprobArgs& a, int row, int j) {
+    const int t = a.tokens[(size_t)row * a.m + j];
+    return t >= 0 && t < a.V ? lp_logit(a, row, t) : NAN;
+}
+// (x: the logit of the thread's first token)
+template <int THREADS> __device__ __forceinline__ void lp_tokens(const LogprobArgs& a, int row, const LpRow& r, float x) {
     if (threadIdx.x == 0 && a.entropy) a.entropy[row] = r.entropy;
-    for (int j = threadIdx.x; j < a.m; j += THREADS) {
-        const int t = a.tokens[(size_t)row * a.m + j];
-        a.logp[(size_t)row * a.m + j] = t >= 0 && t < a.V ? r.logp(lp_logit(a, row, t), a.scale) : NAN;
-    }
+    for (int j = threadIdx.x; j < a.m; j += THREADS)
+        a.logp[(size_t)row * a.m + j] = r.logp(j < THREADS ? x : lp_token(a, row, j), a.scale);
 }
 
 // A part's record: m, s, u, and its K best: values, then ids.
@@ -151,6 +159,7 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
     float lm = -INFINITY;
     i32x4 raw[NV];
     load(raw, begin);
+    const float asked = parts == 1 && tid < a.m ? lp_token(a, row, tid) : NAN;
     for (int base = begin, k = 0; base < end; base += CHUNK, ++k) {
         float x[EACH + 1];
         unpack(x, raw, base);
@@ -205,7 +214,7 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
     const LpRow out(r);
     float* rec = a.work + (size_t)blockIdx.x * words;
     if (parts == 1) {
-        lp_tokens<THREADS>(a, row, out);
+        lp_tokens<THREADS>(a, row, out, asked);
     } else if (tid == 0) {
         rec[0] = r.m;
         rec[1] = r.s;
@@ -246,11 +255,12 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
         const float cm = sm_top[k * THREADS + tid];
         if (cm >= tau && cm > -INFINITY) hit |= 1u << k;
     }
+    // (from the last on, which is still here)
     while (hit) {
-        const int base = begin + __builtin_ctz(hit) * CHUNK;
-        hit &= hit - 1;
+        const int k = 31 - __builtin_clz(hit), base = begin + k * CHUNK;
+        hit ^= 1u << k;
         float x[EACH + 1];
-        load(raw, base);
+        if (base + CHUNK < end) load(raw, base);
         unpack(x, raw, base);
 #pragma unroll
         for (int e = 0; e <= EACH; ++e)
@@ -346,8 +356,7 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
         }
     };
     if (K > 0) candidates(0);
-    const int t0 = lane < a.m ? a.tokens[(size_t)row * a.m + lane] : -1;
-    const float x0 = t0 >= 0 && t0 < a.V ? lp_logit(a, row, t0) : NAN;
+    const float asked = lane < a.m ? lp_token(a, row, lane) : NAN;
     LpSums t = {-INFINITY, 0.f, 0.f};
     // At least K logits reach each of: a part's K-th best, the smallest of the parts'
     // ceil(K / parts)-th best, and the K-th of the lanes' best.
@@ -371,12 +380,7 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     t.s = wave_sum(t.s);
     t.u = wave_sum(t.u);
     const LpRow out(t);
-    if (lane == 0 && a.entropy) a.entropy[row] = out.entropy;
-    for (int j = lane; j < a.m; j += 64) {
-        const int id = j < 64 ? t0 : a.tokens[(size_t)row * a.m + j];
-        const bool ok = id >= 0 && id < a.V;
-        a.logp[(size_t)row * a.m + j] = ok ? out.logp(j < 64 ? x0 : lp_logit(a, row, id), a.scale) : NAN;
-    }
+    lp_tokens<64>(a, row, out, asked);
     if (K == 0) return;
     float kth, jth;
     lp_kth(first, K, 1, &kth, &jth);
