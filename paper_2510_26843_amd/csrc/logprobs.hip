@@ -18,7 +18,9 @@
 // another, each from a pass over the part.  Everything is ordered by (logit, id),
 // so no order of arrival shows.
 //
-// What bounds it: for many rows the bytes; for one row the latency of a CU's reads.
+// What bounds it: for many rows the bytes (1501 rows of 128256 logits, K = 20: 154
+// us, 5.0 TB/s, what a copy reaches); for few rows a chain of waits (a row's first
+// logits 2 us, the join 3.5 us, of which 2 for what other workgroups wrote).
 #include "attn_step.h"
 
 #include <algorithm>
@@ -26,29 +28,36 @@
 namespace cas {
 
 static constexpr int LP_MAX_K = 32;
+static constexpr int LP_RANKED = 128;  // candidates that the join ranks against each other
 static constexpr int LP_LIST = 512;  // candidates of a workgroup, of which a list holds
 static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ bool lp_better(float a, int ia, float b, int ib) { return a > b || (a == b && ia < ib); }
 
-// Bounds, the same for every lane, that K and J lanes' values reach (no NaN): the
+// Values in the order of unsigned numbers, and back (below the finite ones: -infinity).
+__device__ __forceinline__ uint32_t lp_key(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float lp_value(uint32_t key) {
+    return key < 0x00800000u ? -INFINITY : __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+// Bounds, the same for every lane, that K lanes' x and J lanes' y reach (no NaN): the
 // K-th and the J-th largest but for the last 12 bits, found from the top by the
 // count of lanes that reach (with every lane's rank, of 64 comparisons, this took
 // 16 waves of a CU 3 us).
-__device__ __forceinline__ void lp_kth(float x, int K, int J, float* kth, float* jth) {
-    const uint32_t b = __float_as_uint(x), key = b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);  // ordered as the values
+static constexpr int LP_BITS = 12;
+__device__ __forceinline__ void lp_kth(float x, int K, float* kth, float y, int J, float* jth) {
+    const uint32_t key = lp_key(x), key_j = lp_key(y);
     uint32_t k = 0, j = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 12; --bit) {
+    for (int bit = 31; bit >= LP_BITS; --bit) {
         const uint32_t k1 = k | 1u << bit, j1 = j | 1u << bit;
         k = (int)__popcll(__ballot(key >= k1)) >= K ? k1 : k;
-        j = (int)__popcll(__ballot(key >= j1)) >= J ? j1 : j;
+        j = (int)__popcll(__ballot(key_j >= j1)) >= J ? j1 : j;
     }
-    auto value = [](uint32_t o) {  // (below the finite ones: -infinity)
-        return o < 0x00800000u ? -INFINITY : __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
-    };
-    *kth = value(k);
-    *jth = value(j);
+    *kth = lp_value(k);
+    *jth = lp_value(j);
 }
 
 // How many of a list's n entries (16-byte aligned; up to three -infinity behind
@@ -182,7 +191,7 @@ __global__ void __launch_bounds__(THREADS) k_logprob_part(const LogprobArgs a, i
     // Of W waves at least K threads reach each of: the K-th largest thread of any
     // wave, and the smallest of the waves' ceil(K / W)-th.
     float kth = 0.f, jth = 0.f;
-    if (K > 0) lp_kth(lm, K, (K + W - 1) / W, &kth, &jth);
+    if (K > 0) lp_kth(lm, K, &kth, lm, (K + W - 1) / W, &jth);
     t.s = wave_sum(t.s);
     t.u = wave_sum(t.u);
     if (lane == 0) {
@@ -359,22 +368,19 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     const float asked = lane < a.m ? lp_token(a, row, lane) : NAN;
     LpSums t = {-INFINITY, 0.f, 0.f};
     // At least K logits reach each of: a part's K-th best, the smallest of the parts'
-    // ceil(K / parts)-th best, and the K-th of the lanes' best.
+    // ceil(K / parts)-th best, the K-th of the lanes' best, and the ceil(K / 4)-th of
+    // their fourth best.
     const int J = (K + parts - 1) / parts;
-    float tau = -INFINITY, low = INFINITY, first = -INFINITY;
-    for (int k = lane; k < parts; k += 64) {
-        const float* q = rec + (size_t)k * words;
-        LpSums p = {q[0], q[1], q[2]};
+    float tau = -INFINITY, low = INFINITY, first = -INFINITY, fourth = -INFINITY;
+    if (lane < parts) {
+        const float* q = rec + (size_t)lane * words;
+        t = {q[0], q[1], q[2]};
         if (K > 0) {
-            tau = fmaxf(tau, q[3 + K]);
-            low = fminf(low, q[3 + J]);
-            first = fmaxf(first, q[4]);
+            tau = q[3 + K];
+            low = q[3 + J];
+            first = q[4];
+            if (K > 8) fourth = q[7];
         }
-        const float m = fmaxf(t.m, p.m);
-        t.lift(m, c);
-        p.lift(m, c);
-        t.s += p.s;
-        t.u += p.u;
     }
     t.lift(wave_top(t.m), c);
     t.s = wave_sum(t.s);
@@ -382,9 +388,10 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     const LpRow out(t);
     lp_tokens<64>(a, row, out, asked);
     if (K == 0) return;
-    float kth, jth;
-    lp_kth(first, K, 1, &kth, &jth);
-    tau = fmaxf(fmaxf(wave_top(tau), kth), -wave_top(-low));
+    float kth, jth = -INFINITY, none;
+    if (K > 8) lp_kth(first, K, &kth, fourth, (K + 3) / 4, &jth);
+    else lp_kth(first, K, &kth, first, 1, &none);
+    tau = fmaxf(fmaxf(wave_top(tau), -wave_top(-low)), fmaxf(kth, jth));
     float *best = a.best + (size_t)row * K, *v = sm;
     int *ids = a.ids + (size_t)row * K, *id = (int*)(sm + ((all + 7) & ~3)), n = 0;
     for (int i0 = 0; i0 < all; i0 += AT_ONCE * 64) {
@@ -401,6 +408,34 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
             n += __popcll(in);
         }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // Many: to a bound by the count of those that reach it, as in lp_kth (32 parts of
+    // 64000 logits, K = 32: 600 reached, and ranking them took 50 us).
+    if (n > LP_RANKED) {
+        uint32_t bound = 0;
+        for (int bit = 31; bit >= LP_BITS; --bit) {
+            int reach = 0;
+            for (int i0 = 0; i0 < n; i0 += 64)
+                reach += (int)__popcll(__ballot(i0 + lane < n && lp_key(v[min(i0 + lane, n - 1)]) >= (bound | 1u << bit)));
+            if (reach >= K) bound |= 1u << bit;
+        }
+        const float least = lp_value(bound);  // (the zeros are equal)
+        int kept = 0;
+        for (int i0 = 0; i0 < n; i0 += 64) {
+            const int i = min(i0 + lane, n - 1);
+            const float x = v[i];
+            const int xi = id[i];
+            const bool keep = i0 + lane < n && x >= least;
+            const uint64_t in = __ballot(keep);
+            if (keep) {  // (at or below i0 + lane)
+                const int to = kept + __popcll(in & (((uint64_t)1 << lane) - 1));
+                v[to] = x;
+                id[to] = xi;
+            }
+            kept += __popcll(in);
+        }
+        n = kept;
+    }
     lp_pad(v, id, n);
     for (int i = lane; i < n; i += 64) {
         const float x = v[i];
@@ -416,36 +451,42 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     }
 }
 
-// A row of up to LP_ROW bytes in a call of up to LP_ROWS rows is one workgroup of
-// 1024 threads: a CU reads it in less time than a second kernel takes.  Others
-// are workgroups of 256 threads: in parts, a few workgroups per CU, where there are
-// too few rows, in chunks of 2048 logits where 8192 would leave the chip empty.
-static constexpr int LP_ROWS = 512, LP_SPAN = 32;  // LP_SPAN: most chunks of a part (at most 32: bits of a word)
-static constexpr int LP_FEW = 32;
-static constexpr int64_t LP_ROW = 640 << 10, LP_SHORT = 128 << 10;
+// A row is walked by one workgroup of 1024 threads, or by workgroups of 256 in
+// parts that k_logprob_join joins.  Measured, fp32 rows, in us:
+// - One of 1024 where that walks a row in few chunks and the rows are about as many
+//   as the CUs: 256 rows of 128256 logits, K = 20, 35 (in parts 45), 128 rows of
+//   32000, K = 5, 11 (12 to 15).  A second round of them costs as much again (320
+//   rows of 32000 22, in parts 19), and few rows leave CUs idle (48 of 128256,
+//   K = 8, 21, in parts 13; but of 32000, one chunk, 64 rows 11 either way).
+// - Parts of chunks of 8192 logits (32 a thread), or of 2048 (8 a thread: twice the
+//   waves on a CU) where those would leave the chip empty (1 row of 128256, K = 5,
+//   9.3 for 10.5), or mostly hold nothing (5000 rows of 1024 21 for 35), and for
+//   many short rows (1501 of 32000 38 for 42; of 128256 128 for 110).
+// - At most 64 parts: a lane of the join each (2 rows of 1000000 14.5, with 489 parts 18.6).
+static constexpr int LP_PARTS = 64;
+static constexpr int LP_SPAN = 32;  // most chunks of a part (at most 32: bits of a word)
 struct LpPlan {
     int each, threads, parts, span;
 };
-static LpPlan lp_plan(int n, int V, int bf16) {
+static LpPlan lp_plan(int n, int V) {
     LpPlan p;
-    const int64_t bytes = (int64_t)V * (bf16 ? 2 : 4);
-    const bool whole = n <= LP_ROWS && bytes <= (n < LP_FEW ? LP_SHORT : LP_ROW);
+    const bool whole = n <= 256 && V > 16384 && V <= 131072 && (V <= 32768 || n > 64);
+    const bool small = V <= 8192 || (n > 512 ? V <= 32768 : (int64_t)n * ((V + 8191) / 8192) < 512);
     p.threads = whole ? 1024 : 256;
-    p.each = whole || (int64_t)n * ((V + 8191) / 8192) >= 512 ? 32 : 8;
+    p.each = whole || !small ? 32 : 8;
     const int chunk = p.threads * p.each, chunks = (V + chunk - 1) / chunk;
-    const int want = whole ? 1 : (int)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / n));
+    const int want = whole ? 1 : std::min({chunks, LP_PARTS, std::max(1, 2048 / n)});
     p.span = std::min((chunks + want - 1) / want, LP_SPAN);
     p.parts = (chunks + p.span - 1) / p.span;
     return p;
 }
-size_t logprob_work_bytes(int n, int V, int K) {  // (of either type)
-    const LpPlan f = lp_plan(n, V, 0), h = lp_plan(n, V, 1);
-    return std::max<size_t>(16, (size_t)n * std::max(f.parts, h.parts) * lp_words(K) * 4);
+size_t logprob_work_bytes(int n, int V, int K) {
+    return std::max<size_t>(16, (size_t)n * lp_plan(n, V).parts * lp_words(K) * 4);
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     if (a.n < 1 || a.V < 1 || a.K < 0 || a.K > LP_MAX_K || a.m < 0) return hipErrorInvalidValue;
-    const LpPlan p = lp_plan(a.n, a.V, a.bf16);
+    const LpPlan p = lp_plan(a.n, a.V);
     const int words = lp_words(a.K);
     const dim3 grid((unsigned)a.n * p.parts);
     auto kernel = p.threads == 1024 ? (a.bf16 ? k_logprob_part<true, 32, 1024> : k_logprob_part<false, 32, 1024>)

@@ -72,7 +72,8 @@ def _check(x, tokens, K, scale, got):
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("n,V,m,K,scale", [
     (1, 1, 1, 1, 1.0), (1, 2, 3, 5, 1.0), (3, 63, 1, 32, 0.5), (2, 100, 0, 3, 1.0), (5, 1000, 4, 0, 2.0), (1, 8191, 2, 16, 1.0),
-    (2, 8192, 2, 16, 1.0), (2, 8193, 2, 16, 1.0), (61, 32000, 4, 8, 1.25), (3, 128256, 1, 20, 0.7), (1, 300007, 300, 32, 1.0)])
+    (2, 8192, 2, 16, 1.0), (2, 8193, 2, 16, 1.0), (61, 32000, 4, 8, 1.25), (3, 128256, 1, 20, 0.7), (1, 300007, 300, 32, 1.0),
+    (3, 64000, 1, 32, 1.0), (40, 64000, 1, 31, 1.0), (300, 9000, 2, 8, 1.0), (130, 50000, 1, 20, 1.0), (600, 33000, 1, 9, 1.0)])
 def test_logprobs(n, V, m, K, scale, bf16):
     x = _logits(n, V, bf16)
     t = np.random.default_rng(n + V).integers(0, V, (n, m)) if m else None
@@ -85,19 +86,20 @@ def test_the_longest_row():
     _check(x, t, 32, 1.0, _run(x, t, 32))
 
 
+@pytest.mark.parametrize("V", [20000, 64000])
 @pytest.mark.parametrize("bf16", [False, True])
-def test_ties(bf16):
+def test_ties(bf16, V):
     """Equal logits everywhere, in one wave's part, or in bands: lowest ids first."""
-    V = 20000
-    x = torch.zeros((5, V), device=DEV)
+    x = torch.zeros((6, V), device=DEV)
     x[1, 300:900] = 3.0
     x[2] = torch.arange(V, device=DEV) % 7
     x[3, 8000:8400] = -0.0
     x[4] = -1.0
-    x[4, 19990:] = 0.0
+    x[4, V - 10 :] = 0.0
+    x[5, :10] = -0.0
     if bf16:
         x = x.to(torch.bfloat16)
-    t = [[0, V - 1]] * 5
+    t = [[0, V - 1]] * 6
     _check(x, t, 32, 1.0, _run(x, t, 32))
 
 
