@@ -377,8 +377,8 @@ cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t
  * or nothing but -infinity, has no distribution: NaN, and ids -1.
  * scale: finite and > 0 (1 / temperature).  V at most 1048576, n at most
  * 2097152.  Sums in fp32.
- * work: device scratch of cas_op_logprobs_work_bytes(...) bytes, 16-byte
- * aligned, used by one call at a time.
+ * work: device scratch of cas_op_logprobs_work_bytes(...) bytes (no less for
+ * more rows or a larger K), 16-byte aligned, used by one call at a time.
  */
 size_t cas_op_logprobs_work_bytes(int32_t n, int32_t V, int32_t K);
 cas_status cas_op_logprobs(int32_t ltype, const void* logits, int64_t ld, int32_t n, int32_t V, float scale,

@@ -377,9 +377,10 @@ struct LogprobArgs {
     float *logp, *entropy; // [n][m], [n] (nullptr: not wanted)
     int* ids;              // [n][K]
     float* best;           // [n][K]
-    float* work;           // logprob_work_bytes
+    float* work;           // work_bytes of them: logprob_work_bytes of at least n rows and K
+    size_t work_bytes;
 };
-size_t logprob_work_bytes(int n, int V, int K);
+size_t logprob_work_bytes(int n, int V, int K);  // (no less for more rows or K)
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
 
 // RMSNorm of rows of the fp32 residual stream h [T][d] with gains g:

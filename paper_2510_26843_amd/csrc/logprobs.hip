@@ -480,14 +480,18 @@ static LpPlan lp_plan(int n, int V) {
     p.parts = (chunks + p.span - 1) / p.span;
     return p;
 }
+// The records of any call of up to n rows: those of 2048 parts, unless the rows'
+// parts of LP_SPAN chunks are more.
 size_t logprob_work_bytes(int n, int V, int K) {
-    return std::max<size_t>(16, (size_t)n * lp_plan(n, V).parts * lp_words(K) * 4);
+    const int64_t most = std::min(LP_PARTS, (V + 2047) / 2048), least = (V + 8192 * LP_SPAN - 1) / (8192 * LP_SPAN);
+    return (size_t)std::max(std::min(n * most, (int64_t)2048), n * least) * lp_words(K) * 4;
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     if (a.n < 1 || a.V < 1 || a.K < 0 || a.K > LP_MAX_K || a.m < 0) return hipErrorInvalidValue;
     const LpPlan p = lp_plan(a.n, a.V);
     const int words = lp_words(a.K);
+    if (p.parts > 1 && a.work_bytes < (size_t)a.n * p.parts * words * 4) return hipErrorInvalidValue;
     const dim3 grid((unsigned)a.n * p.parts);
     auto kernel = p.threads == 1024 ? (a.bf16 ? k_logprob_part<true, 32, 1024> : k_logprob_part<false, 32, 1024>)
                   : p.each == 32      ? (a.bf16 ? k_logprob_part<true, 32, 256> : k_logprob_part<false, 32, 256>)

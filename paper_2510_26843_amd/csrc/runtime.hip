@@ -1396,6 +1396,7 @@ cas_status cas_logprobs(cas_ctx* c, int32_t n, float scale, const int32_t* token
     a.m = m;
     a.K = K;
     a.work = c->d_logp;
+    a.work_bytes = logprob_work_bytes((int)cap, c->cfg.vocab, kLogpTop);
     hipError_t e = timed(c, CAS_K_TOPK, [&]() -> hipError_t { return launch_logprobs(a, c->stream); });
     if (e != hipSuccess) return hip_fail(c, e, "log probabilities launch");
     HIPCHK(c, hipStreamSynchronize(c->stream));
@@ -2082,6 +2083,7 @@ cas_status cas_op_logprobs(int32_t ltype, const void* logits, int64_t ld, int32_
     a.ids = top_ids;
     a.best = top_logp;
     a.work = (float*)work;
+    a.work_bytes = work_bytes;
     return launch_logprobs(a, (hipStream_t)stream) == hipSuccess ? CAS_OK : CAS_ERR_DEVICE;
 }
 

@@ -174,3 +174,14 @@ def test_replayed():
         torch.cuda.synchronize()
         for w, g in zip(want, out):
             assert np.array_equal(w, g.cpu().numpy())
+
+
+@pytest.mark.parametrize("V", [32000, 70000])
+def test_scratch_of_more_rows(V):
+    """One scratch, sized for the most rows, serves calls of fewer; nothing behind it is written."""
+    need = cas.lib().cas_op_logprobs_work_bytes(128, V, 32)
+    room = torch.full((need + (1 << 20),), 77, dtype=torch.uint8, device=DEV)
+    x = _logits(128, V, False)
+    for n in (1, 2, 17, 31, 32, 33, 64, 65, 128):
+        _check(x[:n], [[n]] * n, 32, 1.0, _run(x[:n], [[n]] * n, 32, work=room[:need]))
+        assert (room[need:] == 77).all()

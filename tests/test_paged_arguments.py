@@ -173,3 +173,12 @@ def test_another_device(calls, monkeypatch):
 def test_a_batch_keeps_its_tensors(calls):
     c = _cache()
     assert len(c.tensors) == 5 and c.tensors[0].data_ptr() == c.pages
+
+
+@pytest.mark.parametrize("vocab", [1, 1000, 8193, 32000, 128256, 1 << 20])
+def test_logprob_work_serves_fewer_rows(vocab):
+    """Scratch for n rows and K serves any call of fewer: the parts of a row go with the rows."""
+    f = cas.lib().cas_op_logprobs_work_bytes
+    sizes = [f(n, vocab, 32) for n in range(1, 700)]
+    assert sizes == sorted(sizes) and sizes[0] >= 16
+    assert all(f(n, vocab, K) <= f(n, vocab, 32) for n in (1, 33, 257) for K in (0, 1, 8))
