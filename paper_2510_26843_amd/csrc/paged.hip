@@ -62,6 +62,10 @@ __device__ __forceinline__ int paged_page(const PagedBatch& p, int b, int tile) 
 // angles serve its key and its queries, and the tile is put together in LDS and
 // stored 16 bytes per lane in one piece.  Another tile's few rows are stored in
 // place, a piece of 8 elements per thread.
+//
+// What bounds it: many rows, memory (16384 rows of 32 + 8 + 8 heads of 128, 411 MB:
+// 84 us, 4.9 TB/s, a copy's rate; with every tile stored in place and the heads of
+// a tile apart 111); one row, its chain of loads (4.4 us).
 static constexpr int PAPP_THREADS = 256;
 
 __device__ __forceinline__ i32x4 paged_ld8(const uint16_t* p, bool vec) {
@@ -419,7 +423,13 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
 // p = token p / G, head p % G of the group), the share's key tiles over eight
 // waves, each with the running maximum and sum of a softmax of its own (attn_step),
 // joined through LDS at the end.  K and V fragments go from memory to the
-// registers that the MFMA reads.
+// registers that the MFMA reads: no other wave wants them.
+//
+// What bounds it: 16 rows, memory (32 sequences of up to 8190 slots, 8 heads, 276
+// MB: 54 us, 5.1 TB/s; one of 131072, 537 MB: 105; with keys and values of a tile
+// loaded together 66); 32 rows, of memory at 4 to 5 TB/s, and of the L2s
+// where several units read the same slots; few slots, the waits at the start and the
+// joins (one row over 500 slots 6.3 us, over 1000 8.1, over 4095, in shares, 9.5).
 static constexpr int PAGED_WAVES = 8;
 static_assert(64 * PAGED_WAVES <= PAGED_MOST_THREADS);
 
@@ -583,9 +593,14 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 // Workgroup = (share of a unit of 128 packed rows, kv head): four waves of two
 // 16-row query tiles each.  The share's key tiles pass through LDS in a ring of
 // four, keys one tile ahead of the values, with direct-to-LDS loads (the
-// fragments lie in memory as the MFMA reads them: no swizzle, no conflict) that
-// are issued three tiles ahead; one barrier per tile.  attn_step issues the next
-// tile's scores under this one's exponentials.
+// fragments lie in memory as the MFMA reads them: no swizzle, no conflict), two
+// tiles a stage, one barrier per stage.  A tile's scores are computed under the
+// exponentials of the one before it.
+//
+// What bounds it: the matrix cores, at the rate that a large product reaches: 2048
+// rows of 8B heads behind 6001 slots, 236 GFLOP, 208 us, 1130 TFLOP/s (one tile a
+// stage, in the compiler's order, 294; 256 rows, four query tiles per wave, 372).
+// Two workgroups share a CU: a tile takes one 0.87 us beside another, 0.57 alone.
 static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
 
 template <int HD>
@@ -602,7 +617,8 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
     const bool tree = a.anc != nullptr;
     // The last rows see the most slots: their shares start first.  Where all of a
     // sequence's run at once, two to a CU, the second half goes the other way, so
-    // that a long one shares its CU with a short one.
+    // that a long one shares its CU with a short one (a prompt's first 2048 rows, 8B
+    // heads: 54 us, else 57).
     const int split = sh.local / sh.nq, at = sh.local - split * sh.nq, half = (sh.nq + 1) / 2;
     const int qt = a.fold && at >= half ? at - half : sh.nq - 1 - at;
     auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
