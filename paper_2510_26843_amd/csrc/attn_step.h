@@ -22,10 +22,8 @@ static hipError_t launch_checked(void (*kernel)(P...), dim3 grid, unsigned threa
 template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_or_0(int x) {
     return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
-template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_0(double x) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(uint32_t)b), hi = (uint32_t)dpp_or_0<CTRL, ROWS>((int)(b >> 32));
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_0(float x) {
+    return __uint_as_float((uint32_t)dpp_or_0<CTRL, ROWS>((int)__float_as_uint(x)));
 }
 template <typename V> __device__ __forceinline__ V wave_scan(V x) {
     x += dpp_or_0<0x111, 0xf>(x);  // the row's lane - 1, - 2, - 4, - 8
@@ -37,14 +35,7 @@ template <typename V> __device__ __forceinline__ V wave_scan(V x) {
     return x;
 }
 template <typename V> __device__ __forceinline__ V wave_total(V x) {
-    const V s = wave_scan(x);
-    if constexpr (sizeof(V) == 4) {
-        return (V)__builtin_amdgcn_readlane((int)s, 63);
-    } else {
-        const uint64_t b = __builtin_bit_cast(uint64_t, s);
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63);
-        return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 | lo);
-    }
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x)), 63));
 }
 // The largest of the lanes' values, the same for every lane (no NaN).
 __device__ __forceinline__ float wave_top(float x) {

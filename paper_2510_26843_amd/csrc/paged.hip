@@ -351,19 +351,20 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         // (many: nothing hangs on how many; sequences that overlap could pass 32 bits)
         constexpr int MANY = 1 << 24;
         int nq = min(own.nq, MANY), most = own.tiles;
-        double w = (double)own.nq * own.tiles;  // (exact)
+        float w = (float)own.nq * own.tiles;
         for (int b0 = 64; b0 < p.B; b0 += 64) {
             const Seq q = seq(b0 + lane);
             nq = min(nq + min(q.nq, MANY), MANY);
             most = max(most, q.tiles);
-            w += (double)q.nq * q.tiles;
+            w += (float)q.nq * q.tiles;
         }
         nq = wave_total<int>(nq);
-        w = wave_total<double>(w);
+        // (a lane's 1024 sums and the wave's: off by at most 1100 2^-24 of it.  Never
+        // below what it stands for, as the bounds need)
+        w = wave_total<float>(w) * 1.0001f;
         most = wave_most(most);
-        // (w / n rounded up, or a little more: never below it, as the bounds need)
         auto share = [&](int n) {
-            return max(a.least, (int)fminf(1073741824.f, ceilf((float)w * __builtin_amdgcn_rcpf((float)n) * 1.000001f)));
+            return max(a.least, (int)fminf(1073741824.f, ceilf(w * __builtin_amdgcn_rcpf((float)n))));
         };
         C = share(a.target);
         // With room left by the units: as many shares as run at once, if the longest is
@@ -925,7 +926,14 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
     __shared__ f32x4 sm_o[NG][D4];
     const PagedBatch& p = a.p;
     const int kvh = blockIdx.x % p.Hkv, G = a.G;
-    const PagedShare sh = paged_share<true>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    // (one wave looks: up to eight workgroups share a CU)
+    __shared__ PagedShare sm_sh;
+    if (threadIdx.x < 64) {
+        const PagedShare found = paged_share<true>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+        if (threadIdx.x == 0) sm_sh = found;
+    }
+    __syncthreads();
+    const PagedShare sh = sm_sh;
     if (!sh.found) return;
     const int ns = sh.ns, NS = ns > 16 ? 8 : ns > 8 ? 4 : ns > 4 ? 2 : 1;
     const int gi = threadIdx.x / D4, d4 = threadIdx.x % D4 * 4, sub = gi % NS;
