@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 // exponentials of the one before it.
 //
 // What bounds it: the matrix cores, at the rate that a large product reaches: 2048
-// rows of 8B heads behind 6001 slots, 236 GFLOP, 208 us, 1130 TFLOP/s (one tile a
+// rows of 8B heads behind 6001 slots, 236 GFLOP, 203 us, 1160 TFLOP/s (one tile a
 // stage, in the compiler's order, 294; 256 rows, four query tiles per wave, 372).
 // Two workgroups share a CU: a tile takes one 0.87 us beside another, 0.57 alone.
 static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
