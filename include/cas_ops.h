@@ -348,8 +348,9 @@ cas_status cas_op_paged_append(const cas_paged* cache, const void* q, int64_t ld
  *         row's own, or a tree row's committed slots, to the first attn_sink and
  *         the last attn_window ones (0: all)
  * Slots and rows that a row does not see never reach it, whatever they hold.  A
- * row that sees no slot gives zeros; one that sees a key that is not finite
- * gives NaN, and one that sees such a value no finite one at its element.
+ * row that sees no slot gives zeros; one with a score of NaN or +infinity gives
+ * NaN, and one that sees a value that is not finite no finite one at its element.
+ * A score of -infinity has no weight.
  * Probabilities are rounded to bf16 for the product with the values (each by at
  * most 2^-8 of itself).  The result does not depend on earlier calls or on timing; it may
  * depend in the last bits on the batch.

@@ -233,6 +233,26 @@ def test_values_that_are_not_finite_reach_their_rows_only(seqs, slot, max_rows):
 
 
 @pytest.mark.usefixtures("table")
+@pytest.mark.parametrize("seqs", [[(6, 100, 0)], [(80, 60, 0)]])
+@pytest.mark.parametrize("slot", [5, 40])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf")])
+def test_infinite_keys(seqs, slot, value):
+    """A score of +infinity gives NaN, one of -infinity takes its slot out."""
+    c = _Batch(seqs, 4, 2, 64)
+    t, Lc, _ = seqs[0]
+    c.pages[c.table[0, slot // 32], 0, 1, int(P.key_places(64)[slot % 32, 7])] = value
+    got = _np(c.run()).reshape(-1, 4, 64)
+    see = P.visible(t, Lc, 0, None, 0, 0)
+    without = see.copy()
+    without[:, slot] = False
+    (ref, err), (ref0, err0) = (P.attention(c.q, *c.kv[0], x) for x in (see, without))
+    ref[:, 2:], err[:, 2:] = ref0[:, 2:], err0[:, 2:]
+    nan = see[:, slot, None] & (np.sign(c.q[..., 7]) == np.sign(value))
+    nan[:, :2] = False
+    assert np.isnan(got[nan]).all() and (np.abs(got - ref) <= err)[~nan].all()
+
+
+@pytest.mark.usefixtures("table")
 def test_pages_outside_the_pool_and_lengths_outside_the_table():
     """Rows that see such a page, and sequences that do not fit: NaN.  The others as ever."""
     seqs = [(2, 70, 0), (2, 70, 0), (1, 40, 0), (3, 10, 0), (2, 5, 0)]

@@ -32,3 +32,14 @@ def test_direct_to_lds_stages_are_waited_for():
             assert "__syncthreads" not in body and "s_barrier" not in body, name
             assert "stage_wait<" in body, name
     assert {"k_gemm_rows", "k_attn_causal"} <= set(seen), seen
+
+
+def test_direct_to_lds_tiles_are_waited_for():
+    seen = []
+    for name, body in _kernels():
+        if "lds_load_tile" in body:
+            seen.append(name)
+            assert "__syncthreads" not in body and "s_barrier" not in body, name
+            # (the last wait: no load outlives the workgroup)
+            assert body.rindex("stage_wait<0>") > body.rindex("load("), name
+    assert "k_paged_rows" in seen, seen
