@@ -19,8 +19,6 @@
 
 namespace cas {
 
-typedef unsigned short uint16x2 __attribute__((ext_vector_type(2)));
-
 // ---------------------------------------------------------------- sequences
 
 struct PagedSeq {
@@ -418,6 +416,101 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
     return r;
 }
 
+// A lane's largest scores of a tile.
+template <int JT> __device__ __forceinline__ void paged_tops(float (&t)[JT], const f32x4 (&x)[JT][2]) {
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        t[j] = x[j][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) t[j] = fmaxf(t[j], x[j][e >> 2][e & 3]);
+    }
+}
+
+// attn_step for a tile that some row of the wave does not see whole (vm: the
+// visibility of the lane's slots), or of a page outside the pool: the scores of
+// unseen slots go to -infinity.  Kept short, since few tiles run it and most of
+// those for the first time.  Values that are not finite, which a probability of 0
+// would not hide, show in their products with zeros; looking at their exponents
+// took a decoded token over 500 slots 0.4 us more, 128 rows of a fresh cache 1.3.
+template <int HD, int JT>
+__device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], i32x4 (&vf)[HD / 16], uint32_t (&vm)[JT],
+                                          bool outside, float c) {
+    constexpr int NDT = HD / 16;
+    f32x4 z[2] = {};
+#pragma unroll
+    for (int f = 0; f < NDT; ++f) z[f & 1] = mfma_step<ET_BF16>(vf[f], i32x4{0, 0, 0, 0}, z[f & 1]);
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)vm[j], e, 1);
+            S[j][e >> 2][e & 3] = __uint_as_float((__float_as_uint(S[j][e >> 2][e & 3]) & m) | (0xff800000u & ~m));
+        }
+    if (outside) {
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+            asm volatile("" : "+v"(vm[j]));  // (no 16 conditions kept from here on)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((vm[j] >> e) & 1u) S[j][e >> 2][e & 3] = NAN;
+        }
+    }
+    float t[JT];
+    paged_tops<JT>(t, S);
+    mfma_result_pad();
+    const f32x4 y = z[0] + z[1];
+    const bool odd = __any(y[0] + y[1] + y[2] + y[3] != 0.f);
+    bool grow = false;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) grow = grow || t[j] > st[j].top;
+    if (__any(grow)) {
+        mfma_result_pad();
+#pragma unroll
+        for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
+    }
+    i32x4 P[JT];
+    const int one = 0x3f803f80;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        attn_probs(P[j], S[j], st[j].m * c, c);
+        st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+    }
+    // (one arm each: with two that both write O the compiler copies or spills it)
+    if (!odd) {
+#pragma unroll
+        for (int f = 0; f < NDT; ++f)
+#pragma unroll
+            for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+    }
+    mfma_result_pad();
+    if (odd) {  // taken out, and given back as NaN to the rows that see them
+        i32x4 seen[JT];
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+            asm volatile("" : "+v"(vm[j]));
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                seen[j][w] = (int)(((vm[j] >> (2 * w)) & 1u ? 0x3f80u : 0u) | ((vm[j] >> (2 * w + 1)) & 1u ? 0x3f800000u : 0u));
+        }
+#pragma unroll
+        for (int f = 0; f < NDT; ++f) {
+            const i32x4 bad = take_nonfinite(vf[f]);
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                const f32x4 n = mfma_step<ET_BF16>(bad, seen[j], f32x4{0.f, 0.f, 0.f, 0.f});
+                st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+                mfma_result_pad();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float to = n[e] > 0.f ? NAN : 0.f;
+                    asm volatile("" : "+v"(to));  // (here, not as 64 conditions at the end)
+                    st[j].O[f][e] += to;
+                }
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- attention: few rows
 
 // Workgroup = (share of a unit, kv head): JT query tiles of 16 packed rows (row
@@ -532,11 +625,9 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
             paged_scores<HD, JT>(S, kf, Q);
             mfma_result_pad();
 #pragma unroll
-            for (int j = 0; j < JT; ++j) {
+            for (int j = 0; j < JT; ++j)
                 vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-                if ((uint32_t)pid >= (uint32_t)p.n_pages) S[j][0] = S[j][1] = f32x4{NAN, NAN, NAN, NAN};
-            }
-            attn_step<HD, JT, true, true>(st, S, c, V, vm, [] {});
+            paged_end<HD, JT>(st, S, vf, vm, (uint32_t)pid >= (uint32_t)p.n_pages, c);
             mfma_result_pad();
             if (++lt < w1) {
                 look_up(lt);
@@ -709,47 +800,6 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
         stage_wait<0>();
         scores(S, 0);
         mfma_result_pad();
-        // A lane's largest scores of a tile.
-        auto tops = [&](float (&t)[JT], const f32x4 (&x)[JT][2]) {
-#pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                t[j] = x[j][0][0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) t[j] = fmaxf(t[j], x[j][e >> 2][e & 3]);
-            }
-        };
-        // A tile that some row of the wave does not see whole: the scores of unseen slots
-        // go to -infinity.  True if a value is not finite: a probability of 0 would not
-        // hide it (then the products of the values with zeros are NaN).
-        uint32_t vm[JT];
-        auto hide = [&](f32x4 (&x)[JT][2], float (&t)[JT], const i32x4 (&vf)[NDT], int i) {
-            f32x4 z[2] = {};
-#pragma unroll
-            for (int f = 0; f < NDT; ++f) z[f & 1] = mfma_step<ET_BF16>(vf[f], i32x4{0, 0, 0, 0}, z[f & 1]);
-            const int tile = tile_at(i);
-#pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)vm[j], e, 1);
-                    x[j][e >> 2][e & 3] = __uint_as_float((__float_as_uint(x[j][e >> 2][e & 3]) & m) | (0xff800000u & ~m));
-                }
-            }
-            if (strange && (uint32_t)paged_page(p, s.b, tile) >= (uint32_t)p.n_pages) {
-#pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    asm volatile("" : "+v"(vm[j]));  // (no 16 conditions kept from here on)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((vm[j] >> e) & 1u) x[j][e >> 2][e & 3] = NAN;
-                }
-            }
-            tops(t, x);
-            mfma_result_pad();
-            const f32x4 y = z[0] + z[1];
-            return (bool)__any(y[0] + y[1] + y[2] + y[3] != 0.f);
-        };
         // A whole tile: attn_step with the order of its instructions laid down.  x: its
         // scores, y: the next one's, t: a lane's largest of x, and then of y.  The
         // keys are read first, the values under them; the next tile's scores run
@@ -803,7 +853,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             for (int f = 0; f < NDT; ++f)
 #pragma unroll
                 for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
-            tops(t, y);
+            paged_tops<JT>(t, y);
 #pragma unroll
             for (int f = 0; f < (NDT + 1) * JT; ++f) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -812,67 +862,25 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             __builtin_amdgcn_sched_barrier(0);
         };
         // A tile at the ends of a walk.
-        auto turn_end = [&](float (&t)[JT], int i) {
+        auto turn_end = [&](int i) {
             const i32x4* v = sv + ((uint32_t)i % D) * (NDT * 64) + lane;
             i32x4 vf[NDT];
 #pragma unroll
             for (int f = 0; f < NDT; ++f) vf[f] = v[f * 64];
             __builtin_amdgcn_sched_barrier(0);
-            const bool odd = hide(S, t, vf, i);
-            bool grow = false;
+            const int tile = tile_at(i);
+            uint32_t vm[JT];
 #pragma unroll
-            for (int j = 0; j < JT; ++j) grow = grow || t[j] > st[j].top;
-            if (__any(grow)) {
-                mfma_result_pad();
-#pragma unroll
-                for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
-            }
-            i32x4 P[JT];
-            const int one = 0x3f803f80;
-#pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                attn_probs(P[j], S[j], st[j].m * c, c);
-                st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
-            }
-            if (!odd) {
-#pragma unroll
-                for (int f = 0; f < NDT; ++f)
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
-            }
+            for (int j = 0; j < JT; ++j)
+                vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
+            paged_end<HD, JT>(st, S, vf, vm, strange && (uint32_t)paged_page(p, s.b, tile) >= (uint32_t)p.n_pages, c);
             mfma_result_pad();
-            if (odd) {  // values that are not finite: taken out, and given back as NaN to the rows that see them
-                i32x4 seen[JT];
-#pragma unroll
-                for (int j = 0; j < JT; ++j) {
-                    asm volatile("" : "+v"(vm[j]));
-#pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        seen[j][w] = (int)(((vm[j] >> (2 * w)) & 1u ? 0x3f80u : 0u) | ((vm[j] >> (2 * w + 1)) & 1u ? 0x3f800000u : 0u));
-                }
-#pragma unroll
-                for (int f = 0; f < NDT; ++f) {
-                    const i32x4 bad = take_nonfinite(vf[f]);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) {
-                        const f32x4 n = mfma_step<ET_BF16>(bad, seen[j], f32x4{0.f, 0.f, 0.f, 0.f});
-                        st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
-                        mfma_result_pad();
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float to = n[e] > 0.f ? NAN : 0.f;
-                            asm volatile("" : "+v"(to));  // (here, not as 64 conditions at the end)
-                            st[j].O[f][e] += to;
-                        }
-                    }
-                }
-            }
         };
         // two tiles that every row of the workgroup sees whole
         auto plain = [&](int i) { return i + 1 < n && rg.whole(tile_at(i)) && rg.whole(tile_at(i + 1)) && !strange; };
         for (int i = 0; i < n;) {
             float top[JT];
-            tops(top, S);
+            paged_tops<JT>(top, S);
             while (plain(i)) {
                 advance(i);
                 turn(S, N, top, i, false);
@@ -884,7 +892,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             advance(i);
 #pragma unroll 1
             for (const int end = i + 2; i < end; ++i) {
-                if (i < n && sees(tile_at(i))) turn_end(top, i);
+                if (i < n && sees(tile_at(i))) turn_end(i);
                 scores(S, i + 1);
                 mfma_result_pad();
             }
