@@ -349,14 +349,14 @@ struct PagedAttnArgs {
     int H, sink, window;
     float *part_o, *part_ml;  // partial states of the shares of split units
     // set by the launch
-    int G, target, least, single, fold;
+    int G, target, whole, single, fold;
     uint32_t inv_G;
 };
 // How a call is launched: rows of a query tile, the most units of a kv head, the
-// shares aimed at beyond them (0: no unit is split), the least tiles of a share,
-// and the bytes of the partial states.
+// shares aimed at beyond them (0: no unit is split), the tiles of sequences that
+// are not split, and the bytes of the partial states.
 struct PagedPlan {
-    int R, units, target, least;
+    int R, units, target, whole;
     size_t work;
 };
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows);

@@ -309,6 +309,9 @@ struct PagedShare {
     int ns, nq, local, part;  // local: place among the sequence's; part: first partial of the sequence's
     bool found;
 };
+// The least tiles of a share: one for each of eight waves (1 row over 4095 slots 9.0
+// us, at least 16 tiles 9.4, 32 tiles 10.7; 32 rows at 1000 12.4, 13.9, 14.6).
+static constexpr int PAGED_LEAST = 8;
 template <bool MERGE>
 __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R, uint32_t inv_G, int item) {
     const PagedBatch& p = a.p;
@@ -362,24 +365,28 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         w = wave_total<float>(w) * 1.0001f;
         most = wave_most(most);
         auto share = [&](int n) {
-            return max(a.least, (int)fminf(1073741824.f, ceilf(w * __builtin_amdgcn_rcpf((float)n))));
+            return max(PAGED_LEAST, (int)fminf(1073741824.f, ceilf(w * __builtin_amdgcn_rcpf((float)n))));
         };
-        C = share(a.target);
-        // With room left by the units: as many shares as run at once, if the longest is
-        // then no longer than two rounds of the finer ones.  On 32 rows only if the
-        // finer ones do not run at once (64 rows, 8 sequences at 16000 slots, 8 heads:
-        // unsplit 160 us, in halves 109); on 16 a share too many costs more than a
-        // CU left over (8 sequences at 4095: three shares each 26 us, four 28).
-        if (nq < a.target) {
-            const int D = share(a.target - nq);
-            if (min(D, most) <= 2 * C && (R != 32 || shares_of(C) > a.target)) C = D;
-        }
-        // Where a workgroup has its CU to itself a tile takes it 0.57 us, where two
-        // share one 0.87; the partial states of twice the shares cost 5 us more.
-        if (nq < a.single) {
-            const int A = share(a.single - nq);
-            auto longest = [&](int c) { return (float)most * __builtin_amdgcn_rcpf(ceilf((float)most * __builtin_amdgcn_rcpf((float)c))); };
-            if (0.57f * longest(A) <= 0.87f * longest(C) + 5.f) C = A;
+        if (most > a.whole) {
+            C = share(a.target);
+            // With room left by the units: as many shares as run at once, if the longest
+            // is then no longer than two rounds of the finer ones.  On 32 rows only if
+            // the finer ones do not run at once (64 rows, 8 sequences at 16000 slots, 8
+            // heads: unsplit 160 us, in halves 109); on 16 a share too many costs more
+            // than a CU left over (8 sequences at 4095: three shares each 26 us, four 28).
+            if (nq < a.target) {
+                const int D = share(a.target - nq);
+                if (min(D, most) <= 2 * C && (R != 32 || shares_of(C) > a.target)) C = D;
+            }
+            // Where a workgroup has its CU to itself a tile takes it 0.57 us, where two
+            // share one 0.87; the partial states of twice the shares cost 5 us more.
+            if (nq < a.single) {
+                const int A = share(a.single - nq);
+                auto longest = [&](int c) {
+                    return (float)most * __builtin_amdgcn_rcpf(ceilf((float)most * __builtin_amdgcn_rcpf((float)c)));
+                };
+                if (0.57f * longest(A) <= 0.87f * longest(C) + 5.f) C = A;
+            }
         }
     }
     const float rC = __builtin_amdgcn_rcpf((float)C);
@@ -523,7 +530,7 @@ __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
 // MB: 54 us, 5.1 TB/s; one of 131072, 537 MB: 105; with keys and values of a tile
 // loaded together 66); 32 rows, of memory at 4 to 5 TB/s, and of the L2s
 // where several units read the same slots; few slots, the waits at the start and the
-// joins (one row over 500 slots 6.3 us, over 1000 8.1, over 4095, in shares, 9.5).
+// joins (one row over 500 slots 5.9 us, over 1000 7.5, over 4095, in shares, 9.0).
 static constexpr int PAGED_WAVES = 8;
 static_assert(64 * PAGED_WAVES <= PAGED_MOST_THREADS);
 
@@ -994,10 +1001,10 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
 // waves, each with every eighth key tile, is done sooner: 64 rows on one sequence of
 // 4000 slots, 8 heads, 14 us of 32 and 19 of 128, at 64000 slots 48 and 57; 256 rows
 // at 1000 slots 14 and 17, at 8000 22 and 27, at 64000 97 and 87.
-// Least: a share of 32 tiles on 16 rows (one of 1000 slots 8 us, in two shares 9.6),
-// of 8 on more (32 rows at 1000 slots 12.4 us, at least 16 tiles 13.9, 32 tiles 14.6).
-// Sequences that no share of 16 tiles would split are not worth a second kernel that
-// looks for split ones (2.6 us).
+// Not split: calls whose sequences have up to 32 tiles on 16 rows (one of 1000 slots
+// 7.5 us, in two shares 9.6), up to 16 on more (128 rows behind 300 slots 11.7 us,
+// split 13.3): a split costs the second kernel's 2.6 us even if it finds nothing,
+// which a table that allows no longer sequence saves too.
 static constexpr int PAGED_CUS = 256;
 
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
@@ -1007,8 +1014,8 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     q.R = most <= 16 ? 16 : most <= 32 || (few && (most <= 64 || p.cap <= 8192)) ? 32 : PROWS_R;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
     q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
-    q.least = q.R == 16 ? 32 : 8;
-    if ((p.cap >> 5) <= (q.R == 16 ? 32 : 16)) q.target = 0;  // no sequence is split
+    q.whole = q.R == 16 ? 32 : 16;
+    if ((p.cap >> 5) <= q.whole) q.target = 0;  // no sequence is split
     q.work = q.target ? (size_t)2 * q.target * p.Hkv * q.R * (p.hd + 2) * sizeof(float) : 0;
     return q;
 }
@@ -1038,7 +1045,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q,
     a.inv_G = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.target = q.target;
     a.single = q.R == PROWS_R ? (PAGED_CUS + p.Hkv - 1) / p.Hkv : 0;
-    a.least = q.least;
+    a.whole = q.whole;
     a.fold = (int64_t)(q.units - p.B) * p.Hkv <= 2 * PAGED_CUS;
     a.part_ml = a.part_o + (size_t)2 * q.target * p.Hkv * q.R * p.hd;
     const float c = (1.0f / sqrtf((float)p.hd)) * 1.4426950408889634f;
