@@ -753,8 +753,9 @@ def op_logprobs(logits, tokens, logp, entropy=None, top_ids=None, top_logp=None,
     n, V = logits.shape
     bf16 = logits.dtype in kv.b16
     ld = _row_stride(what, "logits", logits, n, V, None, kv.b16 if bf16 else kv.f32)
-    m = 0 if tokens is None else tokens.numel() // n if n else 0
-    K = 0 if top_ids is None else top_ids.numel() // n if n else 0
+    m, K = (0 if x is None or not n else x.numel() // n for x in (tokens, top_ids))
+    if tokens is not None and tokens.numel() != n * m or top_ids is not None and top_ids.numel() != n * K:
+        _refuse(what, f"tokens and top_ids are not as many for each of {n} rows")
     if work is None:
         work = _work(L.cas_op_logprobs_work_bytes(n, V, K), stream)
     s, (xa, ta, la, ea, ia, ba, wa) = _call_at(

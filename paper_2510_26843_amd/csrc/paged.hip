@@ -313,7 +313,7 @@ struct PagedShare {
 // us, at least 16 tiles 9.4, 32 tiles 10.7; 32 rows at 1000 12.4, 13.9, 14.6).
 static constexpr int PAGED_LEAST = 8;
 template <bool MERGE>
-__device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R, uint32_t inv_G, int item) {
+__device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R, int item) {
     const PagedBatch& p = a.p;
     const int lane = threadIdx.x & 63, G = a.G;
     const bool tree = a.anc != nullptr;
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4, G = a.G;
     const int kvh = blockIdx.x % p.Hkv;
-    const PagedShare sh = paged_share<false>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    const PagedShare sh = paged_share<false>(a, R, blockIdx.x / p.Hkv);
     if (!sh.found) return;
     const PagedSeq& s = sh.s;
     const bool tree = a.anc != nullptr;
@@ -710,7 +710,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4, G = a.G;
     const int kvh = blockIdx.x % p.Hkv;
-    const PagedShare sh = paged_share<false>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+    const PagedShare sh = paged_share<false>(a, R, blockIdx.x / p.Hkv);
     if (!sh.found) return;
     const PagedSeq& s = sh.s;
     const bool tree = a.anc != nullptr;
@@ -944,7 +944,7 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
     // (one wave looks: up to eight workgroups share a CU)
     __shared__ PagedShare sm_sh;
     if (threadIdx.x < 64) {
-        const PagedShare found = paged_share<true>(a, R, a.inv_G, blockIdx.x / p.Hkv);
+        const PagedShare found = paged_share<true>(a, R, blockIdx.x / p.Hkv);
         if (threadIdx.x == 0) sm_sh = found;
     }
     __syncthreads();

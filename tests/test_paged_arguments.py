@@ -152,7 +152,8 @@ def test_logprobs_takes(calls, change, lt, ld, m, K):
     (dict(logits=_z(ROWS, 2 * V, dtype=F)[:, ::2]), "logits"), (dict(logits=_z(V, ROWS, dtype=F).t()), "logits"),
     (dict(tokens=_z(ROWS, 2, dtype=A)), "tokens"), (dict(tokens=_z(ROWS, 4, dtype=I)[:, ::2]), "tokens"),
     (dict(logp=_z(ROWS, 1, dtype=F)), "logp"), (dict(logp=_z(ROWS, 2)), "logp"), (dict(entropy=_z(ROWS - 1, dtype=F)), "entropy"),
-    (dict(top_ids=_z(ROWS, 4, dtype=A)), "top_ids"), (dict(top_logp=_z(ROWS, 3, dtype=F)), "top_logp")])
+    (dict(top_ids=_z(ROWS, 4, dtype=A)), "top_ids"), (dict(tokens=_z(ROWS + 1, dtype=I)), "tokens"),
+    (dict(top_ids=_z(2 * ROWS - 1, dtype=I)), "tokens and top_ids"), (dict(top_logp=_z(ROWS, 3, dtype=F)), "top_logp")])
 def test_logprobs_refuses(calls, change, name):
     with pytest.raises(cas.CasError, match=rf"CAS_ERR_ARG.*: {name} "):
         _score(**change)
