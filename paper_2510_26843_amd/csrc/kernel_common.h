@@ -147,9 +147,9 @@ template <int NF> __device__ __forceinline__ void lds_load_tile(const char* base
 #pragma unroll
     for (int f = 0; f < NF; f += 4)
         asm volatile(
-            "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024\n\t"
-            "global_load_lds_dwordx4 %0, %1 offset:2048\n\tglobal_load_lds_dwordx4 %0, %1 offset:3072" ::"v"(voff),
-            "s"(base + f * 1024), "s"(lds + f * 1024)
+            "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3\n\t"
+            "global_load_lds_dwordx4 %0, %1 offset:%4\n\tglobal_load_lds_dwordx4 %0, %1 offset:%5" ::"v"(voff),
+            "s"(base + f * 1024), "s"(lds + f * 1024), "n"(1024), "n"(2 * 1024), "n"(3 * 1024)
             : "memory");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
