@@ -370,13 +370,15 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttnArgs& a, int R,
         if (most > a.whole) {
             C = share(a.target);
             // With room left by the units: as many shares as run at once, if the longest
-            // is then no longer than two rounds of the finer ones.  On 32 rows only if
+            // is then no longer than two rounds of the finer ones (and the partial states
+            // of 128 rows, as many bytes written and read as eight tiles: 5 ragged chunks
+            // of up to 400 rows, 40 heads, 53.7 us without, 50.2 with).  On 32 rows only if
             // the finer ones do not run at once (64 rows, 8 sequences at 16000 slots, 8
             // heads: unsplit 160 us, in halves 109); on 16 a share too many costs more
             // than a CU left over (8 sequences at 4095: three shares each 26 us, four 28).
             if (nq < a.target) {
                 const int D = share(a.target - nq);
-                if (min(D, most) <= 2 * C && (R != 32 || shares_of(C) > a.target)) C = D;
+                if (min(D, most) <= 2 * C + (R == 128 ? 8 : 0) && (R != 32 || shares_of(C) > a.target)) C = D;
             }
             // Where a workgroup has its CU to itself a tile takes it 0.57 us, where two
             // share one 0.87; the partial states of twice the shares cost 5 us more.
