@@ -7,6 +7,24 @@
 
 namespace cas {
 
+// x / d for 0 <= x < 2^31 and 1 <= d <= 65536, by a product and a shift: with 2^s < d
+// <= 2^(s + 1) and m = (2^(32 + s) + e) / d whole, 0 <= e < d, the quotient x m /
+// 2^(32 + s) lies above x / d by x e / (d 2^(32 + s)), less than the 1 / d that could
+// change its floor, since x e < 2^(32 + s).
+struct Quotient {
+    uint32_t m = 0;  // 0: d is 1
+    int s = 0;
+    Quotient() = default;
+    explicit Quotient(int d) {
+        if (d < 2) return;
+        while ((2 << s) < d) ++s;
+        m = (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d);
+    }
+    __host__ __device__ __forceinline__ int operator()(int x) const {
+        return m ? (int)((uint32_t)(((uint64_t)(uint32_t)x * m) >> 32) >> s) : x;
+    }
+};
+
 enum ElemType { ET_F32 = 0, ET_BF16 = 1, ET_I8 = 2, ET_I4 = 3 };
 
 // ---------------------------------------------------------------------------
@@ -350,7 +368,7 @@ struct PagedAttnArgs {
     float *part_o, *part_ml;  // partial states of the shares of split units
     // set by the launch
     int G, target, whole, single, fold;
-    uint32_t inv_G;
+    Quotient by_G;
 };
 // How a call is launched: rows of a query tile, the most units of a kv head, the
 // shares aimed at beyond them (0: no unit is split), the tiles of sequences that

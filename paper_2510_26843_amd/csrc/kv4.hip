@@ -972,7 +972,7 @@ hipError_t launch_attention_kv4(const Kv4AttnArgs& k, hipStream_t s) {
     Kv4AttnArgs k2 = k;
     k2.G = a.H / a.Hkv;
     k2.Rp = attn_head_rows(a.T);
-    // (multiplying by these and taking the high word divides exactly below 2^25)
+    // (multiplying by these and taking the high word divides by up to 128 exactly below 2^25)
     auto inverse = [](int d) { return d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u; };
     k2.inv_Rp = inverse(k2.Rp);
     k2.inv_S = inverse(S);

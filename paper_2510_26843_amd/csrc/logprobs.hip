@@ -502,7 +502,7 @@ hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     const hipError_t e = hipLaunchKernel((const void*)kernel, grid, dim3(p.threads), part_at,
                                          a.K > 0 ? (size_t)p.span * p.threads * 4 : 0, s);
     if (e != hipSuccess || p.parts == 1) return e;
-    // (multiplying by it and taking the high word divides exactly below 2^25)
+    // (multiplying by it and taking the high word divides by up to 128 exactly below 2^25)
     uint32_t inv_K = a.K > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.K - 1) / a.K) : 0u;
     void* at[] = {(void*)&b, (void*)&c, (void*)&w, (void*)&inv_K};
     return hipLaunchKernel((const void*)k_logprob_join, dim3(a.n), dim3(64), at, (size_t)(p.parts * a.K + 8) * 8, s);

@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
     const PagedSeq& s = sh.s;
     const bool tree = a.anc != nullptr;
     const int qt = sh.local % sh.nq, split = sh.local / sh.nq;
-    auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
+    auto token = [&](int x) { return a.by_G(x); };
     const int rows = s.T * G, p0 = qt * R;
     const int t0 = token(p0), t1 = token(min(p0 + R, rows) - 1) + 1;
 
@@ -722,7 +722,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
     // heads: 54 us, else 57).
     const int split = sh.local / sh.nq, at = sh.local - split * sh.nq, half = (sh.nq + 1) / 2;
     const int qt = a.fold && at >= half ? at - half : sh.nq - 1 - at;
-    auto token = [&](int x) { return a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x; };
+    auto token = [&](int x) { return a.by_G(x); };
     const int rows = s.T * G, p0 = qt * R, w0 = p0 + wave * 16 * JT;
     const bool live = w0 < rows && s.fits;
 
@@ -988,7 +988,7 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
         }
         if (sub == 0 && i0 + gi / NS < rows) {
             const float inv = L != 0.f ? 1.f / L : 0.f;
-            const int x = p0 + i, t = a.inv_G ? (int)__umulhi((uint32_t)x, a.inv_G) : x;
+            const int x = p0 + i, t = a.by_G(x);
             st4(a.out, ((size_t)(sh.s.row0 + t) * a.H + kvh * G + (x - t * G)) * HD + d4, acc[0][0] * inv,
                 acc[0][1] * inv, acc[0][2] * inv, acc[0][3] * inv);
         }
@@ -1043,8 +1043,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs& args, const PagedPlan& q,
     const PagedBatch& p = a.p;
     if (p.N < 1 || p.B < 1 || p.Hkv < 1 || a.H % p.Hkv) return hipErrorInvalidValue;
     a.G = a.H / p.Hkv;
-    // (multiplying by it and taking the high word divides exactly below 2^25)
-    a.inv_G = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
+    a.by_G = Quotient(a.G);
     a.target = q.target;
     a.single = q.R == PROWS_R ? (PAGED_CUS + p.Hkv - 1) / p.Hkv : 0;
     a.whole = q.whole;
