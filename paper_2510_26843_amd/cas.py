@@ -525,8 +525,8 @@ class _KV4:
         self.attend = (b16, u8, i64, b16, b16, b16, u8)
         self.f32 = f32
         self.paged = (b16, i32, i32, i32, i32)
-        self.append_paged = (b16, b16, b16, b16, i32, f32, f32)
-        self.attend_paged = (b16, b16, i64, u8)
+        self.append_paged = (b16, b16, b16, b16, i32, f32, f32, b16)
+        self.attend_paged = (b16, b16, i64, u8, b16)
         self.logprobs = (b16 + f32, i32, f32, f32, i32, f32, u8)
 
 
@@ -719,9 +719,10 @@ def op_paged_append(cache: Paged, k, v, q=None, q_out=None, pos=None, cos=None, 
             _refuse(what, "cos is not [positions][hd / 2]")
         n_pos = shape[0]
     angles = 2 * n_pos * hd
-    s, (ka, va, qa, oa, pa, ca, sa) = _call_at(
-        kv.torch, stream, what, "k v q q_out pos cos sin", (k, v, q, q_out, pos, cos, sin), kv.append_paged,
-        (0, 0, 0, 2 * N * wq, 4 * N if n_pos else 0, angles, angles))
+    # (the batch's tensors lie where its pages do)
+    s, (ka, va, qa, oa, pa, ca, sa, _) = _call_at(
+        kv.torch, stream, what, "k v q q_out pos cos sin pages", (k, v, q, q_out, pos, cos, sin, cache.tensors[0]),
+        kv.append_paged, (0, 0, 0, 2 * N * wq, 4 * N if n_pos else 0, angles, angles, 0))
     _ochk(lib().cas_op_paged_append(ctypes.addressof(cache), qa, ldq, H, ka, ldk, va, ldv, pa, ca, sa, n_pos, oa, s), what)
 
 
@@ -737,8 +738,8 @@ def op_attention_paged(cache: Paged, q, out, anc=None, sink: int = 0, window: in
         need = L.cas_op_attention_paged_work_bytes(at, H)
         work = _work(need, stream) if need else None
     rows = 2 * N * H * cache.head_dim
-    s, (qa, oa, aa, wa) = _call_at(kv.torch, stream, what, "q out anc work", (q, out, anc, work), kv.attend_paged,
-                                   (rows, rows, 16 * N, 0))
+    s, (qa, oa, aa, wa, _) = _call_at(kv.torch, stream, what, "q out anc work pages", (q, out, anc, work, cache.tensors[0]),
+                                      kv.attend_paged, (rows, rows, 16 * N, 0, 0))
     _ochk(L.cas_op_attention_paged(at, qa, H, aa, sink, window, oa, wa, 0 if work is None else work.nbytes, s), what)
 
 

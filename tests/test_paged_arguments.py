@@ -183,3 +183,29 @@ def test_logprob_work_serves_fewer_rows(vocab):
     sizes = [f(n, vocab, 32) for n in range(1, 700)]
     assert sizes == sorted(sizes) and sizes[0] >= 16
     assert all(f(n, vocab, K) <= f(n, vocab, 32) for n in (1, 33, 257) for K in (0, 1, 8))
+
+
+class _Elsewhere:
+    """A tensor that says it lies on device 0."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def get_device(self):
+        return 0
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+@pytest.mark.parametrize("call", [_append, _attend])
+def test_a_batch_of_another_device(calls, monkeypatch, call):
+    """Made where device 0 is current, used with rows of another one that is current then."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cache = cas.Paged(*(_Elsewhere(x) if isinstance(x, torch.Tensor) else x for x in (
+        _z(7, 2, HKV, PAGE * HD), PAGE, HD, _z(SEQS, 4, dtype=I), _z(SEQS + 1, dtype=I), _z(SEQS, dtype=I), N)))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(cas, "Paged", lambda **kw: cache)
+    with pytest.raises(cas.CasError, match="CAS_ERR_ARG.*not on the current device"):
+        call()
+    assert not calls
