@@ -334,6 +334,8 @@ class Model:
         last forward, softmax(scale * logits): (logp of the tokens' shape,
         entropy [n], top ids [n][K], their log probabilities [n][K])."""
         t = np.ascontiguousarray(tokens, dtype=np.int32)
+        if t.ndim > 2:
+            _refuse("cas_logprobs", "tokens is neither [rows] nor [rows][tokens]")
         n, m = t.shape[0], 1 if t.ndim == 1 else t.shape[1]
         logp, entropy = np.zeros(t.shape, dtype=np.float32), np.zeros(n, dtype=np.float32)
         ids, best = np.zeros((n, K), dtype=np.int32), np.zeros((n, K), dtype=np.float32)
