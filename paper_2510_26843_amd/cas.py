@@ -167,6 +167,12 @@ def _p(a: np.ndarray) -> int:
     return a.ctypes.data
 
 
+def token_ids(tokens) -> np.ndarray:
+    """Tokens in 32 bits; -1, which is none, for what they do not hold."""
+    t = np.asarray(tokens)
+    return np.ascontiguousarray(np.where((t >= 0) & (t < 2**31), t, -1), dtype=np.int32)
+
+
 def tree_info(parents: Sequence[int]) -> Tuple[np.ndarray, np.ndarray]:
     """Depth and 128-bit ancestor-or-self masks ([n][2] uint64) as the library computes them."""
     par = np.ascontiguousarray(parents, dtype=np.int32)
@@ -333,7 +339,7 @@ class Model:
         """Log probabilities of tokens [n][m] (or [n]) under the n rows of the
         last forward, softmax(scale * logits): (logp of the tokens' shape,
         entropy [n], top ids [n][K], their log probabilities [n][K])."""
-        t = np.ascontiguousarray(tokens, dtype=np.int32)
+        t = token_ids(tokens)
         if t.ndim > 2:
             _refuse("cas_logprobs", "tokens is neither [rows] nor [rows][tokens]")
         n, m = t.shape[0], 1 if t.ndim == 1 else t.shape[1]

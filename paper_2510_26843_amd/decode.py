@@ -12,7 +12,7 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 
-from .cas import Model
+from .cas import Model, token_ids
 
 
 def _top(row: np.ndarray, b: int) -> List[int]:
@@ -41,7 +41,7 @@ def score(model: Model, tokens: Sequence[int], K: int = 0, scale: float = 1.0):
     before it: (logp [n - 1], entropy [n - 1], top ids [n - 1][K], their log
     probabilities).  The text is committed, a chain of up to max_tree tokens per
     forward, whose rows are scored on the device."""
-    t = np.ascontiguousarray(tokens, dtype=np.int32)
+    t = token_ids(tokens)
     model.set_committed(0)
     parts = []
     for a in range(0, len(t), model.max_tree):

@@ -5,7 +5,7 @@ import ctypes
 import numpy as np
 import pytest
 
-from paper_2510_26843_amd import cas
+from paper_2510_26843_amd import cas, decode
 
 V = 100
 
@@ -48,3 +48,17 @@ def test_tokens_that_are_not_of_rows(model, tokens):
     with pytest.raises(cas.CasError) as e:
         model.logprobs(tokens)
     assert e.value.status == cas.ERR_ARG and not model._L.calls
+
+
+def test_ids_that_32_bits_do_not_hold_are_no_tokens(model):
+    logp = model.logprobs(np.array([[2**32 + 5, 7], [-(2**32) + 5, 2**31]], dtype=np.int64))[0]
+    assert np.array_equal(np.isnan(logp), [[True, False], [True, True]]) and logp[0, 1] == -8
+    logp = model.logprobs(np.array([2**64 - 2**32 + 5, 6], dtype=np.uint64))[0]
+    assert np.isnan(logp[0]) and logp[1] == -7
+
+
+def test_a_text_with_such_an_id_reaches_no_other_token(model, monkeypatch):
+    seen = []
+    monkeypatch.setattr(model, "forward", lambda t, *a, **kw: seen.extend(np.asarray(t, dtype=np.int32).tolist()))
+    decode.score(model, np.array([1, 2**32 + 5, 3], dtype=np.int64))
+    assert seen == [1, -1, 3]  # (the library refuses a token of -1)
