@@ -39,8 +39,9 @@ def ar_decode(model: Model, prompt: Sequence[int], n_new: int) -> List[int]:
 def score(model: Model, tokens: Sequence[int], K: int = 0, scale: float = 1.0):
     """Log probability of every token of a text but its first, given those
     before it: (logp [n - 1], entropy [n - 1], top ids [n - 1][K], their log
-    probabilities).  The text is committed, a chain of up to max_tree tokens per
-    forward, whose rows are scored on the device."""
+    probabilities); empty ones for a text of one token or none.  The text takes
+    the place of what the model had committed, a chain of up to max_tree tokens
+    per forward, whose rows are scored on the device."""
     t = token_ids(tokens)
     model.set_committed(0)
     parts = []
@@ -50,6 +51,8 @@ def score(model: Model, tokens: Sequence[int], K: int = 0, scale: float = 1.0):
         model.compact(range(n))
         given = np.append(t[a + 1:a + n + 1], [-1] * (a + n + 1 - len(t)))  # (nothing follows the last token)
         parts.append(model.logprobs(given, K, scale))
+    if not parts:
+        return (np.zeros(0, np.float32), np.zeros(0, np.float32), np.zeros((0, K), np.int32), np.zeros((0, K), np.float32))
     return tuple(np.concatenate(p)[:-1] for p in zip(*parts))
 
 

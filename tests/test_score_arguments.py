@@ -62,3 +62,11 @@ def test_a_text_with_such_an_id_reaches_no_other_token(model, monkeypatch):
     monkeypatch.setattr(model, "forward", lambda t, *a, **kw: seen.extend(np.asarray(t, dtype=np.int32).tolist()))
     decode.score(model, np.array([1, 2**32 + 5, 3], dtype=np.int64))
     assert seen == [1, -1, 3]  # (the library refuses a token of -1)
+
+
+@pytest.mark.parametrize("K", [0, 3])
+def test_a_text_without_tokens_has_no_scores(model, K):
+    logp, entropy, ids, best = decode.score(model, [], K)
+    assert logp.shape == entropy.shape == (0,) and ids.shape == best.shape == (0, K)
+    one = decode.score(model, [7], K)
+    assert [(x.shape, x.dtype) for x in one] == [(x.shape, x.dtype) for x in (logp, entropy, ids, best)]
