@@ -376,7 +376,7 @@ cas_status cas_op_attention_paged(const cas_paged* cache, const void* q, int32_t
  *            -infinity past the row's finite entries)
  * A logit of -infinity has probability 0.  A row that holds a NaN or +infinity,
  * or nothing but -infinity, has no distribution: NaN, and ids -1.
- * scale: finite and > 0 (1 / temperature).  V at most 1048576, n at most
+ * scale: > 0 (1 / temperature), its product with log2(e) finite.  V at most 1048576, n at most
  * 2097152.  Sums in fp32.
  * work: device scratch of cas_op_logprobs_work_bytes(...) bytes (no less for
  * more rows or a larger K), 16-byte aligned, used by one call at a time.

@@ -1353,6 +1353,9 @@ cas_status cas_topk(cas_ctx* c, int32_t n, int32_t K, int32_t* ids, float* probs
     return CAS_OK;
 }
 
+// (the exponents are in log2 units: 1.44 times the scale has to be a number too)
+static bool logprob_scale(float scale) { return scale > 0.f && std::isfinite(scale * 1.4426950408889634f); }
+
 static constexpr int kLogpTokens = 128, kLogpTop = 32;  // most tokens and alternatives of a row
 
 cas_status cas_logprobs(cas_ctx* c, int32_t n, float scale, const int32_t* tokens, int32_t m, float* logp,
@@ -1362,7 +1365,7 @@ cas_status cas_logprobs(cas_ctx* c, int32_t n, float scale, const int32_t* token
     if (K < 0 || K > kLogpTop) return fail(c, CAS_ERR_ARG, "K must be in [0, 32]");
     if ((m && (!tokens || !logp)) || (K && (!top_ids || !top_logp)))
         return fail(c, CAS_ERR_ARG, "tokens and output pointers must not be NULL");
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(c, CAS_ERR_ARG, "scale must be finite and > 0");
+    if (!logprob_scale(scale)) return fail(c, CAS_ERR_ARG, "scale must be > 0 and scale * log2(e) finite");
     if (c->logits_rows < 1) return fail(c, CAS_ERR_STATE, "cas_logprobs needs a forward first");
     if (n != c->logits_rows)
         return fail(c, CAS_ERR_ARG, "n must equal the last forward's row count " + std::to_string(c->logits_rows));
@@ -2064,7 +2067,7 @@ cas_status cas_op_logprobs(int32_t ltype, const void* logits, int64_t ld, int32_
     if (ltype != CAS_W_F32 && ltype != CAS_W_BF16) return CAS_ERR_UNSUPPORTED;
     if (!logits || !work || !logprobs_shape(n, V, K) || ld < V || m < 0) return CAS_ERR_ARG;
     if ((m && (!tokens || !logp)) || (K && (!top_ids || !top_logp))) return CAS_ERR_ARG;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return CAS_ERR_ARG;
+    if (!logprob_scale(scale)) return CAS_ERR_ARG;
     if ((uintptr_t)logits & (ltype == CAS_W_F32 ? 3 : 1)) return CAS_ERR_ARG;
     if (((uintptr_t)tokens | (uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)top_ids | (uintptr_t)top_logp) & 3) return CAS_ERR_ARG;
     if (!aligned16(work) || work_bytes < logprob_work_bytes(n, V, K)) return CAS_ERR_ARG;

@@ -229,6 +229,7 @@ static void host_checks(void) {
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 0.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, NAN, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, INFINITY, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
+    CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 2.4e38f, NULL, 0, NULL, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 1, f, f, 0, NULL, NULL, p, 1 << 20, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 2, NULL, f, p, 1 << 20, NULL) == CAS_ERR_ARG);
     CHECK(cas_op_logprobs(CAS_W_F32, p, 100, 1, 100, 1.f, NULL, 0, NULL, f, 0, NULL, NULL, p, 0, NULL) == CAS_ERR_ARG);
@@ -352,6 +353,7 @@ static void error_paths(cas_ctx* c, const shape_t* s) {
     CHECK(cas_logprobs(c, 4, 1.f, NULL, 2, probs, NULL, 0, NULL, NULL) == CAS_ERR_ARG);
     CHECK(cas_logprobs(c, 4, 1.f, NULL, 0, NULL, NULL, 33, ids, probs) == CAS_ERR_ARG);
     CHECK(cas_logprobs(c, 4, 1.f, NULL, 0, NULL, NULL, 2, ids, NULL) == CAS_ERR_ARG);
+    CHECK(cas_logprobs(c, 4, 2.4e38f, NULL, 0, NULL, probs, 0, NULL, NULL) == CAS_ERR_ARG);
     CHECK(cas_logprobs(c, 4, -1.f, NULL, 0, NULL, probs, 0, NULL, NULL) == CAS_ERR_ARG);
     CHECK(cas_logits_device(c, NULL, &na) == CAS_ERR_ARG);
     CHECK(committed(c) == Lc);

@@ -1,0 +1,44 @@
+"""Scores at the ends of what the calls take: the largest scale, parts of as many
+chunks as one may have, scratch of exactly the reported size."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2510_26843_amd import cas, synth
+from tests.test_gpu_logprobs import DEV, _logits, _run
+
+pytestmark = pytest.mark.gpu
+
+# the largest fp32 whose product with log2(e) is one
+LARGEST = np.nextafter(np.float32(np.finfo(np.float32).max / np.log2(np.e)), np.float32(0))
+
+
+@pytest.mark.parametrize("V", [500, 40000])
+def test_the_largest_scale(V):
+    x = _logits(3, V, False)
+    x[1] = -2.0
+    x[2, 3:7] = x[2].max()
+    best = x[2].max().item()
+    logp, ent, ids, top = _run(x, [[3, 0]] * 3, 2, scale=float(LARGEST))
+    M = int(x[0].argmax())
+    assert logp[0, 0] == (0 if M == 3 else -np.inf) and ent[0] == 0 and ids[0, 0] == M and top[0, 0] == 0
+    # (equal logits: - log n, within 2^-22 of it and of the sum's 2^-18)
+    assert np.abs(logp[1] + np.log(V)).max() < 1e-5 and abs(ent[1] - np.log(V)) < 1e-5 and list(ids[1]) == [0, 1]
+    n = int((x[2] == best).sum())
+    assert abs(logp[2, 0] + np.log(n)) < 1e-5 and abs(ent[2] - np.log(n)) < 1e-5
+    for scale in (float(np.nextafter(LARGEST, np.float32(np.inf))) * (1 + 1e-6), 3e38):
+        with pytest.raises(cas.CasError, match="CAS_ERR_ARG"):
+            _run(x, [[3, 0]] * 3, 2, scale=scale)
+
+
+def test_the_largest_scale_of_a_model():
+    shape = synth.SHAPES["tiny"]
+    m = cas.Model(shape, max_ctx=128)
+    m.load_weights(synth.gen_weights(shape, seed=3))
+    logits = m.forward([1, 2], [-1, 0])
+    logp, ent, ids, best = m.logprobs(logits.argmax(1), 1, float(LARGEST))
+    assert (logp == 0).all() and (ent == 0).all() and np.array_equal(ids[:, 0], logits.argmax(1)) and (best == 0).all()
+    with pytest.raises(cas.CasError) as e:
+        m.logprobs([1, 2], 0, 3e38)
+    assert e.value.status == cas.ERR_ARG
+    m.close()

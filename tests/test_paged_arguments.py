@@ -209,3 +209,10 @@ def test_a_batch_of_another_device(calls, monkeypatch, call):
     with pytest.raises(cas.CasError, match="CAS_ERR_ARG.*not on the current device"):
         call()
     assert not calls
+
+
+@pytest.mark.parametrize("scale,status", [(2.4e38, cas.ERR_ARG), (3.4e38, cas.ERR_ARG), (float("inf"), cas.ERR_ARG)])
+def test_scales_whose_exponents_overflow(scale, status):
+    """In log2 units the scale is 1.44 times itself, which fp32 has to hold."""
+    p = 4096  # (an address that a refused call does not look at)
+    assert cas.lib().cas_op_logprobs(cas.W_F32, p, 100, 1, 100, scale, None, 0, None, p, 0, None, None, p, 1 << 20, None) == status
