@@ -246,13 +246,14 @@ cas_status cas_topk(cas_ctx* ctx, int32_t n, int32_t K, int32_t* ids, float* pro
 /*
  * Log probabilities under the last forward's logits (verify or draft): row i's
  * distribution is softmax(scale * logits[i]) (scale = 1 / temperature, > 0, its
- * product with log2(e) finite).  tokens [n][m]: logp [n][m] their log probabilities (NaN for an id
- * outside [0, vocab)); entropy [n] (may be NULL); top_ids, top_logp [n][K]: the
- * K tokens of highest logit (as cas_topk) with their log probabilities, -1 and
- * -infinity past the row's finite entries.  n must equal the last forward's row
- * count; m in [0, 128], K in [0, 32], host arrays.  NaN logits give
- * CAS_ERR_DEVICE.  The first call allocates its buffers (freed with the
- * context).  Synchronous.
+ * product with log2(e) finite).  tokens [n][m]: logp [n][m] their log
+ * probabilities (NaN for an id outside [0, vocab)); entropy [n] (may be NULL);
+ * top_ids, top_logp [n][K]: the K tokens of highest logit (as cas_topk) with
+ * their log probabilities, -1 and -infinity past the row's finite entries.  n
+ * must equal the last forward's row count; m in [0, 128], K in [0, 32], host
+ * arrays.  A row that holds a NaN or +infinity, or nothing but -infinity, has no
+ * distribution: CAS_ERR_DEVICE.  The first call allocates its buffers (freed with
+ * the context).  Synchronous.
  */
 cas_status cas_logprobs(cas_ctx* ctx, int32_t n, float scale, const int32_t* tokens, int32_t m, float* logp,
                         float* entropy, int32_t K, int32_t* top_ids, float* top_logp);

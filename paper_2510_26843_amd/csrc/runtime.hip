@@ -1406,7 +1406,9 @@ cas_status cas_logprobs(cas_ctx* c, int32_t n, float scale, const int32_t* token
     cas_status cst = poll_checks(c);
     if (cst != CAS_OK) return cst;
     for (int i = 0; i < n; ++i)
-        if (a.entropy[i] != a.entropy[i]) return fail(c, CAS_ERR_DEVICE, "NaN in the logits of row " + std::to_string(i));
+        if (a.entropy[i] != a.entropy[i])
+            return fail(c, CAS_ERR_DEVICE, "row " + std::to_string(i) +
+                                               " has no distribution (a logit of NaN or +infinity, or none that is finite)");
     if (m) memcpy(logp, a.logp, sizeof(float) * (size_t)n * m);
     if (entropy) memcpy(entropy, a.entropy, sizeof(float) * (size_t)n);
     if (K) {

@@ -42,3 +42,26 @@ def test_the_largest_scale_of_a_model():
         m.logprobs([1, 2], 0, 3e38)
     assert e.value.status == cas.ERR_ARG
     m.close()
+
+
+def test_a_row_without_a_distribution_is_called_that():
+    """A logit of +infinity leaves none, and holds no NaN; one of -infinity has probability 0."""
+    shape = synth.SHAPES["tiny"]
+    w = synth.gen_weights(shape, seed=3)
+    w["lm_head"] = w["lm_head"].copy()
+    signs = set()
+    for value in (np.inf, -np.inf):
+        w["lm_head"][5, 0] = value
+        m = cas.Model(shape, max_ctx=128)
+        m.load_weights(w)
+        logits = m.forward([1], [-1])
+        assert np.isinf(logits[0, 5]) and np.isfinite(np.delete(logits[0], 5)).all()
+        signs.add(float(np.sign(logits[0, 5])))
+        if logits[0, 5] > 0:
+            with pytest.raises(cas.CasError, match="row 0 has no distribution") as e:
+                m.logprobs([5])
+            assert e.value.status == cas.ERR_DEVICE
+        else:
+            assert m.logprobs([5])[0][0] == -np.inf
+        m.close()
+    assert len(signs) == 2
