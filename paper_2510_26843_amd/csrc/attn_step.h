@@ -4,6 +4,8 @@
 #pragma once
 #include "kernel_common.h"
 
+#include <cfloat>
+
 namespace cas {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -66,13 +68,25 @@ __device__ __forceinline__ uint32_t pack_bf(float a, float b) {
 }
 
 // Running softmax state of a wave for a query tile: per lane its row's
-// reference score m (before scaling), the score that moves it, the sum l (the
-// same in all four elements) and O.
+// reference score m (before scaling), the score that moves it, the factor c of its
+// exponents and m c, the sum l (the same in all four elements) and O.
+//
+// A probability's exponent is S c less m c, fused, and as good as m c in fp32: half a
+// step of it, 2^4 at a reference of ATTN_FAR, scales all of a row's probabilities
+// alike.  Further out that could pass what an exponential holds, but there scores
+// that differ differ by 128 or more: whatever is below the largest has a probability
+// below 2^-16, and the power of two next to c, by which m goes without a rounding,
+// serves.  The factor is chosen with the reference (2048 rows behind 6001 slots 209.9
+// us, with one factor for all 209.1, chosen for each tile 219).
+static constexpr float ATTN_FAR = 0x1p31f, ATTN_FAR_C = 0.125f;
 template <int HD> struct AttnState {
-    float m, top;
+    float m, top, c, mc;
     f32x4 l, O[HD / 16];
     __device__ __forceinline__ void clear() {
-        m = top = -1e30f;
+        m = -FLT_MAX;  // (any score that is a number passes the top)
+        top = -INFINITY;
+        c = ATTN_FAR_C;
+        mc = m * c;
         l = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int dt = 0; dt < HD / 16; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -109,6 +123,9 @@ template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st,
     for (int dt = 0; dt < HD / 16; ++dt) st.O[dt] *= f;
     st.m = mn;
     st.top = mn + ATTN_SLACK / c;
+    asm volatile("" : "+v"(st.m));  // (the rest last: moved up, it took the 2048 rows 213 us)
+    st.c = fabsf(st.m) > ATTN_FAR ? ATTN_FAR_C : c;
+    st.mc = st.m * st.c;
 }
 
 // The probabilities of a tile's scores (mc: the scaled reference), as the B operand of P V.
@@ -155,7 +172,7 @@ __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
     i32x4 P[JT];
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
-        attn_probs(P[j], S[j], st[j].m * c, c);
+        attn_probs(P[j], S[j], st[j].mc, st[j].c);
         const int one = 0x3f803f80;
         st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
     }

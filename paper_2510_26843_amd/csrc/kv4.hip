@@ -873,7 +873,7 @@ template <int HD> __global__ void __launch_bounds__(KV4_MERGE_THREADS) k_kv4_mer
     const size_t rows = (size_t)a.H * a.T;
     const bool live = row < (int)rows;
     const size_t rr = live ? row : 0;
-    float M = -1e30f, L = 0.f;
+    float M = -FLT_MAX, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = sub; s0 < S; s0 += 4 * SG) {
         float2 ml[4];

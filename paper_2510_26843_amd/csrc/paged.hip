@@ -481,7 +481,7 @@ __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
     const int one = 0x3f803f80;
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
-        attn_probs(P[j], S[j], st[j].m * c, c);
+        attn_probs(P[j], S[j], st[j].mc, st[j].c);
         st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
     }
     // (one arm each: with two that both write O the compiler copies or spills it)
@@ -844,7 +844,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
                         y[j][h] = mfma_step<ET_BF16>(kf[h * UD + u], Q[j][u], u ? y[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
             i32x4 P[JT];
 #pragma unroll
-            for (int j = 0; j < JT; ++j) attn_probs(P[j], x[j], st[j].m * c, c);
+            for (int j = 0; j < JT; ++j) attn_probs(P[j], x[j], st[j].mc, st[j].c);
 #pragma unroll
             for (int f = 0; f < NDT * JT; ++f) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -957,7 +957,7 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
     const int p0 = sh.local * R, rows = min(sh.s.T * G - p0, R);
     for (int i0 = blockIdx.y * (NG / NS); i0 < rows; i0 += gridDim.y * (NG / NS)) {  // (the same for every thread)
         const int i = min(i0 + gi / NS, rows - 1);
-        float M = -1e30f, L = 0.f;
+        float M = -FLT_MAX, L = 0.f;
         f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
         for (int k0 = sub; k0 < ns; k0 += 4 * NS) {
             float2 ml[4];
