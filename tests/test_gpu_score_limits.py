@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2510_26843_amd import cas, synth
-from tests.test_gpu_logprobs import DEV, _logits, _run
+from tests.test_gpu_logprobs import DEV, _check, _logits, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +65,25 @@ def test_a_row_without_a_distribution_is_called_that():
             assert m.logprobs([5])[0][0] == -np.inf
         m.close()
     assert len(signs) == 2
+
+
+@pytest.mark.parametrize("n,V", [(1100, 270000), (600, 20000), (2100, 70000), (513, 32768)])
+def test_parts_of_many_rows(n, V):
+    """Parts of as many chunks as one may have (270000 logits in two), many short rows in
+    parts, rows more than the records' first bound; in scratch of the reported size."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    x = torch.randn((n, V), generator=g, device="cuda", dtype=torch.bfloat16)
+    rows = [0, 1, n // 2, n - 2, n - 1]
+    # the best of some rows in the last chunks of their parts
+    for r, ids in zip(rows, ([V - 1, V - 2, 0], [31 * 8192 + 7, 32 * 8192 - 1, 32 * 8192], [V // 2, 8191, 8192])):
+        for i, best in zip(ids, (9.0, 8.0, 8.0)):
+            if i < V:
+                x[r, i] = best
+    tokens = torch.randint(V, (n, 2), generator=g, device="cuda").cpu().numpy()
+    need = cas.lib().cas_op_logprobs_work_bytes(n, V, 32)
+    room = torch.full((need + (1 << 16),), 77, dtype=torch.uint8, device=DEV)
+    got = _run(x, tokens, 32, work=room[:need])
+    assert (room[need:] == 77).all()
+    assert np.isfinite(got[0]).all() and np.isfinite(got[1]).all() and (got[2] >= 0).all()
+    _check(x[rows], tokens[rows], 32, 1.0, [y[rows] for y in got])
