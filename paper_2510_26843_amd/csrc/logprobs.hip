@@ -22,8 +22,7 @@
 // us, 5.0 TB/s, what a copy reaches); for few rows a chain of waits (a row's first
 // logits 2 us, the join 3.5 us, of which 2 for what other workgroups wrote).
 #include "attn_step.h"
-
-#include <algorithm>
+#include "logprob_plan.h"
 
 namespace cas {
 
@@ -123,9 +122,6 @@ template <int THREADS> __device__ __forceinline__ void lp_tokens(const LogprobAr
     for (int j = threadIdx.x; j < a.m; j += THREADS)
         a.logp[(size_t)row * a.m + j] = r.logp(j < THREADS ? x : lp_token(a, row, j), a.scale);
 }
-
-// A part's record: m, s, u, and its K best: values, then ids.
-static int lp_words(int K) { return 4 + 2 * K; }
 
 // Workgroup = (row, part): chunks [part span, (part + 1) span) of EACH logits per
 // thread.  One part: it gives the row's results itself.  Dynamic LDS: the largest
@@ -451,41 +447,7 @@ __global__ void __launch_bounds__(64) k_logprob_join(const LogprobArgs a, int pa
     }
 }
 
-// A row is walked by one workgroup of 1024 threads, or by workgroups of 256 in
-// parts that k_logprob_join joins.  Measured, fp32 rows, in us:
-// - One of 1024 where that walks a row in few chunks and the rows are about as many
-//   as the CUs: 256 rows of 128256 logits, K = 20, 35 (in parts 45), 128 rows of
-//   32000, K = 5, 11 (12 to 15).  A second round of them costs as much again (320
-//   rows of 32000 22, in parts 19), and few rows leave CUs idle (48 of 128256,
-//   K = 8, 21, in parts 13; but of 32000, one chunk, 64 rows 11 either way).
-// - Parts of chunks of 8192 logits (32 a thread), or of 2048 (8 a thread: twice the
-//   waves on a CU) where those would leave the chip empty (1 row of 128256, K = 5,
-//   9.3 for 10.5), or mostly hold nothing (5000 rows of 1024 21 for 35), and for
-//   many short rows (1501 of 32000 38 for 42; of 128256 128 for 110).
-// - At most 64 parts: a lane of the join each (2 rows of 1000000 14.5, with 489 parts 18.6).
-static constexpr int LP_PARTS = 64;
-static constexpr int LP_SPAN = 32;  // most chunks of a part (at most 32: bits of a word)
-struct LpPlan {
-    int each, threads, parts, span;
-};
-static LpPlan lp_plan(int n, int V) {
-    LpPlan p;
-    const bool whole = n <= 256 && V > 16384 && V <= 131072 && (V <= 32768 || n > 64);
-    const bool small = V <= 8192 || (n > 512 ? V <= 32768 : (int64_t)n * ((V + 8191) / 8192) < 512);
-    p.threads = whole ? 1024 : 256;
-    p.each = whole || !small ? 32 : 8;
-    const int chunk = p.threads * p.each, chunks = (V + chunk - 1) / chunk;
-    const int want = whole ? 1 : std::min({chunks, LP_PARTS, std::max(1, 2048 / n)});
-    p.span = std::min((chunks + want - 1) / want, LP_SPAN);
-    p.parts = (chunks + p.span - 1) / p.span;
-    return p;
-}
-// The records of any call of up to n rows: those of 2048 parts, unless the rows'
-// parts of LP_SPAN chunks are more.
-size_t logprob_work_bytes(int n, int V, int K) {
-    const int64_t most = std::min(LP_PARTS, (V + 2047) / 2048), least = (V + 8192 * LP_SPAN - 1) / (8192 * LP_SPAN);
-    return (size_t)std::max(std::min(n * most, (int64_t)2048), n * least) * lp_words(K) * 4;
-}
+size_t logprob_work_bytes(int n, int V, int K) { return lp_work_bytes(n, V, K); }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s) {
     if (a.n < 1 || a.V < 1 || a.K < 0 || a.K > LP_MAX_K || a.m < 0) return hipErrorInvalidValue;
