@@ -286,8 +286,10 @@ cas_status cas_op_attention_kv4(const void* q, const void* kv4, int32_t ctx_cap,
  *   table:     [n_seqs][table_len] page numbers; slot s of sequence b is slot
  *              s % page_size of page table[b][s / page_size].  Entries past a
  *              sequence's slots are not read.  Sequences may share pages
- *   seq_start: [n_seqs + 1]: sequence b's rows are the rows seq_start[b] ..
- *              seq_start[b + 1] - 1 of the call (none: it takes no part)
+ *   seq_start: [n_seqs + 1], not decreasing: sequence b's rows are the rows
+ *              seq_start[b] .. seq_start[b + 1] - 1 of the call (none, or not
+ *              rows of the call: it takes no part).  Where it decreases some
+ *              rows may be left out; nothing outside the buffers is touched
  *   ctx_len:   [n_seqs] committed slots
  *   nodes:     NULL, or [n_seqs] slots of the sequence's round behind the
  *              committed ones, appended by earlier calls.  Row i of sequence b
