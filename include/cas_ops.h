@@ -353,9 +353,11 @@ cas_status cas_op_paged_append(const cas_paged* cache, const void* q, int64_t ld
  * row that sees no slot gives zeros; one with a score of NaN or +infinity gives
  * NaN, and one that sees a value that is not finite no finite one at its element.
  * A score of -infinity has no weight.
- * Probabilities are rounded to bf16 for the product with the values (each by at
- * most 2^-8 of itself).  The result does not depend on earlier calls or on timing; it may
- * depend in the last bits on the batch.
+ * Probabilities are rounded for the product with the values, each by at most 2^-16
+ * of itself where max_rows (0: n_rows) times n_heads / n_kv_heads is at most 32 (as
+ * in cas_op_attention), and by 2^-8, to bf16, where it is more.  The result does
+ * not depend on earlier calls or on timing; it may depend in the last bits on the
+ * batch.
  * n_heads <= 4096.  work: device scratch of cas_op_attention_paged_work_bytes
  * (...) bytes (0: none is needed, work may be NULL), 16-byte aligned, used by
  * one call at a time.  The size rests on the struct's numbers, not on its arrays.

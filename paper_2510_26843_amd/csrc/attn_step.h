@@ -128,13 +128,19 @@ template <int HD> __device__ __forceinline__ void attn_follow(AttnState<HD>& st,
     st.mc = st.m * st.c;
 }
 
-// The probabilities of a tile's scores (mc: the scaled reference), as the B operand of P V.
-__device__ __forceinline__ void attn_probs(i32x4& P, const f32x4 (&S)[2], float mc, float c) {
+// The probabilities of a tile's scores (mc: the scaled reference), as the B operand of
+// P V: in one bf16 term, off by 2^-8 of each, or in two, the second what the first
+// leaves, off by 2^-16.
+template <int TERMS>
+__device__ __forceinline__ void attn_probs(i32x4 (&P)[TERMS], const f32x4 (&S)[2], float mc, float c) {
+    static_assert(TERMS == 1 || TERMS == 2, "terms");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1)], c, -mc));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1) + 1], c, -mc));
-        P[i] = (int)pack_bf(p0, p1);
+        const uint32_t w = pack_bf(p0, p1);
+        P[0][i] = (int)w;
+        if constexpr (TERMS == 2) P[1][i] = (int)pack_bf(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
     }
 }
 
@@ -144,7 +150,7 @@ __device__ __forceinline__ void attn_probs(i32x4& P, const f32x4 (&S)[2], float 
 // MASKED: vm has the visibility of the lane's 8 slots to its row of each query
 // tile; CARE: values of unseen slots may not be finite.
 // The sum of the (rounded) probabilities is one more row of the PV product.
-template <int HD, int JT, bool MASKED, bool CARE, typename VF, typename NF>
+template <int HD, int JT, bool MASKED, bool CARE, int TERMS = 1, typename VF, typename NF>
 __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], float c, VF V,
                                          const uint32_t (&vm)[JT], NF next) {
     constexpr int NDT = HD / 16;
@@ -169,12 +175,13 @@ __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
         for (int j = 0; j < JT; ++j) attn_follow(st[j], mt[j], c);
     }
     next();
-    i32x4 P[JT];
+    i32x4 P[JT][TERMS];
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
         attn_probs(P[j], S[j], st[j].mc, st[j].c);
         const int one = 0x3f803f80;
-        st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j][k], st[j].l);
     }
 #pragma unroll
     for (int m = 0; m < NDT / 2; ++m) {
@@ -207,7 +214,9 @@ __device__ __forceinline__ void attn_step(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < JT; ++j) st[j].O[2 * m + h] = mfma_step<ET_BF16>(Vf[h], P[j], st[j].O[2 * m + h]);
+            for (int j = 0; j < JT; ++j)
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) st[j].O[2 * m + h] = mfma_step<ET_BF16>(Vf[h], P[j][k], st[j].O[2 * m + h]);
     }
 }
 

@@ -372,9 +372,9 @@ struct PagedAttnArgs {
 };
 // How a call is launched: rows of a query tile, the most units of a kv head, the
 // shares aimed at beyond them (0: no unit is split), the tiles of sequences that
-// are not split, and the bytes of the partial states.
+// are not split, the bf16 terms of a probability, and the bytes of the partial states.
 struct PagedPlan {
-    int R, units, target, whole;
+    int R, units, target, whole, terms;
     size_t work;
 };
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows);

@@ -441,7 +441,7 @@ template <int JT> __device__ __forceinline__ void paged_tops(float (&t)[JT], con
 // those for the first time.  Values that are not finite, which a probability of 0
 // would not hide, show in their products with zeros; looking at their exponents
 // took a decoded token over 500 slots 0.4 us more, 128 rows of a fresh cache 1.3.
-template <int HD, int JT>
+template <int HD, int JT, int TERMS>
 __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT][2], i32x4 (&vf)[HD / 16], uint32_t (&vm)[JT],
                                           bool outside, float c) {
     constexpr int NDT = HD / 16;
@@ -477,19 +477,22 @@ __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
 #pragma unroll
         for (int j = 0; j < JT; ++j) attn_follow(st[j], t[j], c);
     }
-    i32x4 P[JT];
+    i32x4 P[JT][TERMS];
     const int one = 0x3f803f80;
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
         attn_probs(P[j], S[j], st[j].mc, st[j].c);
-        st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j][k], st[j].l);
     }
     // (one arm each: with two that both write O the compiler copies or spills it)
     if (!odd) {
 #pragma unroll
         for (int f = 0; f < NDT; ++f)
 #pragma unroll
-            for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+            for (int j = 0; j < JT; ++j)
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j][k], st[j].O[f]);
     }
     mfma_result_pad();
     if (odd) {  // taken out, and given back as NaN to the rows that see them
@@ -507,7 +510,8 @@ __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
                 const f32x4 n = mfma_step<ET_BF16>(bad, seen[j], f32x4{0.f, 0.f, 0.f, 0.f});
-                st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j][k], st[j].O[f]);
                 mfma_result_pad();
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -548,7 +552,7 @@ __device__ __forceinline__ void paged_scores(f32x4 (&S)[JT][2], const i32x4 (&k)
         }
 }
 
-template <int HD, int JT>
+template <int HD, int JT, int TERMS>
 __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedAttnArgs a, float c) {
     constexpr int UD = HD / 32, DG = HD / 4, NDT = HD / 16, RS = HD + 4, W = PAGED_WAVES, R = 16 * JT;
     const PagedBatch& p = a.p;
@@ -625,7 +629,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
                 look_up(min(lt + 1, w1 - 1));
                 paged_scores<HD, JT>(S, kf, Q);
                 load_k();
-                attn_step<HD, JT, false, false>(st, S, c, V, vm, [] {});
+                attn_step<HD, JT, false, false, TERMS>(st, S, c, V, vm, [] {});
                 load_v();
                 if (++lt >= w1) break;
             }
@@ -636,7 +640,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 #pragma unroll
             for (int j = 0; j < JT; ++j)
                 vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-            paged_end<HD, JT>(st, S, vf, vm, (uint32_t)pid >= (uint32_t)p.n_pages, c);
+            paged_end<HD, JT, TERMS>(st, S, vf, vm, (uint32_t)pid >= (uint32_t)p.n_pages, c);
             mfma_result_pad();
             if (++lt < w1) {
                 look_up(lt);
@@ -842,7 +846,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
 #pragma unroll
                     for (int j = 0; j < JT; ++j)
                         y[j][h] = mfma_step<ET_BF16>(kf[h * UD + u], Q[j][u], u ? y[j][h] : f32x4{0.f, 0.f, 0.f, 0.f});
-            i32x4 P[JT];
+            i32x4 P[JT][1];
 #pragma unroll
             for (int j = 0; j < JT; ++j) attn_probs(P[j], x[j], st[j].mc, st[j].c);
 #pragma unroll
@@ -857,11 +861,11 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
             __builtin_amdgcn_s_setprio(0);
             const int one = 0x3f803f80;
 #pragma unroll
-            for (int j = 0; j < JT; ++j) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j], st[j].l);
+            for (int j = 0; j < JT; ++j) st[j].l = mfma_step<ET_BF16>(i32x4{one, one, one, one}, P[j][0], st[j].l);
 #pragma unroll
             for (int f = 0; f < NDT; ++f)
 #pragma unroll
-                for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j], st[j].O[f]);
+                for (int j = 0; j < JT; ++j) st[j].O[f] = mfma_step<ET_BF16>(vf[f], P[j][0], st[j].O[f]);
             paged_tops<JT>(t, y);
 #pragma unroll
             for (int f = 0; f < (NDT + 1) * JT; ++f) {
@@ -882,7 +886,7 @@ __global__ void __launch_bounds__(64 * PROWS_WAVES, 2) k_paged_rows(const PagedA
 #pragma unroll
             for (int j = 0; j < JT; ++j)
                 vm[j] = paged_vis8(s, tok[j], tile * 32 + 8 * g, tree, an[j][0], an[j][1], a.sink, a.window);
-            paged_end<HD, JT>(st, S, vf, vm, strange && (uint32_t)paged_page(p, s.b, tile) >= (uint32_t)p.n_pages, c);
+            paged_end<HD, JT, 1>(st, S, vf, vm, strange && (uint32_t)paged_page(p, s.b, tile) >= (uint32_t)p.n_pages, c);
             mfma_result_pad();
         };
         // two tiles that every row of the workgroup sees whole
@@ -1007,6 +1011,14 @@ template <int HD> __global__ void __launch_bounds__(PMERGE_THREADS) k_paged_merg
 // 7.5 us, in two shares 9.6), up to 16 on more (128 rows behind 300 slots 11.7 us,
 // split 13.3): a split costs the second kernel's 2.6 us even if it finds nothing,
 // which a table that allows no longer sequence saves too.
+// Probabilities go into the product with the values in two bf16 terms where a sequence
+// has up to 32 packed rows, as in the decoder's attention, and in one where it has more.
+// Up to 32 rows wait for memory: the second term takes 32 decoding sequences 53.5 ->
+// 53.9 us, one row at 131072 slots nothing, at 500 5.9 -> 6.0, 64 sequences of up to
+// 300 8.7 -> 9.1, draft trees of 8 conversations 32.0 -> 32.8.  More rows wait for the
+// matrix cores: 256 at 8000 slots 23 -> 25.4, a chunk of 509 rows among 8 decoding
+// sequences 65.5 -> 84.5, 2048 rows behind 6001 slots 211 -> 287.  Against 64 bits
+// an output is off by 0.0016 of the norm in two terms, its own rounding, by 0.0023 in one.
 static constexpr int PAGED_CUS = 256;
 
 PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
@@ -1014,6 +1026,7 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
     const int64_t most = (int64_t)std::min(max_rows, p.N) * (H / p.Hkv);  // packed rows of a sequence
     const bool few = ((int64_t)p.N * (H / p.Hkv) / 32 + p.B) * p.Hkv <= PAGED_CUS;
     q.R = most <= 16 ? 16 : most <= 32 || (few && (most <= 64 || p.cap <= 8192)) ? 32 : PROWS_R;
+    q.terms = most <= 32 ? 2 : 1;
     q.units = (int)(((int64_t)p.N * (H / p.Hkv)) / q.R) + p.B;
     q.target = (PAGED_CUS * (q.R == PROWS_R ? 2 : 1) + p.Hkv - 1) / p.Hkv;
     q.whole = q.R == 16 ? 32 : 16;
@@ -1025,8 +1038,9 @@ PagedPlan paged_plan(const PagedBatch& p, int H, int max_rows) {
 template <int HD> static hipError_t paged_attn_go(const PagedAttnArgs& a, const PagedPlan& q, float c, hipStream_t s) {
     const PagedBatch& p = a.p;
     const dim3 grid((unsigned)paged_attn_grid(p, q));
-    hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1>, grid, 64 * PAGED_WAVES, s, a, c)
-                   : q.R == 32 ? launch_checked(k_paged_attn<HD, 2>, grid, 64 * PAGED_WAVES, s, a, c)
+    hipError_t e = q.R == 16   ? launch_checked(k_paged_attn<HD, 1, 2>, grid, 64 * PAGED_WAVES, s, a, c)
+                   : q.R == 32 ? launch_checked(q.terms == 2 ? k_paged_attn<HD, 2, 2> : k_paged_attn<HD, 2, 1>, grid,
+                                                64 * PAGED_WAVES, s, a, c)
                                : launch_checked(k_paged_rows<HD>, grid, 64 * PROWS_WAVES, s, a, c);
     if (e != hipSuccess || q.target == 0) return e;
     const unsigned units = (unsigned)std::min(q.units, q.target);
