@@ -18,8 +18,8 @@
 // another, each from a pass over the part.  Everything is ordered by (logit, id),
 // so no order of arrival shows.
 //
-// What bounds it: for many rows the bytes (1501 rows of 128256 logits, K = 20: 154
-// us, 5.0 TB/s, what a copy reaches); for few rows a chain of waits (a row's first
+// What bounds it: for many rows the bytes (1501 rows of 128256 logits, K = 20: 151
+// us, 5.1 TB/s, what a copy reaches); for few rows a chain of waits (a row's first
 // logits 2 us, the join 3.5 us, of which 2 for what other workgroups wrote).
 #include "attn_step.h"
 #include "logprob_plan.h"

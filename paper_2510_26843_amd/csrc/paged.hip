@@ -533,10 +533,12 @@ __device__ __forceinline__ void paged_end(AttnState<HD> (&st)[JT], f32x4 (&S)[JT
 // registers that the MFMA reads: no other wave wants them.
 //
 // What bounds it: 16 rows, memory (32 sequences of up to 8190 slots, 8 heads, 276
-// MB: 53 us, 5.2 TB/s; one of 131072, 537 MB: 105; with keys and values of a tile
-// loaded together 66); 32 rows, of memory at 4 to 5 TB/s, and of the L2s
-// where several units read the same slots; few slots, the waits at the start and the
-// joins (one row over 500 slots 5.9 us, over 1000 7.5, over 4095, in shares, 9.0).
+// MB: 64 us with the join, 4.3 TB/s; one of 131072, 537 MB: 101, 5.3 TB/s.  With keys
+// and values of a tile loaded together the 32 took 66 where this took 54, over inputs
+// of which the memory-side cache keeps a part); 32 rows, memory (trees of 8 sequences,
+// 119 MB: 3.7 TB/s), and the L2s where several units read the same slots; few slots,
+// the waits at the start and the joins (one row over 500 slots 6.0 us, over 1000 7.7,
+// over 4095, in shares, 9.0).
 static constexpr int PAGED_WAVES = 8;
 static_assert(64 * PAGED_WAVES <= PAGED_MOST_THREADS);
 
@@ -703,7 +705,7 @@ __global__ void __launch_bounds__(64 * PAGED_WAVES, 2) k_paged_attn(const PagedA
 // exponentials of the one before it.
 //
 // What bounds it: the matrix cores, at the rate that a large product reaches: 2048
-// rows of 8B heads behind 6001 slots, 236 GFLOP, 209 us, 1130 TFLOP/s (one tile a
+// rows of 8B heads behind 6001 slots, 236 GFLOP, 204 us, 1154 TFLOP/s (one tile a
 // stage, in the compiler's order, 294; 256 rows, four query tiles per wave, 372).
 // Two workgroups share a CU: a tile takes one 0.87 us beside another, 0.57 alone.
 static constexpr int PROWS_WAVES = 4, PROWS_JT = 2, PROWS_R = 16 * PROWS_JT * PROWS_WAVES, PROWS_D = 4;
