@@ -12,7 +12,7 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 
-from .cas import Model, token_ids
+from .cas import ERR_ARG, CasError, Model, token_ids
 
 
 def _top(row: np.ndarray, b: int) -> List[int]:
@@ -43,6 +43,8 @@ def score(model: Model, tokens: Sequence[int], K: int = 0, scale: float = 1.0):
     the place of what the model had committed, a chain of up to max_tree tokens
     per forward, whose rows are scored on the device."""
     t = token_ids(tokens)
+    if t.ndim != 1:
+        raise CasError(ERR_ARG, "score: tokens are those of one text")
     model.set_committed(0)
     parts = []
     for a in range(0, len(t), model.max_tree):

@@ -70,3 +70,12 @@ def test_a_text_without_tokens_has_no_scores(model, K):
     assert logp.shape == entropy.shape == (0,) and ids.shape == best.shape == (0, K)
     one = decode.score(model, [7], K)
     assert [(x.shape, x.dtype) for x in one] == [(x.shape, x.dtype) for x in (logp, entropy, ids, best)]
+
+
+def test_several_texts_at_once_are_refused(model, monkeypatch):
+    """(the first row's tokens would have been scored as each other's continuations)"""
+    seen = []
+    monkeypatch.setattr(model, "forward", lambda t, *a, **kw: seen.append(np.shape(t)))
+    with pytest.raises(cas.CasError) as e:
+        decode.score(model, [[1, 2, 3], [4, 5, 6]])
+    assert e.value.status == cas.ERR_ARG and not seen
